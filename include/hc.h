@@ -406,6 +406,75 @@ hc_status hc_prefill_init(hc_ctx* ctx, hc_layer* layer, const void* kv_prefill, 
                           int32_t* topk_idx, int32_t* base_idx, int32_t* slot_pos, int32_t* ring, void* work,
                           size_t work_bytes, void* stream);
 
+/* ---- In front of the cache: from the projections of a layer to the rows that cache and attention take ------------------
+ * The calls above start from K and V rows that are there and queries that are ready.  These three make them: norms and position
+ * rotation of the projected heads (hc_prefill_rope for a prompt's tokens, hc_append_rope for the decode token) and the prompt's own
+ * attention (hc_prefill_attn).  A prompt, whole or in chunks, goes  hc_prefill_rope -> hc_prefill_attn  layer by layer; then
+ * hc_prefill_init takes the same kv_prefill and the last token's rows of q_out; then every token goes  hc_append_rope ->
+ * hc_decode_attn.  All enqueue-only; no allocation, no waits; may be captured (hc_append_rope as little as hc_append_kv: the host's
+ * copy of the lengths moves with every call).  The structs and HOST arrays are read before a call returns. */
+enum { HC_BF16 = 0, HC_F32 = 1 };
+enum { HC_ROPE_HALF = 0,          /* pairs (i, i + rot_dim/2)                                              */
+       HC_ROPE_INTERLEAVED = 1 }; /* pairs (2i, 2i + 1)                                                    */
+enum { HC_ROPE_LINEAR = 0,        /* every frequency divided by factor (positions interpolated)            */
+       HC_ROPE_BASE = 1,          /* theta multiplied by factor^(rot_dim / (rot_dim - 2))                  */
+       HC_ROPE_BANDS = 2 };       /* by full turns inside `original` positions: at most low: divided by factor; at least
+                                     high: kept; between them the two mixed linearly (low 1, high 4: Llama 3.1;
+                                     low 1, high 32 with gain 0.1 ln(factor) + 1: YaRN)                    */
+/* What happens to a query or key head: y = x (mean(x^2) + eps)^(-1/2) w over its 128 elements (only where w is given), then the pairs of
+ * its first rot_dim elements turn by position * freq[i]:  (u, v) -> gain (u cos - v sin, v cos + u sin).  The elements behind
+ * rot_dim are not turned and not multiplied by gain.  A plain struct: set or change any field. */
+typedef struct {
+    int32_t layout;        /* HC_ROPE_HALF or HC_ROPE_INTERLEAVED                                           */
+    int32_t rot_dim;       /* multiple of 8, 0 (nothing turns) .. 128                                      */
+    float gain;            /* 1 from hc_rope_init                                                          */
+    float eps;             /* 1e-6 from hc_rope_init                                                       */
+    const float* q_norm;   /* dev f32 [128], 16-byte aligned, or NULL (no norm of the queries)             */
+    const float* k_norm;   /* the same for the keys                                                        */
+    double freq[64];       /* radians a position, the first rot_dim/2; at most 1e6 in magnitude            */
+} hc_rope;
+typedef struct {
+    int32_t kind;          /* HC_ROPE_LINEAR, ...                                                          */
+    int32_t original;      /* HC_ROPE_BANDS: context length that the model was trained with                */
+    double factor;         /* >= 1                                                                         */
+    double low, high;      /* HC_ROPE_BANDS: full turns                                                    */
+} hc_rope_scaling;
+/* freq[i] = theta^(-2i / rot_dim), fitted to a longer context by scaling (NULL: not); no norms, gain 1, eps 1e-6.  Host only. */
+hc_status hc_rope_init(hc_rope* out, int32_t layout, int32_t rot_dim, double theta, const hc_rope_scaling* scaling);
+
+/* The tokens of a call are packed: sequence b brings count[b] >= 0 of them, at positions first[b] .. first[b] + count[b] - 1 (HOST arrays
+ * of B; first + count <= max_ctx), sequence after sequence without gaps; T is their sum (T Hq below 2^31; 0: nothing happens).  first[b] > 0: a chunk behind
+ * what earlier calls brought.  At most 128 KV heads.
+ *   q, k, v       dev, in_type HC_BF16 or HC_F32; token t's heads, [Hq][128] or [Hkv][128], at element t * q_stride (k_stride, v_stride):
+ *                 views of one [T][(Hq + 2 Hkv) * 128] product, or tensors of their own.  16-byte aligned, strides multiples of 8
+ *   q_out         dev bf16 [T][Hq][128]: the queries, through norm and rotation
+ *   kv_prefill    dev bf16: K row of position p of head (b, h) at element k_off[b*Hkv+h] + p * 128, through norm and rotation; V row,
+ *                 as it is, at v_off[..] + p * 128 (HOST arrays of B*Hkv, multiples of 8).  Nothing else in it is written
+ * Angles are formed in 64 bits, norms and rotation in 32; one rounding, to bf16.  q_out and kv_prefill must not overlap the inputs. */
+hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                          int64_t v_stride, int32_t in_type, const int32_t* first, const int32_t* count, void* q_out, void* kv_prefill,
+                          const int64_t* k_off, const int64_t* v_off, void* stream);
+
+/* Causal attention of packed tokens over kv_prefill: the token at position p of sequence b sees positions 0 .. p,
+ *     out[t,a,:] = softmax_j( q[t,a,:] . K_{b,h}[j,:] / sqrt(D) ) V_{b,h}[j,:],  h = a / G;   lse[t,a]: log-sum-exp of these logits.
+ *   q      dev bf16 [T][Hq][128] (q_out of hc_prefill_rope);  kv_prefill, k_off, v_off, first, count: as there, rows 0 .. first + count - 1
+ *          of every head present
+ *   out    dev bf16 [T][Hq][128], not q itself;  lse  dev f32 [T][Hq] or NULL
+ *   work   dev, at least hc_prefill_attn_work_bytes(ctx) bytes (enough for every call of this context), 256-byte aligned, scratch:
+ *          two calls that may overlap, captured ones among them, need one each
+ * bf16 products on the matrix cores, everything else 32-bit; the weights are rounded to bf16 for the second product.  A value of V that is
+ * not finite reaches the rows that see it and no others.  One token a sequence is a call like any other: its keys are split over the GPU. */
+size_t hc_prefill_attn_work_bytes(const hc_ctx* ctx);
+hc_status hc_prefill_attn(hc_ctx* ctx, const void* q, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                          const int32_t* count, void* out, float* lse, void* work, size_t work_bytes, void* stream);
+
+/* hc_append_kv from the projections: the decode token of sequence b, at position ctx_b, has its query and key heads put through norm and
+ * rotation; its K and V rows enter every head as hc_append_kv says (same order with other calls, same refusals) and ctx_b grows by
+ * one; the queries go to q_out (dev bf16 [B][Hq][128]) for hc_decode_attn.  q, k, v, strides, in_type: as hc_prefill_rope, one row of heads a
+ * sequence.  kv_arena and host_tier 16-byte aligned. */
+hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
+                         int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* kv_arena, void* host_tier, void* stream);
+
 /* ---- Algorithm 1, the loop over the window's buffered queries at t mod W = 0 (HC_WINDOW_RESCORED) ------
  * Call once per decode step and layer, after hc_decode_attn and BEFORE hc_rep_topk_drift, on the stream
  * of the monitor (hc_decode_step does).  The layer counts the steps of the window: slot = monitored

@@ -26,10 +26,14 @@ EXPORTS = ["hc_create", "hc_destroy", "hc_strerror", "hc_last_error", "hc_layer_
            "hc_append_kv", "hc_rescore_work_bytes", "hc_rescore_work_layout", "hc_rescore_window", "hc_prefill_work_bytes", "hc_prefill_work_layout", "hc_prefill_init",
            "hc_layer_window_slot",
            "hc_layer_set_window_slot", "hc_layer_context",
+           "hc_rope_init", "hc_prefill_rope", "hc_prefill_attn_work_bytes", "hc_prefill_attn", "hc_append_rope",
            "hc_decode_step", "hc_taxonomy", "hc_budgets", "hc_probe_stream_read", "hc_probe_host_copy"]
 
 
 HC_WINDOW_SLIDING, HC_WINDOW_TUMBLING, HC_WINDOW_RESCORED = 0, 1, 2
+HC_BF16, HC_F32 = 0, 1
+HC_ROPE_HALF, HC_ROPE_INTERLEAVED = 0, 1
+HC_ROPE_LINEAR, HC_ROPE_BASE, HC_ROPE_BANDS = 0, 1, 2
 
 
 class hc_config(C.Structure):
@@ -53,6 +57,15 @@ class hc_layer_io(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("layer", "kv_arena", "host_tier", "q", "out", "lse", "rep_logits", "scores",
                                           "topk_idx", "base_idx", "ring", "inter", "flag", "slot_pos", "k_new", "v_new",
                                           "q_window", "rescore_work")] + [("rescore_work_bytes", C.c_size_t)]
+
+
+class hc_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("gain", C.c_float), ("eps", C.c_float), ("q_norm", C.c_void_p),
+                ("k_norm", C.c_void_p), ("freq", C.c_double * 64)]
+
+
+class hc_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("original", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double)]
 
 
 class HcError(RuntimeError):
@@ -120,13 +133,20 @@ def lib():
         L.hc_budgets.argtypes = [i32, vp, vp, i32, i32, i32, vp]
         L.hc_probe_stream_read.argtypes = [vp, C.c_size_t, vp, i32, i32, vp]
         L.hc_probe_host_copy.argtypes = [vp, vp, C.c_size_t, i32, vp]
+        i64 = C.c_int64
+        L.hc_rope_init.argtypes = [vp, i32, i32, C.c_double, vp]
+        L.hc_prefill_rope.argtypes = [vp] * 5 + [i64] * 3 + [i32] + [vp] * 7
+        L.hc_prefill_attn_work_bytes.argtypes = [vp]
+        L.hc_prefill_attn_work_bytes.restype = C.c_size_t
+        L.hc_prefill_attn.argtypes = [vp] * 10 + [C.c_size_t, vp]
+        L.hc_append_rope.argtypes = [vp] * 6 + [i64] * 3 + [i32] + [vp] * 4
         L.hc_layer_context.argtypes = [vp, i32]
         L.hc_layer_context.restype = i32
         L.hc_decode_step.argtypes = [vp, C.POINTER(hc_layer_io), i32, i32, vp, vp]
         for n in EXPORTS:
             if n not in ("hc_strerror", "hc_last_error", "hc_layer_num_reps", "hc_layer_rep_slot",
                          "hc_layer_num_workgroups", "hc_layer_num_partials", "hc_rescore_work_bytes", "hc_prefill_work_bytes",
-                         "hc_layer_window_slot"):
+                         "hc_prefill_attn_work_bytes", "hc_layer_window_slot"):
                 getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -365,6 +385,71 @@ def hc_prefill_init(ctx: int, layer: int, kv_prefill: Ptr, k_src_off, v_src_off,
     vo = (C.c_int64 * n)(*[int(x) for x in v_src_off])
     _check(lib().hc_prefill_init(ctx, layer, _p(kv_prefill), ko, vo, _p(q_last), pool, _p(kv_arena), _p(host_tier), _p(topk_idx),
                                  _p(base_idx), _p(slot_pos), _p(ring), _p(work), work_bytes, _stream(stream)), "hc_prefill_init", ctx)
+
+
+def hc_rope_init(layout: int, rot_dim: int, theta: float, scaling: Optional[hc_rope_scaling] = None, q_norm: Optional[torch.Tensor] = None,
+                 k_norm: Optional[torch.Tensor] = None, eps: Optional[float] = None, gain: Optional[float] = None) -> hc_rope:
+    """The frequencies, and the norms' weights (f32 [128] on the device, kept alive by the struct) as given."""
+    r = hc_rope()
+    _check(lib().hc_rope_init(C.byref(r), layout, rot_dim, float(theta), None if scaling is None else C.byref(scaling)), "hc_rope_init")
+    for w in (q_norm, k_norm):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (128,)):
+            raise ValueError("hc_rope_init: norm weights are f32 [128]")
+    r.q_norm, r.k_norm, r.keep = _p(q_norm), _p(k_norm), (q_norm, k_norm)
+    if eps is not None:
+        r.eps = eps
+    if gain is not None:
+        r.gain = gain
+    return r
+
+
+def _heads(x: torch.Tensor):
+    """(address, elements from token to token, type) of x [tokens, heads, 128], whose heads lie side by side."""
+    kind = {torch.bfloat16: HC_BF16, torch.float32: HC_F32}.get(x.dtype)
+    if kind is None or x.dim() != 3 or x.shape[2] != 128 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != 128):
+        raise ValueError("projected heads are bf16 or f32 [tokens, heads, 128], a token's heads side by side")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0, kind
+
+
+def _qkv(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
+    (qp, qs, qt), (kp, ks, kt), (vp, vs, vt) = _heads(q), _heads(k), _heads(v)
+    if not (qt == kt == vt and q.shape[0] == k.shape[0] == v.shape[0]):
+        raise ValueError("q, k and v are of one type and of as many tokens")
+    return qp, kp, vp, qs, ks, vs, qt
+
+
+def _check_chunks(first, count, k_off, v_off):
+    if len(first) != len(count) or len(k_off) != len(v_off) or len(k_off) % max(1, len(first)):
+        raise ValueError("first and count have a number a sequence, k_off and v_off one a sequence and KV head")
+
+
+def hc_prefill_rope(ctx: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: Sequence[int], count: Sequence[int],
+                    q_out: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], stream=None) -> None:
+    """q [T, Hq, 128], k and v [T, Hkv, 128]: tensors or views with any stride from token to token."""
+    if sum(count) != q.shape[0] or k.shape[1] * len(first) != len(k_off):
+        raise ValueError("hc_prefill_rope: q has another number of tokens than count adds up to, or k_off another than first's sequences and k's heads")
+    _check_chunks(first, count, k_off, v_off)
+    n, m = len(first), len(k_off)
+    _check(lib().hc_prefill_rope(ctx, C.byref(rope), *_qkv(q, k, v), (C.c_int32 * n)(*first), (C.c_int32 * len(count))(*count), _p(q_out), _p(kv_prefill),
+                                 (C.c_int64 * m)(*k_off), (C.c_int64 * len(v_off))(*v_off), _stream(stream)), "hc_prefill_rope", ctx)
+
+
+def hc_prefill_attn_work_bytes(ctx: int) -> int:
+    return int(lib().hc_prefill_attn_work_bytes(ctx))
+
+
+def hc_prefill_attn(ctx: int, q: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], first: Sequence[int], count: Sequence[int], out: Ptr,
+                    lse: Ptr, work: Ptr, work_bytes: int, stream=None) -> None:
+    _check_chunks(first, count, k_off, v_off)
+    n, m = len(first), len(k_off)
+    _check(lib().hc_prefill_attn(ctx, _p(q), _p(kv_prefill), (C.c_int64 * m)(*k_off), (C.c_int64 * len(v_off))(*v_off), (C.c_int32 * n)(*first),
+                                 (C.c_int32 * len(count))(*count), _p(out), _p(lse), _p(work), work_bytes, _stream(stream)), "hc_prefill_attn", ctx)
+
+
+def hc_append_rope(ctx: int, layer: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Ptr, kv_arena: Ptr,
+                   host_tier: Ptr = None, stream=None) -> None:
+    """q [B, Hq, 128], k and v [B, Hkv, 128]: tensors or views with any stride from sequence to sequence."""
+    _check(lib().hc_append_rope(ctx, layer, C.byref(rope), *_qkv(q, k, v), _p(q_out), _p(kv_arena), _p(host_tier), _stream(stream)), "hc_append_rope", ctx)
 
 
 def hc_layer_window_slot(layer: int) -> int:

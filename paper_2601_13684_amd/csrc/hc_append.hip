@@ -63,20 +63,7 @@ __global__ __launch_bounds__(64) void append_kernel(AppendBatch B)
         row[HC_D / 2 + t] = vw;
     }
     __syncthreads();                                             // everyone has read the old table entry
-    if (t == 0) {
-        heads[bh].ctx = pos + 1;
-        if (hd.role == HC_ROLE_FULL) {
-            heads[bh].len = hd.len + 1;
-            if (hd.tail_seg >= 0) segs[hd.tail_seg].row_end = hd.len + 1;
-            if (hd.tail_blk >= 0) blks[hd.tail_blk].first.row_end = hd.len + 1;
-            if (hd.rep_slot >= 0) {
-                RepDev* r = reps + hd.rep_slot;
-                const int hi = r->hi + 1;
-                r->hi = hi;
-                r->nchunk = (hi - r->lo + HC_SEL_CHUNK - 1) / HC_SEL_CHUNK;
-            }
-        }
-    }
+    if (t == 0) hc_advance_head(heads, segs, blks, reps, bh, hd);
 }
 
 }   // namespace

@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <limits.h>
+#include <math.h>
 
 #include <algorithm>
 #include <numeric>
@@ -994,19 +995,19 @@ static hc_status replan(hc_ctx* ctx, hc_layer* L, hipStream_t st)
 }
 
 static hc_status append_check(hc_ctx* ctx, const hc_layer* layer, const void* k_new, const void* v_new, const void* kv_arena,
-                              const void* host_tier)
+                              const void* host_tier, const char* who = "hc_append_kv")
 {
-    if (!layer_ok(layer) || layer->ctx != ctx) return hc_fail(ctx, HC_ESTATE, "hc_append_kv: layer does not belong to this context");
-    if (!k_new || !v_new || !kv_arena) return hc_fail(ctx, HC_EINVAL, "hc_append_kv: null pointer");
+    if (!layer_ok(layer) || layer->ctx != ctx) return hc_fail(ctx, HC_ESTATE, "%s: layer does not belong to this context", who);
+    if (!k_new || !v_new || !kv_arena) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
     if (((uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)kv_arena | (uintptr_t)host_tier) & 3)
-        return hc_fail(ctx, HC_EINVAL, "hc_append_kv: pointers must be 4-byte aligned");
+        return hc_fail(ctx, HC_EINVAL, "%s: pointers must be 4-byte aligned", who);
     for (int i = 0; i < layer->n_heads; ++i) {
         const hc_head_desc& h = layer->hd_host[i];
         const bool grows = h.role == HC_ROLE_FULL || h.role == HC_ROLE_SATELLITE;
         if (h.ctx + 1 > ctx->cfg.max_ctx || (grows && h.ctx + 1 > (h.cap ? h.cap : h.ctx)))
-            return hc_fail(ctx, HC_ESHAPE, "hc_append_kv: head %d has no room for position %d (cap %d, max_ctx %d)", i, h.ctx,
+            return hc_fail(ctx, HC_ESHAPE, "%s: head %d has no room for position %d (cap %d, max_ctx %d)", who, i, h.ctx,
                            h.cap, ctx->cfg.max_ctx);
-        if (h.role == HC_ROLE_SATELLITE && !host_tier) return hc_fail(ctx, HC_EINVAL, "hc_append_kv: host_tier is needed for satellites");
+        if (h.role == HC_ROLE_SATELLITE && !host_tier) return hc_fail(ctx, HC_EINVAL, "%s: host_tier is needed for satellites", who);
     }
     return HC_OK;
 }
@@ -1043,6 +1044,95 @@ extern "C" hc_status hc_append_kv(hc_ctx* ctx, hc_layer* layer, const void* k_ne
     hipStream_t st = (hipStream_t)stream;
     const hc_append_call call{layer, k_new, v_new, kv_arena, host_tier};
     s = hc_launch_append(ctx, 1, &call, st);
+    if (s != HC_OK) return s;
+    return append_done(ctx, layer, st);
+}
+
+// ---- in front of the cache: rotation, prompt attention, append with rotation ----
+static hc_status rope_check(hc_ctx* ctx, const char* who, const hc_rope* r, const hc_rows_in& in, int32_t in_type, const void* q_out)
+{
+    if (!r || !in.q || !in.k || !in.v || !q_out) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
+    if (in_type != HC_BF16 && in_type != HC_F32) return hc_fail(ctx, HC_EINVAL, "%s: in_type %d", who, (int)in_type);
+    if (((uintptr_t)in.q | (uintptr_t)in.k | (uintptr_t)in.v | (uintptr_t)q_out | (uintptr_t)r->q_norm | (uintptr_t)r->k_norm) & 15)
+        return hc_fail(ctx, HC_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if (in.q_stride < 0 || in.k_stride < 0 || in.v_stride < 0 || ((in.q_stride | in.k_stride | in.v_stride) & 7) ||
+        std::max(in.q_stride, std::max(in.k_stride, in.v_stride)) > ((int64_t)1 << 32))
+        return hc_fail(ctx, HC_EINVAL, "%s: strides must be multiples of 8 elements, 0 .. 2^32", who);
+    if (r->layout != HC_ROPE_HALF && r->layout != HC_ROPE_INTERLEAVED) return hc_fail(ctx, HC_EINVAL, "%s: rope layout %d", who, (int)r->layout);
+    if (r->rot_dim < 0 || r->rot_dim > HC_D || r->rot_dim % 8 != 0)
+        return hc_fail(ctx, HC_ESHAPE, "%s: rot_dim %d must be a multiple of 8, 0 .. %d", who, (int)r->rot_dim, HC_D);
+    if (!(r->eps >= 0.f) || !isfinite(r->eps) || !isfinite(r->gain)) return hc_fail(ctx, HC_EINVAL, "%s: eps must be finite and not negative, gain finite", who);
+    for (int i = 0; i < r->rot_dim / 2; ++i)
+        if (!(fabs(r->freq[i]) <= HC_ROPE_MAX_FREQ)) return hc_fail(ctx, HC_EINVAL, "%s: freq[%d] is not a number of at most 1e6", who, i);
+    return HC_OK;
+}
+
+// Packed tokens and the blocks of kv_prefill that they go to or come from; total: how many tokens.
+static hc_status chunk_check(hc_ctx* ctx, const char* who, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                             const int32_t* count, long long* total)
+{
+    const hc_config& c = ctx->cfg;
+    if (!kv_prefill || !k_off || !v_off || !first || !count) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
+    if ((uintptr_t)kv_prefill & 15) return hc_fail(ctx, HC_EINVAL, "%s: kv_prefill must be 16-byte aligned", who);
+    if (c.Hkv > HC_PROMPT_HEADS) return hc_fail(ctx, HC_ESHAPE, "%s: at most %d KV heads", who, HC_PROMPT_HEADS);
+    long long t = 0;
+    for (int b = 0; b < c.B; ++b) {
+        if (first[b] < 0 || count[b] < 0) return hc_fail(ctx, HC_EINVAL, "%s: sequence %d: first and count must not be negative", who, b);
+        if ((int64_t)first[b] + count[b] > c.max_ctx)
+            return hc_fail(ctx, HC_ESHAPE, "%s: sequence %d: %d tokens behind %d are more than max_ctx %d", who, b, (int)count[b], (int)first[b], (int)c.max_ctx);
+        t += count[b];
+    }
+    if (t > INT_MAX / c.Hq) return hc_fail(ctx, HC_ESHAPE, "%s: %lld tokens of %d query heads are more than one call takes", who, t, (int)c.Hq);
+    for (int i = 0; i < c.B * c.Hkv; ++i)
+        if (count[i / c.Hkv] > 0 && (k_off[i] < 0 || v_off[i] < 0 || (k_off[i] & 7) || (v_off[i] & 7)))
+            return hc_fail(ctx, HC_EINVAL, "%s: head %d: offsets must be non-negative multiples of 8 elements", who, i);
+    *total = t;
+    return HC_OK;
+}
+
+extern "C" hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                                     int64_t v_stride, int32_t in_type, const int32_t* first, const int32_t* count, void* q_out, void* kv_prefill,
+                                     const int64_t* k_off, const int64_t* v_off, void* stream)
+{
+    if (!ctx_ok(ctx)) return HC_ESTATE;
+    const hc_rows_in in{q, k, v, q_stride, k_stride, v_stride, in_type == HC_F32};
+    long long tokens = 0;
+    hc_status s = chunk_check(ctx, "hc_prefill_rope", kv_prefill, k_off, v_off, first, count, &tokens);
+    if (s != HC_OK || tokens == 0) return s;                 // (q and the like may be NULL where there are no tokens)
+    s = rope_check(ctx, "hc_prefill_rope", rope, in, in_type, q_out);
+    if (s != HC_OK) return s;
+    return hc_launch_prefill_rope(ctx, rope, in, first, count, q_out, kv_prefill, k_off, v_off, (hipStream_t)stream);
+}
+
+extern "C" size_t hc_prefill_attn_work_bytes(const hc_ctx* ctx) { return ctx_ok(ctx) ? hc_prompt_work_bytes(ctx) : 0; }
+
+extern "C" hc_status hc_prefill_attn(hc_ctx* ctx, const void* q, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                                     const int32_t* count, void* out, float* lse, void* work, size_t work_bytes, void* stream)
+{
+    if (!ctx_ok(ctx)) return HC_ESTATE;
+    long long tokens = 0;
+    const hc_status s = chunk_check(ctx, "hc_prefill_attn", kv_prefill, k_off, v_off, first, count, &tokens);
+    if (s != HC_OK || tokens == 0) return s;
+    if (!q || !out || !work) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: null pointer");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: q and out must be 16-byte aligned");
+    if ((uintptr_t)lse & 3) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: misaligned float pointer");
+    if ((uintptr_t)work & 255) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: work must be 256-byte aligned");
+    if (work_bytes < hc_prompt_work_bytes(ctx))
+        return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: work buffer of %zu bytes, %zu needed", work_bytes, hc_prompt_work_bytes(ctx));
+    return hc_launch_prefill_attn(ctx, q, kv_prefill, k_off, v_off, first, count, out, lse, work, (hipStream_t)stream);
+}
+
+extern "C" hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
+                                    int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* kv_arena, void* host_tier, void* stream)
+{
+    if (!ctx_ok(ctx)) return HC_ESTATE;
+    const hc_rows_in in{q, k, v, q_stride, k_stride, v_stride, in_type == HC_F32};
+    hc_status s = append_check(ctx, layer, k, v, kv_arena, host_tier, "hc_append_rope");
+    if (s == HC_OK) s = rope_check(ctx, "hc_append_rope", rope, in, in_type, q_out);
+    if (s != HC_OK) return s;
+    if (((uintptr_t)kv_arena | (uintptr_t)host_tier) & 15) return hc_fail(ctx, HC_EINVAL, "hc_append_rope: buffers must be 16-byte aligned");
+    hipStream_t st = (hipStream_t)stream;
+    s = hc_launch_append_rope(ctx, layer, rope, in, q_out, kv_arena, host_tier, st);
     if (s != HC_OK) return s;
     return append_done(ctx, layer, st);
 }

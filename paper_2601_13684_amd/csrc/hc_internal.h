@@ -224,6 +224,23 @@ __device__ __forceinline__ uint32_t hc_score_key(float s)
     if (u == 0x80000000u) u = 0u;             // -0 and +0 are the same score
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+// A head's lengths in the device's tables after its next token, by one thread of the kernel that placed the token's rows; hd: the entry as it was.
+__device__ __forceinline__ void hc_advance_head(HeadDev* __restrict__ heads, SegDev* __restrict__ segs, BlkDev* __restrict__ blks,
+                                                RepDev* __restrict__ reps, int bh, const HeadDev& hd)
+{
+    heads[bh].ctx = hd.ctx + 1;
+    if (hd.role == HC_ROLE_FULL) {
+        heads[bh].len = hd.len + 1;
+        if (hd.tail_seg >= 0) segs[hd.tail_seg].row_end = hd.len + 1;
+        if (hd.tail_blk >= 0) blks[hd.tail_blk].first.row_end = hd.len + 1;
+        if (hd.rep_slot >= 0) {
+            RepDev* r = reps + hd.rep_slot;
+            const int hi = r->hi + 1;
+            r->hi = hi;
+            r->nchunk = (hi - r->lo + HC_SEL_CHUNK - 1) / HC_SEL_CHUNK;
+        }
+    }
+}
 #endif
 
 constexpr uint32_t HC_CTX_MAGIC = 0x48435458u;    // "HCTX"
@@ -378,3 +395,17 @@ struct hc_append_call {
     void* tier;            // or nullptr (a layer without satellites)
 };
 hc_status hc_launch_append(hc_ctx* ctx, int n, const hc_append_call* calls, hipStream_t st);
+constexpr double HC_ROPE_MAX_FREQ = 1.0e6;      // radians a position: keeps position * frequency far from the ends of 64 bits
+constexpr int HC_PROMPT_SEQS = 64, HC_PROMPT_HEADS = 128;   // sequences and (sequence, KV head) pairs that a launch over packed tokens has room for
+// Projected rows as a caller hands them in: elements from token to token (from sequence to sequence), 32-bit or bf16.
+struct hc_rows_in {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    bool f32;
+};
+hc_status hc_launch_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const hc_rows_in& in, const int32_t* first, const int32_t* count, void* q_out,
+                                 void* kv, const int64_t* k_off, const int64_t* v_off, hipStream_t st);
+hc_status hc_launch_append_rope(hc_ctx* ctx, const hc_layer* L, const hc_rope* rope, const hc_rows_in& in, void* q_out, void* arena, void* tier, hipStream_t st);
+size_t hc_prompt_work_bytes(const hc_ctx* ctx);
+hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                                 const int32_t* count, void* out, float* lse, void* work, hipStream_t st);

@@ -222,6 +222,15 @@ class LayerRuntime:
                            self.arena, self.tier, self.topk_idx, self.base_idx, self.slot_pos, self.ring, self.prefill_work,
                            self.prefill_work.numel(), stream)
 
+    def prefill_from(self, prompt: "Prompt", q_last: torch.Tensor, pool: int = 1, stream=None) -> None:
+        """The same from a Prompt that has taken all of its tokens; q_last [B, Hq, 128]: the last tokens' rows of its queries."""
+        spec = self.spec
+        if prompt.length != spec.ctx:
+            raise ValueError("the prompt's sequences have other lengths than the layer's")
+        self.kv_prefill, self._k_src, self._v_src = prompt.kv, prompt.k_off, prompt.v_off
+        self.prefill_work = torch.zeros((hc.hc_prefill_work_bytes(self.ctx.handle, self.handle),), dtype=torch.uint8, device=self.ctx.device)
+        self.prefill_init(None, q_last, pool, stream)
+
     def prefill_scores(self) -> dict:
         """{table row of a selecting head: view of the fp32 scores its selection was taken on}."""
         lay = hc.hc_prefill_work_layout(self.ctx.handle, self.handle, self.spec.B * self.spec.Hkv)
@@ -259,6 +268,15 @@ class LayerRuntime:
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, stream=None) -> None:
         """The decode token's K/V rows (bf16 [B, Hkv, D] on the device) enter the cache (hc_append_kv)."""
         hc.hc_append_kv(self.ctx.handle, self.handle, k_new, v_new, self.arena, self.tier, stream)
+
+    def append_rope(self, rope: hc.hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+        """The decode token's projected heads (q [B, Hq, D], k and v [B, Hkv, D], bf16 or f32): norm, rotation and append in one
+        launch (hc_append_rope).  Returns the queries for ``attn``."""
+        if q_out is None:
+            q_out = torch.empty((self.spec.B, self.spec.Hq, D), dtype=torch.bfloat16, device=self.ctx.device)
+        hc.hc_append_rope(self.ctx.handle, self.handle, rope, q, k, v, q_out, self.arena, self.tier, stream)
+        return q_out
 
     def context(self, b: int) -> int:
         return hc.hc_layer_context(self.handle, b)
@@ -302,6 +320,38 @@ class LayerRuntime:
         if self.handle:
             hc.hc_layer_destroy(self.handle)
             self.handle = None
+
+
+class Prompt:
+    """The prompt stage of one layer: a buffer with a K and a V block for every (sequence, KV head), room[b] rows each, that takes the
+    prompt in one or several chunks and attends over what is there."""
+
+    def __init__(self, ctx: Context, room: List[int]):
+        self.ctx = ctx
+        cfg = ctx.cfg
+        self.room, self.length = list(room), [0] * cfg.B
+        self.k_off, self.v_off, off = [], [], 0
+        for rows in self.room:
+            for _ in range(cfg.Hkv):
+                self.k_off.append(off)
+                self.v_off.append(off + rows * D)
+                off += 2 * rows * D
+        self.kv = torch.zeros((off,), dtype=torch.bfloat16, device=ctx.device)
+        self.work = torch.zeros((hc.hc_prefill_attn_work_bytes(ctx.handle),), dtype=torch.uint8, device=ctx.device)
+
+    def chunk(self, rope: hc.hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, count: List[int], stream=None):
+        """The next count[b] tokens of every sequence, packed (q [T, Hq, D], k and v [T, Hkv, D], bf16 or f32): norm and rotation, rows to the
+        buffer, attention.  Returns (queries bf16, outputs bf16 [T, Hq, D], lse [T, Hq])."""
+        if any(n + c > r for n, c, r in zip(self.length, count, self.room)):
+            raise ValueError("a sequence has no room for its chunk")
+        T, Hq, dev = q.shape[0], self.ctx.cfg.Hq, self.ctx.device
+        qr = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
+        out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        hc.hc_prefill_rope(self.ctx.handle, rope, q, k, v, self.length, count, qr, self.kv, self.k_off, self.v_off, stream)
+        hc.hc_prefill_attn(self.ctx.handle, qr, self.kv, self.k_off, self.v_off, self.length, count, out, lse, self.work, self.work.numel(), stream)
+        self.length = [n + c for n, c in zip(self.length, count)]
+        return qr, out, lse
 
 
 class _DeviceInts:
