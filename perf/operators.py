@@ -135,7 +135,7 @@ def _rope_inputs(c, g, T):
 
 def _context(c, max_ctx):
     from paper_2601_13684_amd import binding as hc
-    cfg = hc.hc_config(B=len(_ints(c["first"])), Hq=c["Hkv"] * c["G"], Hkv=c["Hkv"], D=D, max_ctx=(max_ctx + 63) // 64 * 64, max_k=SLOTS, window=1,
+    cfg = hc.hc_config(B=len(_ints(c["first"])), Hq=c["Hkv"] * c["G"], Hkv=c["Hkv"], D=D, max_ctx=(max(max_ctx, SLOTS) + 63) // 64 * 64, max_k=SLOTS, window=1,
                        metric=0, tau_num=4, tau_den=5, agg=0, window_mode=0)
     return Handle(hc.hc_create(cfg), hc.hc_destroy)
 
