@@ -91,6 +91,11 @@ extern "C" hc_status hc_create(const hc_config* cfg, hc_ctx** out)
 
     hc_ctx* c = new (std::nothrow) hc_ctx();
     if (!c) return HC_ENOMEM;
+    c->prompt_scratch = new (std::nothrow) char[hc_prompt_scratch_bytes(*cfg)];
+    if (!c->prompt_scratch) {
+        delete c;
+        return HC_ENOMEM;
+    }
     c->magic = HC_CTX_MAGIC;
     c->cfg = *cfg;
     c->G = G;
@@ -101,6 +106,7 @@ extern "C" hc_status hc_create(const hc_config* cfg, hc_ctx** out)
     hipError_t e = hipGetDevice(&c->device);
     if (e == hipSuccess) e = hipGetDeviceProperties(&prop, c->device);
     if (e != hipSuccess) {
+        delete[] c->prompt_scratch;
         delete c;
         return HC_EHIP;
     }
@@ -122,6 +128,7 @@ extern "C" hc_status hc_create(const hc_config* cfg, hc_ctx** out)
     uint32_t* base = nullptr;
     e = hipMalloc((void**)&base, ws_w * sizeof(uint32_t));
     if (e != hipSuccess) {
+        delete[] c->prompt_scratch;
         delete c;
         return e == hipErrorOutOfMemory ? HC_ENOMEM : HC_EHIP;
     }
@@ -137,6 +144,7 @@ extern "C" hc_status hc_create(const hc_config* cfg, hc_ctx** out)
         }
         if (e != hipSuccess) {
             (void)hipFree(base);
+            delete[] c->prompt_scratch;
             delete c;
             return e == hipErrorOutOfMemory ? HC_ENOMEM : HC_EHIP;
         }
@@ -171,6 +179,7 @@ extern "C" hc_status hc_destroy(hc_ctx* ctx)
     (void)hipFree(ctx->part_acc);
     (void)hipFree(ctx->part_ml);
     (void)hipFree(ctx->part_more);
+    delete[] ctx->prompt_scratch;
     ctx->magic = 0;
     delete ctx;
     return HC_OK;

@@ -132,6 +132,7 @@ struct hc_ctx {
     int32_t* pair_pos = nullptr;   // [HC_MAX_GROUP][B*Hkv][max_k]
     int32_t* npairs = nullptr;     // [HC_MAX_GROUP][B*Hkv]
     int32_t* gather_done = nullptr;// [HC_MAX_GROUP][B*Hkv] zero between launches
+    char* prompt_scratch = nullptr;// host memory in which a call of hc_prefill_attn puts its sequences in order
 };
 
 struct hc_layer {
@@ -407,5 +408,6 @@ hc_status hc_launch_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const hc_rows
                                  void* kv, const int64_t* k_off, const int64_t* v_off, hipStream_t st);
 hc_status hc_launch_append_rope(hc_ctx* ctx, const hc_layer* L, const hc_rope* rope, const hc_rows_in& in, void* q_out, void* arena, void* tier, hipStream_t st);
 size_t hc_prompt_work_bytes(const hc_ctx* ctx);
+size_t hc_prompt_scratch_bytes(const hc_config& cfg);
 hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
                                  const int32_t* count, void* out, float* lse, void* work, hipStream_t st);

@@ -18,6 +18,8 @@
 // under the present one's arithmetic.  A tile lies in blocks of 16 rows by 4 chunks of 16 bytes (a load instruction's kilobyte), chunk c of
 // row r at place c ^ (r / 4 mod 4) of its 64 bytes: the reads of K (16 rows, one chunk) and the transposed reads of V (4 rows, 4 chunks) then
 // both go over all banks once, and all of a wave's reads of a tile are two addresses a lane and an offset that the instruction holds.
+#include <math.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -27,16 +29,16 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int PA_BLK = 256, PA_ROWS = 128;        // four waves of 32 query rows
+constexpr int PA_BLK = 256;                       // four waves, 32 query rows to each
 constexpr int PA_PER_CU = 2;                      // workgroups that a compute unit holds
 constexpr int PA_KEYS = 64;                       // keys of a tile in LDS
 constexpr int PA_TILE = PA_KEYS * HC_D * 2;       // its bytes
@@ -44,20 +46,64 @@ constexpr float PA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // lo
 constexpr float PA_LN2 = 0.6931471805599453f;
 constexpr float PA_SLACK = 8.0f;                  // log2 units: a weight is at most 2^8 before the reference moves
 
+constexpr int PA_SEQS = HC_PROMPT_SEQS, PA_HEADS = HC_PROMPT_HEADS;
 struct PromptSeq {
     int unit_end;          // of the launch's work units, sequence by sequence
     int first, count;      // positions before the chunk, tokens of the chunk
     int tok0;              // its first token among the packed ones
     int tiles, splits;     // tiles of query rows of a KV head; pieces of the keys
+    int tile_end;          // tiles of all heads up to here
 };
 struct PromptArgs {
     const uint16_t *q, *kv;
     uint16_t* out;
     float *lse, *part_acc, *part_ml;
-    int Hkv, n_seq, chunk, tokens;                // chunk: keys of a piece
-    PromptSeq seq[HC_PROMPT_SEQS];
-    int64_t k_off[HC_PROMPT_HEADS], v_off[HC_PROMPT_HEADS];
+    int Hkv, n_seq, chunk;                        // chunk: keys of a piece
+    int n_cu, mirror;                             // compute units; units of the second round, which is dealt out backwards (0: it is not)
+    // what is to be done, and where K and V are: here, or, of more sequences and heads than there is room for here, in the work buffer
+    const PromptSeq* table;
+    const int64_t* table_off;                     // K's, then V's, table_rows of each
+    int table_rows;
+    PromptSeq seq[PA_SEQS];
+    int64_t k_off[PA_HEADS], v_off[PA_HEADS];
 };
+static_assert(sizeof(PromptArgs) <= 4096, "what a launch's arguments have room for");
+// (what comes from the table is the same for all lanes; told so, the compiler keeps it, and what follows from it, in scalar registers)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+__device__ __forceinline__ PromptSeq seq_of(const PromptArgs& a, int i)
+{
+    if (!a.table) return a.seq[i];
+    const PromptSeq s = a.table[i];
+    return PromptSeq{uniform(s.unit_end), uniform(s.first), uniform(s.count), uniform(s.tok0), uniform(s.tiles), uniform(s.splits), uniform(s.tile_end)};
+}
+// First sequence whose `end` is past x, 64 of them looked at at a time.
+template <class End>
+__device__ __forceinline__ int find_seq(const PromptArgs& a, int x, int lane, End end)
+{
+    if (a.n_seq == 1) return 0;
+    int lo = 0, n = a.n_seq;
+    for (;;) {
+        const int step = (n + 63) / 64, last = min((lane + 1) * step, n) - 1;
+        const int skip = __popcll(__builtin_amdgcn_ballot_w64(lane * step < n && end(lo + last) <= x));
+        lo += skip * step;
+        if (step == 1) return lo;
+        n = min(step, n - skip * step);
+    }
+}
+// Entries of the table from a launch's arguments (seq and the offsets hold up to PA_SEQS and PA_HEADS of them).
+__global__ __launch_bounds__(PA_HEADS) void prompt_table_kernel(PromptArgs a, PromptSeq* seq, int n_seq, int64_t* off, int n_off)
+{
+    const int i = threadIdx.x;
+    if (i < n_seq) seq[i] = a.seq[i];
+    if (i < n_off) {
+        off[i] = a.k_off[i];
+        off[a.table_rows + i] = a.v_off[i];
+    }
+}
 
 __device__ __forceinline__ void swap_halves32(uint32_t& x, uint32_t& y)
 {
@@ -75,9 +121,12 @@ __device__ __forceinline__ uint32_t pack2(float x, float y)
 }
 
 // Every wave's loads to LDS have arrived, and every wave is through with the tile before.  (The barrier alone does not wait for them.)
+// `later`: loads issued after these, which are not waited for.
+template <int later = 0>
 __device__ __forceinline__ void tile_ready()
 {
-    __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0)
+    static_assert(later < 16, "the low bits of vmcnt");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | later);   // vmcnt(later)
     __syncthreads();
 }
 
@@ -113,10 +162,22 @@ struct RowState {
     float ref, lim, l;
 };
 
-// Four waves of 32 rows.
-template <int G>
+// A unit is the work of a workgroup.  The first n_cu workgroups go to a compute unit each, the next n_cu beside them: these are dealt out
+// backwards, the lightest beside the heaviest (head by head, so that a head stays with its die).
+__device__ __forceinline__ int mirrored(int block, int n_cu, int second, int Hkv)
+{
+    const int r = block - n_cu;
+    return r >= second ? block : n_cu + (second / Hkv - 1 - r / Hkv) * Hkv + r % Hkv;
+}
+
+// KS = 1: a tile has 128 rows, a wave takes all keys of its 32.  KS = 2: a tile has 64 rows, two waves share 32 of them, one half of every 64
+// keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the traffic into LDS.
+template <int KS>
+constexpr int pa_rows = 128 / KS;
+template <int G, int KS>
 __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 {
+    constexpr int PA_ROWS = pa_rows<KS>;
     // (arrays of their own, so that the compiler sees that a buffer's loads in flight are not what the reads of the other wait for)
     __shared__ __attribute__((aligned(1024))) char sm_k0[PA_TILE], sm_k1[PA_TILE], sm_v0[PA_TILE], sm_v1[PA_TILE];
     __shared__ unsigned long long sm_bad;
@@ -125,10 +186,10 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 
     // which tile, which piece of its keys, which head: the longest sequence's last tiles first, heads fastest, so that the workgroups
     // that stream the same K and V land on the same die
-    const int unit = blockIdx.x;
-    const int si = __popcll(__builtin_amdgcn_ballot_w64(lane < a.n_seq && a.seq[lane].unit_end <= unit));
-    const PromptSeq sq = a.seq[si];
-    int u = unit - (si > 0 ? a.seq[si - 1].unit_end : 0);
+    const int unit = a.mirror > 0 && (int)blockIdx.x >= a.n_cu ? mirrored(blockIdx.x, a.n_cu, a.mirror, a.Hkv) : blockIdx.x;
+    const int si = find_seq(a, unit, lane, [&](int i) { return a.table ? a.table[i].unit_end : a.seq[i].unit_end; });
+    const PromptSeq sq = seq_of(a, si);
+    int u = unit - (sq.unit_end - sq.tiles * sq.splits * a.Hkv);
     const int h = u % a.Hkv;
     u /= a.Hkv;
     const int split = u % sq.splits, tile = sq.tiles - 1 - u / sq.splits;
@@ -140,8 +201,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     const int n_tiles = (key_end - key_begin + PA_KEYS - 1) / PA_KEYS;
     const int n_full = max(0, min(key_end, sq.first + m0 / G + 1) - key_begin) / PA_KEYS;      // tiles that every row sees whole
 
-    // this wave's rows and how far each sees
-    const int w0 = m0 + w * 32;
+    // this wave's rows and how far each sees; its half of the keys
+    const int wr = w % (4 / KS), wk = w / (4 / KS);
+    const int w0 = m0 + wr * 32;
     const int wtok0 = w0 / G;
     const bool idle = wtok0 >= sq.count;
     const int wave_end = sq.first + min((w0 + 31) / G, sq.count - 1) + 1;
@@ -154,8 +216,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         for (int d = 0; d < 8; ++d) Q[d] = *reinterpret_cast<const bf16x8*>(from + 16 * d);
     }
     const int head = si * a.Hkv + h;
-    const char* kb = (const char*)(a.kv + a.k_off[head]) + (size_t)key_begin * (HC_D * 2);
-    const char* vb = (const char*)(a.kv + a.v_off[head]) + (size_t)key_begin * (HC_D * 2);
+    const int64_t k_off = a.table ? uniform(a.table_off[head]) : a.k_off[head], v_off = a.table ? uniform(a.table_off[a.table_rows + head]) : a.v_off[head];
+    const char* kb = (const char*)(a.kv + k_off) + (size_t)key_begin * (HC_D * 2);
+    const char* vb = (const char*)(a.kv + v_off) + (size_t)key_begin * (HC_D * 2);
 
     // loads: instruction i of wave w takes chunks 4 i .. 4 i + 3 of rows 16 w .. 16 w + 15, a lane one of them
     const int ld_row = 16 * w + (lane >> 2), ld_off = ld_row * 256 + ((lane & 3) ^ (lane >> 4)) * 16;
@@ -175,8 +238,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     uint32_t k_at[2], v_at[2];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        k_at[p] = n / 16 * 4096 + n16 * 64 + (((2 * p + hh) ^ (n16 >> 2)) * 16);
-        v_at[p] = (8 * p + 4 * hh + (n16 >> 2)) * 64 + (((2 * (n / 16) + ((n16 & 3) >> 1)) ^ (2 * p + hh)) * 16) + (n16 & 1) * 8;
+        k_at[p] = wk * 8192 + n / 16 * 4096 + n16 * 64 + (((2 * p + hh) ^ (n16 >> 2)) * 16);
+        v_at[p] = wk * 8192 + (8 * p + 4 * hh + (n16 >> 2)) * 64 + (((2 * (n / 16) + ((n16 & 3) >> 1)) ^ (2 * p + hh)) * 16) + (n16 & 1) * 8;
         asm("" : "+v"(k_at[p]), "+v"(v_at[p]));      // (opaque, so that a buffer goes into an instruction's offset and not into registers of its own)
     }
 
@@ -268,7 +331,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         read_k(tile_k, k, F);
         logits(F, S);
         read_v(tile_v, k, F);
-        const int see = min(limit, key_end - 1) - key - 32 * k - 4 * hh;
+        const int see = min(limit, key_end - 1) - key - 32 * (k + wk) - 4 * hh;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (8 * (i / 4) + i % 4 > see) S[i] = -INFINITY;
@@ -282,7 +345,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         using B1 = std::integral_constant<int, 1>;
         load_k(0, B0{});
         load_v(0, B0{});
-        int k_next = 1;                              // first tile of K whose loads are not under way
+        int k_next = 1, v_next = 1;                  // first tiles of K and V whose loads are not under way
         if (n_full > 0) {
             // Tiles that every row sees whole, in steps of 32 keys, three of them at a time: the logits of step i + 1 and the sums of step
             // i - 1 on the matrix cores, between them the weights of step i, which wait for neither.  Operands are read from LDS one
@@ -292,58 +355,119 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             f32x16 S0, S1;
             bf16x8 P0[2]{}, P1[2], K[8], V[8];
             if (n_tiles > 1) load_k(1, B1{});
-            tile_ready();
-            read_k(sm_k0, 0, K);
-            logits(K, S0);
-            read_k(sm_k0, 1, K);
-            settle(largest(S0), P0);
-            logits(K, S1);
-            weights(S0, P0);
-            settle(largest(S1), P0);
-            tile_ready();
-            if (n_tiles > 1) load_v(1, B1{});
-            if (n_tiles > 2) load_k(2, B0{});
-            read_k(sm_k1, 0, K);                     // (of tile 1; nothing comes of it where there is none)
-            // tile t's sums and tile t + 1's logits; vbuf: where V of tile t is, and where K of t + 1 is not
-            auto body = [&](int t, auto vbuf) {
-                char* const tile_k = vbuf() ? sm_k0 : sm_k1;
-                char* const next_k = vbuf() ? sm_k1 : sm_k0;
-                char* const tile_v = vbuf() ? sm_v1 : sm_v0;
-                read_v(tile_v, 0, V);
+            if constexpr (KS == 1) {
+                if (n_tiles > 1) tile_ready<8>();
+                else tile_ready<4>();
+                read_k(sm_k0, 0, K);
                 logits(K, S0);
-                weights(S1, P1);
-                read_k(tile_k, 1, K);
-                values(V, P0);
-                const float top0 = largest(S0);
-                interleave();
-                settle(top0, P1);
-                read_v(tile_v, 1, V);
+                read_k(sm_k0, 1, K);
+                settle(largest(S0), P0);
                 logits(K, S1);
                 weights(S0, P0);
-                interleave_half();
-                tile_ready();
-                if (t + 3 < n_tiles) load(kb, t + 3, tile_k);
-                if (t + 2 < n_tiles) load(vb, t + 2, tile_v);
-                read_k(next_k, 0, K);
-                values(V, P1);
                 settle(largest(S1), P0);
-            };
-            int t = 0;
-            for (; t + 2 < n_full; t += 2) {
-                body(t, B0{});
-                body(t + 1, B1{});
+                tile_ready();
+                if (n_tiles > 1) load_v(1, B1{});
+                if (n_tiles > 2) load_k(2, B0{});
+                read_k(sm_k1, 0, K);                     // (of tile 1; nothing comes of it where there is none)
+                // tile t's sums and tile t + 1's logits; vbuf: where V of tile t is, and where K of t + 1 is not
+                auto body = [&](int t, auto vbuf) {
+                    char* const tile_k = vbuf() ? sm_k0 : sm_k1;
+                    char* const next_k = vbuf() ? sm_k1 : sm_k0;
+                    char* const tile_v = vbuf() ? sm_v1 : sm_v0;
+                    read_v(tile_v, 0, V);
+                    logits(K, S0);
+                    weights(S1, P1);
+                    read_k(tile_k, 1, K);
+                    values(V, P0);
+                    const float top0 = largest(S0);
+                    interleave();
+                    settle(top0, P1);
+                    read_v(tile_v, 1, V);
+                    logits(K, S1);
+                    weights(S0, P0);
+                    interleave_half();
+                    tile_ready();
+                    if (t + 3 < n_tiles) load(kb, t + 3, tile_k);
+                    if (t + 2 < n_tiles) load(vb, t + 2, tile_v);
+                    read_k(next_k, 0, K);
+                    values(V, P1);
+                    settle(largest(S1), P0);
+                };
+                int t = 0;
+                for (; t + 2 < n_full; t += 2) {
+                    body(t, B0{});
+                    body(t + 1, B1{});
+                }
+                if (t + 1 < n_full) {
+                    body(t, B0{});
+                    ++t;
+                }
+                const char* tile_v = t & 1 ? sm_v1 : sm_v0;
+                read_v(tile_v, 0, V);
+                weights(S1, P1);
+                values(V, P0);
+                read_v(tile_v, 1, V);
+                values(V, P1);
+                k_next = n_full + 2;
+                v_next = n_full + 1;
+            } else {
+                // the same with a step a tile: logits of tile t + 1, sums of tile t - 1, weights of tile t
+                if (n_tiles > 1) {
+                    load_v(1, B1{});
+                    tile_ready<12>();
+                } else {
+                    tile_ready<4>();
+                }
+                read_k(sm_k0, 0, K);
+                logits(K, S0);
+                settle(largest(S0), P0);
+                tile_ready();
+                if (n_tiles > 2) load_k(2, B0{});
+                read_k(sm_k1, 0, K);
+                auto body = [&](int t, auto odd, auto start) {
+                    f32x16 &S_now = odd() ? S1 : S0, &S_next = odd() ? S0 : S1;
+                    bf16x8(&P_now)[2] = odd() ? P1 : P0;
+                    bf16x8(&P_last)[2] = odd() ? P0 : P1;
+                    char* const tile_k = odd() ? sm_k1 : sm_k0;          // of K t + 2
+                    char* const spent_k = odd() ? sm_k0 : sm_k1;
+                    char* const tile_v = odd() ? sm_v0 : sm_v1;          // of V t - 1
+                    if (!start()) read_v(tile_v, 0, V);
+                    logits(K, S_next);
+                    weights(S_now, P_now);
+                    interleave_half();
+                    tile_ready();
+                    if (t + 3 < n_tiles) load(kb, t + 3, spent_k);
+                    if (!start() && t + 1 < n_tiles) load(vb, t + 1, tile_v);
+                    read_k(tile_k, 0, K);
+                    if (!start()) values(V, P_last);
+                    settle(largest(S_next), P_now);
+                };
+                int t = 0;
+                if (n_full > 1) body(t++, B0{}, std::true_type{});
+                for (; t + 2 < n_full; t += 2) {
+                    body(t, B1{}, std::false_type{});
+                    body(t + 1, B0{}, std::false_type{});
+                }
+                if (t + 1 < n_full) {
+                    body(t, B1{}, std::false_type{});
+                    ++t;
+                }
+                // t == n_full - 1: its logits are there, and the weights of tile t - 1 if there is one
+                char *const tile_v = t & 1 ? sm_v1 : sm_v0, *const other_v = t & 1 ? sm_v0 : sm_v1;
+                if (t > 0) {
+                    read_v(other_v, 0, V);
+                    if (t & 1) values(V, P0);
+                    else values(V, P1);
+                }
+                if (t & 1) weights(S1, P1);
+                else weights(S0, P1);
+                tile_ready();
+                if (t > 0 && t + 1 < n_tiles) load(vb, t + 1, other_v);
+                read_v(tile_v, 0, V);
+                values(V, P1);
+                k_next = n_full + 2;
+                v_next = n_full + 1;
             }
-            if (t + 1 < n_full) {
-                body(t, B0{});
-                ++t;
-            }
-            const char* tile_v = t & 1 ? sm_v1 : sm_v0;
-            read_v(tile_v, 0, V);
-            weights(S1, P1);
-            values(V, P0);
-            read_v(tile_v, 1, V);
-            values(V, P1);
-            k_next = n_full + 2;
         }
         tile_ready();
         // The tiles behind them, in which some row sees only the first keys.
@@ -351,11 +475,11 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             const int key = key_begin + t * PA_KEYS;
             if (t + 1 < n_tiles) {
                 if (t + 1 >= k_next) load_k(t + 1, std::integral_constant<int, 1 - buf()>{});
-                load_v(t + 1, std::integral_constant<int, 1 - buf()>{});
+                if (t + 1 >= v_next) load_v(t + 1, std::integral_constant<int, 1 - buf()>{});
             }
             if (!idle && key < wave_end) {
-                masked(buf() ? sm_k1 : sm_k0, buf() ? sm_v1 : sm_v0, key, 0);
-                masked(buf() ? sm_k1 : sm_k0, buf() ? sm_v1 : sm_v0, key, 1);
+#pragma unroll
+                for (int k = 0; k < 2 / KS; ++k) masked(buf() ? sm_k1 : sm_k0, buf() ? sm_v1 : sm_v0, key, k);
             }
             tile_ready();
         };
@@ -397,8 +521,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 __syncthreads();
                 if (!idle && key < wave_end) {
 #pragma unroll 1
-                    for (int k = 0; k < 2; ++k) masked(sm_k0, sm_v0, key, k);
-                    for (unsigned long long bad = sm_bad; bad; bad &= bad - 1) {
+                    for (int k = 0; k < 2 / KS; ++k) masked(sm_k0, sm_v0, key, k);
+                    for (unsigned long long bad = KS == 1 ? sm_bad : sm_bad & (0xffffffffull << (32 * wk)); bad; bad &= bad - 1) {
                         const int j = __builtin_ctzll(bad), at = min(key + j, key_end - 1);
                         const uint16_t* from = (const uint16_t*)(vb + (size_t)(at - key_begin) * (HC_D * 2)) + 4 * hh;
                         const bool sees = key + j == at && at <= limit;
@@ -420,9 +544,34 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 
     float l = row.l;
     l += other_half(l);
+    if constexpr (KS == 2) {
+        // the upper half's sums to the wave that has the lower half (the tiles' places are free: a barrier ended the last of them)
+        f32x4* const o = reinterpret_cast<f32x4*>(wr ? sm_k1 : sm_k0) + lane;
+        RowState* const other = reinterpret_cast<RowState*>(sm_v0) + wr * 64 + lane;
+        if (wk) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i * 64] = f32x4{O[i / 4][4 * (i % 4)], O[i / 4][4 * (i % 4) + 1], O[i / 4][4 * (i % 4) + 2], O[i / 4][4 * (i % 4) + 3]};
+            *other = RowState{row.ref, row.lim, l};
+        }
+        __syncthreads();
+        if (wk) return;
+        const RowState x = *other;
+        const bool mine = row.lim != -INFINITY, has = x.lim != -INFINITY;
+        const float ref = mine && has ? fmaxf(row.ref, x.ref) : mine ? row.ref : x.ref;
+        const float f = mine ? __builtin_amdgcn_exp2f(row.ref - ref) : 0.f, g = has ? __builtin_amdgcn_exp2f(x.ref - ref) : 0.f;
+        l = l * f + x.l * g;
+        row.ref = ref;
+        row.lim = fmaxf(row.lim, x.lim);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const f32x4 y = o[i * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[i / 4][4 * (i % 4) + e] = O[i / 4][4 * (i % 4) + e] * f + y[e] * g;
+        }
+    }
     int late = tid;                                  // (opaque: what follows is not worked out before the loops and kept through them)
     asm volatile("" : "+v"(late));
-    const int r = w * 32 + (late & 31), half = (late >> 5) & 1;
+    const int r = wr * 32 + (late & 31), half = (late >> 5) & 1;
     if (m0 + r >= sq.count * G) return;
     if (sq.splits == 1) {
         const float f = 1.0f / l;
@@ -440,128 +589,259 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             }
         if (a.lse && half == 0) a.lse[row_out] = (row.ref + __builtin_amdgcn_logf(l)) * PA_LN2;
     } else {
-        const size_t at = (size_t)unit * PA_ROWS + r;
-        float* to = a.part_acc + at * HC_D + 4 * half;
+        // as the registers lie: 1 KB to a store
+        f32x4* to = reinterpret_cast<f32x4*>(a.part_acc) + ((size_t)unit * (PA_ROWS / 32) + wr) * 1024 + (late & 63);
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(to + 32 * d + 8 * i) = f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
-        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{row.lim == -INFINITY ? -INFINITY : row.ref, l};
+        for (int i = 0; i < 16; ++i) to[i * 64] = f32x4{O[i / 4][4 * (i % 4)], O[i / 4][4 * (i % 4) + 1], O[i / 4][4 * (i % 4) + 2], O[i / 4][4 * (i % 4) + 3]};
+        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((size_t)unit * PA_ROWS + r) * 2) = f32x2{row.lim == -INFINITY ? -INFINITY : row.ref, l};
     }
 }
 
-// The pieces of a row's keys together: a wave per row of (token, query head), two dimensions a lane.
-template <int G>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a)
+// The pieces of the keys together, for 32 rows of a tile and 32 of their dimensions: wave v takes pieces v, v + PJ_WAVES, ..., PJ_AHEAD of them at a
+// time (what bounds this kernel is how long a read takes, not how much there is to read), a lane what the same lane of the attention kernel's wave
+// left: row lane % 32, four times four dimensions.  The waves' sums meet in LDS.
+constexpr int PJ_WAVES = 8, PJ_AHEAD = 4;
+template <int G, int KS>
+__global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int token = row / (a.Hkv * G), x = row - token * (a.Hkv * G), h = x / G, g = x - h * G;
-    if (token >= a.tokens) return;
-    const int si = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.n_seq && token >= a.seq[lane].tok0 && token < a.seq[lane].tok0 + a.seq[lane].count));
-    const PromptSeq sq = a.seq[si];
+    constexpr int PA_ROWS = pa_rows<KS>;
+    __shared__ f32x4 sm_o[PJ_WAVES][4][64];
+    __shared__ f32x2 sm_ml[PJ_WAVES][32];
+    const int tid = threadIdx.x, v = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
+    const int dims = blockIdx.x % 4, block = blockIdx.x / 4 % (PA_ROWS / 32);
+    int u = blockIdx.x / 4 / (PA_ROWS / 32);                 // tile by tile, as the units but for the pieces
+    const PromptSeq sq = seq_of(a, find_seq(a, u, lane, [&](int i) { return a.table ? a.table[i].tile_end : a.seq[i].tile_end; }));
     if (sq.splits == 1) return;
-    const int r = (token - sq.tok0) * G + g, tile = r / PA_ROWS;
+    u -= sq.tile_end - sq.tiles * a.Hkv;
+    int unit0 = sq.unit_end - sq.tiles * sq.splits * a.Hkv;
+    const int h = u % a.Hkv, tile = u / a.Hkv, w0 = tile * PA_ROWS + block * 32;
+    if (w0 >= sq.count * G) return;
     const int last_tok = min((tile * PA_ROWS + PA_ROWS - 1) / G, sq.count - 1);
     const int pieces = (sq.first + last_tok + a.chunk) / a.chunk;          // those that have a key of the tile
-    const int unit0 = (si > 0 ? a.seq[si - 1].unit_end : 0) + (sq.tiles - 1 - tile) * sq.splits * a.Hkv + h;
-    const size_t step = (size_t)a.Hkv * PA_ROWS, at = (size_t)unit0 * PA_ROWS + r % PA_ROWS;
-    float M = -INFINITY;
-    for (int s = lane; s < pieces; s += 64) M = fmaxf(M, a.part_ml[(at + s * step) * 2]);
+    unit0 += (sq.tiles - 1 - tile) * sq.splits * a.Hkv + h;
+    const bool row = w0 + n < sq.count * G;
+    float ref = -INFINITY, l = 0.f;
+    f32x4 o[4];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    const float ref = M == -INFINITY ? 0.f : M;
-    float l = 0.f;
-    f32x2 o{0.f, 0.f};
-    for (int s = 0; s < pieces; ++s) {
-        const size_t p = at + s * step;
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + p * 2);
-        const f32x2 v = *reinterpret_cast<const f32x2*>(a.part_acc + p * HC_D + 2 * lane);
-        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-        l = fmaf(ml.y, f, l);
-        o.x = fmaf(v.x, f, o.x);
-        o.y = fmaf(v.y, f, o.y);
+    for (int i = 0; i < 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (row)
+        for (int s0 = v; s0 < pieces; s0 += PJ_WAVES * PJ_AHEAD) {
+            f32x2 ml[PJ_AHEAD];
+            f32x4 x[PJ_AHEAD][4];
+#pragma unroll
+            for (int k = 0; k < PJ_AHEAD; ++k) {
+                const int s = s0 + k * PJ_WAVES;
+                const size_t unit = unit0 + (size_t)min(s, pieces - 1) * a.Hkv;
+                ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + (unit * PA_ROWS + block * 32 + n) * 2);
+                if (s >= pieces) ml[k] = f32x2{-INFINITY, 0.f};
+                const f32x4* from = reinterpret_cast<const f32x4*>(a.part_acc) + (unit * (PA_ROWS / 32) + block) * 1024 + dims * 256 + lane;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[k][i] = from[i * 64];
+            }
+            float next = ref;
+#pragma unroll
+            for (int k = 0; k < PJ_AHEAD; ++k) next = fmaxf(next, ml[k].x);
+            const float zero = next == -INFINITY ? 0.f : next, f = __builtin_amdgcn_exp2f(ref - zero);
+            ref = next;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] *= f;
+#pragma unroll
+            for (int k = 0; k < PJ_AHEAD; ++k) {
+                if (s0 + k * PJ_WAVES >= pieces) break;      // (the last piece once more: an infinity times nothing must not count)
+                const float g = __builtin_amdgcn_exp2f(ml[k].x - zero);
+                l = fmaf(ml[k].y, g, l);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i][e] = fmaf(x[k][i][e], g, o[i][e]);
+            }
+        }
+    if (half == 0) sm_ml[v][n] = f32x2{ref, l};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sm_o[v][i][lane] = o[i];
+    __syncthreads();
+    if (v >= 4 || !row) return;                              // wave v: the v-th four dimensions
+    float top = -INFINITY;
+    for (int p = 0; p < PJ_WAVES; ++p) top = fmaxf(top, sm_ml[p][n].x);
+    const float zero = top == -INFINITY ? 0.f : top;
+    l = 0.f;
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < PJ_WAVES; ++p) {
+        const float f = __builtin_amdgcn_exp2f(sm_ml[p][n].x - zero);
+        l = fmaf(sm_ml[p][n].y, f, l);
+        x += sm_o[p][v][lane] * f;
     }
-    const float f = 1.0f / l;
-    reinterpret_cast<uint32_t*>(a.out + (size_t)row * HC_D)[lane] = pack2(o.x * f, o.y * f);
-    if (a.lse && lane == 0) a.lse[row] = (ref + __builtin_amdgcn_logf(l)) * PA_LN2;
+    const float inv = 1.0f / l;
+    const size_t at = ((size_t)(sq.tok0 + (w0 + n) / G) * a.Hkv + h) * G + (w0 + n) % G;
+    *reinterpret_cast<u32x2*>(a.out + at * HC_D + dims * 32 + v * 8 + 4 * half) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
+    if (a.lse && half == 0 && v == 0 && dims == 0) a.lse[at] = (zero + __builtin_amdgcn_logf(l)) * PA_LN2;
 }
 
-template <int G>
-void launch(const PromptArgs& a, int units, bool join, hipStream_t st)
+template <int G, int KS>
+void launch(const PromptArgs& a, int units, bool join, int tiles, hipStream_t st)
 {
-    prompt_attn_kernel<G><<<dim3(units), dim3(PA_BLK), 0, st>>>(a);
-    if (join) prompt_join_kernel<G><<<dim3((a.tokens * a.Hkv * G + 3) / 4), dim3(256), 0, st>>>(a);
+    prompt_attn_kernel<G, KS><<<dim3(units), dim3(PA_BLK), 0, st>>>(a);
+    if (join) prompt_join_kernel<G, KS><<<dim3(tiles * (pa_rows<KS> / 32) * 4), dim3(PJ_WAVES * 64), 0, st>>>(a);
 }
+
+struct PromptPlan {
+    int ks, chunk;         // waves to 32 rows, keys of a piece
+};
+// How long a call takes, in microseconds, if 128 / ks rows make a tile and `chunk` keys a piece; < 0: that is more units than are worth looking
+// at, or than the work buffer has room for.  What a tile of 64 keys takes a compute unit (0.94 us for 128 rows, 0.55 for 64, 15 %
+// more if it has one workgroup alone) and a workgroup (0.93 and 0.60), what memory gives (5.4 TB/s to 256 workgroups and more), what a workgroup needs before its first product (4 us),
+// and what the join costs, are measured.
+float plan_cost(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int ks, int chunk, int slots)
+{
+    const int rows = 128 / ks;
+    float work = 0.f, units = 0.f, longest = 0.f, kv = 0.f, parts = 0.f;
+    long long room = 0;
+    bool split = false;
+    for (int i = 0; i < n; ++i) {
+        const int b = order[i];
+        const float f = (float)first[b], c = (float)count[b], mean = f + 0.5f * c;
+        const long long t = ((long long)count[b] * G + rows - 1) / rows * Hkv, s = ((long long)first[b] + count[b] + chunk - 1) / chunk;
+        room += t * s;
+        work += t * (mean / PA_KEYS + 0.5f);
+        const float active = s > 1 ? t * std::min((float)s, std::max(1.f, mean / chunk + 0.5f)) : (float)t;
+        units += active;
+        longest = std::max(longest, std::min((float)chunk, f + c) / PA_KEYS);
+        kv += (f + c) * Hkv * 512.f;
+        if (s > 1) {
+            split = true;
+            parts += active * std::min(rows, count[b] * G) * 520.f;
+        }
+    }
+    if (split && (room * rows > (long long)2 * slots * 128 || units > 2.5f * slots)) return -1.f;
+    // pieces are of one length, so that compute units have one more or one less of them; and those beyond what the GPU holds at a time
+    // come when the others have ended, to a GPU that is otherwise idle
+    const float cus = 0.5f * slots, last = units - floorf((units - 1.f) / slots) * slots;
+    const float uneven = split ? ceilf(units / cus) / (units / cus) : 1.f;
+    const float arithmetic = std::max(work * (ks == 1 ? 0.94f : 0.55f) / cus * uneven * (units <= cus ? 1.15f : 1.f), longest * (ks == 1 ? 0.93f : 0.60f));
+    const float read = kv / 5.4e6f * (1.f + 0.12f * (uneven - 1.f));
+    const float memory = units > slots ? read * (1.f - last / units) + std::max(read * last / units, longest * 0.9f) : read / std::min(1.f, units / cus);
+    return std::max(arithmetic, memory) + (units > slots ? 8.f : 4.f) + (split ? 6.f + parts * (2.f / 4.5e6f) : 0.f);
+}
+PromptPlan make_plan(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int slots)
+{
+    PromptPlan best{1, 1 << 30};
+    float cost = plan_cost(n, order, first, count, G, Hkv, 1, 1 << 30, slots);
+    const int longest = first[order[0]] + count[order[0]];
+    for (int ks = 1; ks <= 2; ++ks)
+        for (int pieces = 1; pieces <= 1024 && longest / pieces >= 128; pieces += 1 + pieces / 12) {
+            const int chunk = pieces == 1 ? 1 << 30 : ((longest + pieces - 1) / pieces + PA_KEYS - 1) / PA_KEYS * PA_KEYS;
+            const float c = plan_cost(n, order, first, count, G, Hkv, ks, chunk, slots);
+            if (c < 0.f) break;
+            if (c < cost) {
+                cost = c;
+                best = PromptPlan{ks, chunk};
+            }
+        }
+    return best;
+}
+
+// Rows of partial results that there is room for: two tiles of 128 for every workgroup that the GPU holds at a time.
+size_t part_rows(const hc_ctx* ctx) { return (size_t)2 * PA_PER_CU * ctx->n_cu * 128; }
 
 }   // namespace
 
-// Partial results of the keys' pieces: at most two tiles for every workgroup that the GPU holds at a time.
-size_t hc_prompt_work_bytes(const hc_ctx* ctx) { return (size_t)2 * PA_PER_CU * ctx->n_cu * PA_ROWS * (HC_D + 2) * sizeof(float); }
+// The work buffer: partial results, then the table.
+struct PromptWork {
+    size_t ml, seq, off, bytes;
+};
+static PromptWork work_of(const hc_ctx* ctx)
+{
+    const size_t rows = part_rows(ctx), B = (size_t)ctx->cfg.B;
+    PromptWork w{};
+    w.ml = rows * HC_D * sizeof(float);
+    w.seq = w.ml + rows * 2 * sizeof(float);
+    w.off = w.seq + (B * sizeof(PromptSeq) + 255) / 256 * 256;
+    w.bytes = w.off + B * ctx->cfg.Hkv * 2 * sizeof(int64_t);
+    return w;
+}
+size_t hc_prompt_work_bytes(const hc_ctx* ctx) { return work_of(ctx).bytes; }
+size_t hc_prompt_scratch_bytes(const hc_config& c) { return (size_t)c.B * (sizeof(PromptSeq) + 2 * sizeof(int)); }
 
 hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
                                  const int32_t* count, void* out, float* lse, void* work, hipStream_t st)
 {
     const hc_config& c = ctx->cfg;
     const int G = ctx->G, slots = PA_PER_CU * ctx->n_cu;
-    const int most = std::min(HC_PROMPT_SEQS, HC_PROMPT_HEADS / c.Hkv);
-    long long tok_done = 0;
-    for (int b0 = 0; b0 < c.B; b0 += most) {
-        const int nb = std::min(most, c.B - b0);
-        PromptArgs a{};
-        int order[HC_PROMPT_SEQS], tok0[HC_PROMPT_SEQS], n = 0;
-        long long tokens = 0, tiles = 0, keys = 0;
-        for (int i = 0; i < nb; ++i) {
-            const int b = b0 + i;
-            tok0[i] = (int)tokens;
-            tokens += count[b];
-            if (count[b] == 0) continue;
-            order[n++] = i;
-            const long long t = ((long long)count[b] * G + PA_ROWS - 1) / PA_ROWS * c.Hkv;
-            tiles += t;
-            keys += t * (first[b] + count[b]);
-        }
-        if (n == 0) continue;
-        std::stable_sort(order, order + n, [&](int x, int y) { return first[b0 + x] + count[b0 + x] > first[b0 + y] + count[b0 + y]; });
-        // fewer tiles than the GPU holds: the keys are cut into pieces, about as many in all as it holds
-        long long chunk = 1 << 30;
-        if (tiles < slots) chunk = std::max<long long>(256, (keys + slots - 1) / slots);
-        a.chunk = (int)((chunk + PA_KEYS - 1) / PA_KEYS * PA_KEYS);
-        long long units = 0;
-        bool join = false;
-        for (int i = 0; i < n; ++i) {
-            const int b = b0 + order[i];
-            PromptSeq& s = a.seq[i];
-            s.first = first[b];
-            s.count = count[b];
-            s.tok0 = tok0[order[i]];
-            s.tiles = (int)(((long long)count[b] * G + PA_ROWS - 1) / PA_ROWS);
-            s.splits = (int)(((long long)first[b] + count[b] + a.chunk - 1) / a.chunk);
-            join |= s.splits > 1;
-            units += (long long)s.tiles * s.splits * c.Hkv;
-            s.unit_end = (int)units;
-            for (int h = 0; h < c.Hkv; ++h) {
-                a.k_off[i * c.Hkv + h] = k_off[b * c.Hkv + h];
-                a.v_off[i * c.Hkv + h] = v_off[b * c.Hkv + h];
-            }
-        }
-        a.q = (const uint16_t*)q + (size_t)tok_done * c.Hq * HC_D;
-        a.out = (uint16_t*)out + (size_t)tok_done * c.Hq * HC_D;
-        a.lse = lse ? lse + (size_t)tok_done * c.Hq : nullptr;
-        a.kv = (const uint16_t*)kv;
-        a.Hkv = c.Hkv;
-        a.n_seq = n;
-        a.tokens = (int)tokens;
-        a.part_acc = (float*)work;
-        a.part_ml = (float*)work + (size_t)2 * slots * PA_ROWS * HC_D;
-        switch (G) {
-        case 1: launch<1>(a, (int)units, join, st); break;
-        case 2: launch<2>(a, (int)units, join, st); break;
-        case 4: launch<4>(a, (int)units, join, st); break;
-        default: launch<8>(a, (int)units, join, st); break;
-        }
-        HC_HIP(ctx, hipGetLastError());
-        tok_done += tokens;
+    const PromptWork lay = work_of(ctx);
+    // the sequences that bring tokens, the longest first
+    PromptSeq* const seq = (PromptSeq*)ctx->prompt_scratch;
+    int *const order = (int*)(seq + c.B), *const tok0 = order + c.B;
+    int n = 0;
+    long long tokens = 0;
+    for (int b = 0; b < c.B; ++b) {
+        tok0[b] = (int)tokens;
+        tokens += count[b];
+        if (count[b] > 0) order[n++] = b;
     }
+    std::sort(order, order + n, [&](int x, int y) { return first[x] + count[x] != first[y] + count[y] ? first[x] + count[x] > first[y] + count[y] : x < y; });
+    const PromptPlan plan = make_plan(n, order, first, count, G, c.Hkv, slots);
+    const int rows = 128 / plan.ks;
+    long long units = 0, tiles = 0;
+    bool join = false;
+    for (int i = 0; i < n; ++i) {
+        const int b = order[i];
+        PromptSeq& s = seq[i];
+        s.first = first[b];
+        s.count = count[b];
+        s.tok0 = tok0[b];
+        s.tiles = (int)(((long long)count[b] * G + rows - 1) / rows);
+        s.splits = (int)(((long long)first[b] + count[b] + plan.chunk - 1) / plan.chunk);
+        join |= s.splits > 1;
+        tiles += (long long)s.tiles * c.Hkv;
+        units += (long long)s.tiles * s.splits * c.Hkv;
+        s.unit_end = (int)units;
+        s.tile_end = (int)tiles;
+    }
+    PromptArgs a{};
+    a.q = (const uint16_t*)q;
+    a.kv = (const uint16_t*)kv;
+    a.out = (uint16_t*)out;
+    a.lse = lse;
+    a.part_acc = (float*)work;
+    a.part_ml = (float*)((char*)work + lay.ml);
+    a.Hkv = c.Hkv;
+    a.n_seq = n;
+    a.chunk = plan.chunk;
+    a.n_cu = ctx->n_cu;
+    a.mirror = !join && ctx->n_cu % c.Hkv == 0 && units > ctx->n_cu ? (int)std::min<long long>(units - ctx->n_cu, ctx->n_cu) : 0;
+    a.table_rows = n * c.Hkv;
+    const bool in_table = n > PA_SEQS || a.table_rows > PA_HEADS;
+    const int most = std::max(1, std::min(PA_SEQS, PA_HEADS / c.Hkv));          // sequences of an upload
+    for (int i0 = 0; i0 < n; i0 += most) {
+        const int m = std::min(most, n - i0);
+        std::copy(seq + i0, seq + i0 + m, a.seq);
+        for (int i = 0; i < m * c.Hkv; ++i) {
+            const size_t from = (size_t)order[i0 + i / c.Hkv] * c.Hkv + i % c.Hkv;
+            a.k_off[i] = k_off[from];
+            a.v_off[i] = v_off[from];
+        }
+        if (in_table) {
+            prompt_table_kernel<<<dim3(1), dim3(PA_HEADS), 0, st>>>(a, (PromptSeq*)((char*)work + lay.seq) + i0, m,
+                                                                   (int64_t*)((char*)work + lay.off) + (size_t)i0 * c.Hkv, m * c.Hkv);
+            HC_HIP(ctx, hipGetLastError());
+        }
+    }
+    if (in_table) {
+        a.table = (const PromptSeq*)((char*)work + lay.seq);
+        a.table_off = (const int64_t*)((char*)work + lay.off);
+    }
+    switch (G * 4 + plan.ks) {
+    case 5: launch<1, 1>(a, (int)units, join, (int)tiles, st); break;
+    case 6: launch<1, 2>(a, (int)units, join, (int)tiles, st); break;
+    case 9: launch<2, 1>(a, (int)units, join, (int)tiles, st); break;
+    case 10: launch<2, 2>(a, (int)units, join, (int)tiles, st); break;
+    case 17: launch<4, 1>(a, (int)units, join, (int)tiles, st); break;
+    case 18: launch<4, 2>(a, (int)units, join, (int)tiles, st); break;
+    case 33: launch<8, 1>(a, (int)units, join, (int)tiles, st); break;
+    default: launch<8, 2>(a, (int)units, join, (int)tiles, st); break;
+    }
+    HC_HIP(ctx, hipGetLastError());
     return HC_OK;
 }
