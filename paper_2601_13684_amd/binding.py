@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence, Union
 
 import torch
@@ -404,34 +405,50 @@ def hc_rope_init(layout: int, rot_dim: int, theta: float, scaling: Optional[hc_r
 
 
 def _heads(x: torch.Tensor):
-    """(address, elements from token to token, type) of x [tokens, heads, 128], whose heads lie side by side."""
-    kind = {torch.bfloat16: HC_BF16, torch.float32: HC_F32}.get(x.dtype)
-    if kind is None or x.dim() != 3 or x.shape[2] != 128 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != 128):
-        raise ValueError("projected heads are bf16 or f32 [tokens, heads, 128], a token's heads side by side")
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0, kind
+    """(address, elements from token to token, tokens) of x [tokens, heads, 128], whose heads lie side by side."""
+    tokens, heads, width = x.shape
+    step, between, one = x.stride()
+    if width != 128 or one != 1 or (between != 128 and heads > 1):
+        raise ValueError("projected heads are [tokens, heads, 128], a token's heads side by side")
+    return x.data_ptr(), step if tokens > 1 else 0, tokens
 
 
 def _qkv(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
-    (qp, qs, qt), (kp, ks, kt), (vp, vs, vt) = _heads(q), _heads(k), _heads(v)
-    if not (qt == kt == vt and q.shape[0] == k.shape[0] == v.shape[0]):
+    kind = q.dtype
+    (qp, qs, nq), (kp, ks, nk), (vp, vs, nv) = _heads(q), _heads(k), _heads(v)
+    if kind is not k.dtype or kind is not v.dtype or nk != nq or nv != nq:
         raise ValueError("q, k and v are of one type and of as many tokens")
-    return qp, kp, vp, qs, ks, vs, qt
+    if kind is torch.bfloat16:
+        return qp, kp, vp, qs, ks, vs, HC_BF16
+    if kind is torch.float32:
+        return qp, kp, vp, qs, ks, vs, HC_F32
+    raise ValueError("projected heads are bf16 or f32")
 
 
-def _check_chunks(first, count, k_off, v_off):
+def _ints(x: Sequence[int], code: str) -> array:
+    """x as C int32 ('i') or int64 ('q'); an array of that type (a caller's that keeps it) as it is."""
+    return x if type(x) is array and x.typecode == code else array(code, x)
+
+
+def _chunks(first, count, k_off, v_off):
+    first, count, k_off, v_off = _ints(first, "i"), _ints(count, "i"), _ints(k_off, "q"), _ints(v_off, "q")
     if len(first) != len(count) or len(k_off) != len(v_off) or len(k_off) % max(1, len(first)):
         raise ValueError("first and count have a number a sequence, k_off and v_off one a sequence and KV head")
+    return first, count, k_off, v_off
+
+
+def _at(x: array) -> int:
+    return x.buffer_info()[0]
 
 
 def hc_prefill_rope(ctx: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: Sequence[int], count: Sequence[int],
                     q_out: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], stream=None) -> None:
     """q [T, Hq, 128], k and v [T, Hkv, 128]: tensors or views with any stride from token to token."""
-    if sum(count) != q.shape[0] or k.shape[1] * len(first) != len(k_off):
+    first, count, k_off, v_off = _chunks(first, count, k_off, v_off)
+    if sum(count) != len(q) or k.shape[1] * len(first) != len(k_off):
         raise ValueError("hc_prefill_rope: q has another number of tokens than count adds up to, or k_off another than first's sequences and k's heads")
-    _check_chunks(first, count, k_off, v_off)
-    n, m = len(first), len(k_off)
-    _check(lib().hc_prefill_rope(ctx, C.byref(rope), *_qkv(q, k, v), (C.c_int32 * n)(*first), (C.c_int32 * len(count))(*count), _p(q_out), _p(kv_prefill),
-                                 (C.c_int64 * m)(*k_off), (C.c_int64 * len(v_off))(*v_off), _stream(stream)), "hc_prefill_rope", ctx)
+    _check(lib().hc_prefill_rope(ctx, C.byref(rope), *_qkv(q, k, v), _at(first), _at(count), _p(q_out), _p(kv_prefill), _at(k_off), _at(v_off),
+                                 _stream(stream)), "hc_prefill_rope", ctx)
 
 
 def hc_prefill_attn_work_bytes(ctx: int) -> int:
@@ -440,10 +457,9 @@ def hc_prefill_attn_work_bytes(ctx: int) -> int:
 
 def hc_prefill_attn(ctx: int, q: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], first: Sequence[int], count: Sequence[int], out: Ptr,
                     lse: Ptr, work: Ptr, work_bytes: int, stream=None) -> None:
-    _check_chunks(first, count, k_off, v_off)
-    n, m = len(first), len(k_off)
-    _check(lib().hc_prefill_attn(ctx, _p(q), _p(kv_prefill), (C.c_int64 * m)(*k_off), (C.c_int64 * len(v_off))(*v_off), (C.c_int32 * n)(*first),
-                                 (C.c_int32 * len(count))(*count), _p(out), _p(lse), _p(work), work_bytes, _stream(stream)), "hc_prefill_attn", ctx)
+    first, count, k_off, v_off = _chunks(first, count, k_off, v_off)
+    _check(lib().hc_prefill_attn(ctx, _p(q), _p(kv_prefill), _at(k_off), _at(v_off), _at(first), _at(count), _p(out), _p(lse), _p(work), work_bytes,
+                                 _stream(stream)), "hc_prefill_attn", ctx)
 
 
 def hc_append_rope(ctx: int, layer: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Ptr, kv_arena: Ptr,

@@ -11,6 +11,7 @@ bytes per position, so that one retrieved position is one contiguous host read.
 """
 from __future__ import annotations
 
+from array import array
 from typing import Dict, List, Optional, Tuple
 
 import torch
@@ -336,6 +337,7 @@ class Prompt:
                 self.k_off.append(off)
                 self.v_off.append(off + rows * D)
                 off += 2 * rows * D
+        self.k_off, self.v_off = array("q", self.k_off), array("q", self.v_off)      # as the library takes them
         self.kv = torch.zeros((off,), dtype=torch.bfloat16, device=ctx.device)
         self.work = torch.zeros((hc.hc_prefill_attn_work_bytes(ctx.handle),), dtype=torch.uint8, device=ctx.device)
 
