@@ -7,8 +7,11 @@
 // product S^T = K Q^T on the matrix cores (v_mfma_f32_32x32x16_bf16), keys along the registers and a query to each lane, so that a
 // row's maximum and sum stay inside a lane but for one exchange between the halves of the wave; and the registers that hold P^T
 // are, rounded to bf16, the second product's operand as they are: O^T = V^T P^T may take the keys of a step in any order as long
-// as both operands do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass with running
-// maximum and sum; the reference moves only when a logit exceeds it by more than 2^PA_SLACK, so that the accumulators are seldom rescaled.
+// as both operands do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
+// A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights, sums and bf16 are
+// floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.  A workgroup
+// that finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that keeps masked infinities
+// and NaNs of V out): what that costs is paid by inputs that need it.
 //
 // P is rounded to bf16 for the matrix cores, to the nearest: the error of an output is that of its 2^-9 per weight, independent
 // from key to key, about what the output's own rounding to bf16 adds.  Sum, maximum, lse and accumulators are 32-bit, the sum
@@ -44,7 +47,10 @@ constexpr int PA_KEYS = 64;                       // keys of a tile in LDS
 constexpr int PA_TILE = PA_KEYS * HC_D * 2;       // its bytes
 constexpr float PA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
 constexpr float PA_LN2 = 0.6931471805599453f;
-constexpr float PA_SLACK = 8.0f;                  // log2 units: a weight is at most 2^8 before the reference moves
+constexpr float PA_SLACK = 8.0f;                  // log2 units: where there is a running maximum, a weight is at most 2^8 before the reference moves
+// Where there is none: what a row's sum of weights lies between (below 2^-60 weights that are lost as denormals might count: 2^24 of 2^-126), and what the
+// magnitudes of a lane's 64 sums add up to (the join adds up to 2^11 of them, of at most 2^24 weights).
+constexpr float PA_LEAST = 0x1p-60f, PA_MOST = 0x1p100f, PA_LARGEST = 0x1p112f;
 
 constexpr int PA_SEQS = HC_PROMPT_SEQS, PA_HEADS = HC_PROMPT_HEADS;
 struct PromptSeq {
@@ -130,34 +136,23 @@ __device__ __forceinline__ void tile_ready()
     __syncthreads();
 }
 
-// How a step's instructions are to follow each other: behind each product operand reads for the next eight and a share of the weights'
+// How the instructions of eight products are to follow each other: behind each of them operand reads for later ones and a share of the weights'
 // arithmetic.
-__device__ __forceinline__ void interleave_half()
-{
-    constexpr int PRODUCT = 0x8, READ = 0x100, VALU = 0x2, TRANS = 0x400;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(PRODUCT, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(VALU, 4, 0);
-        __builtin_amdgcn_sched_group_barrier(TRANS, 2, 0);
-    }
-}
+template <int products, int reads, int valu, int exps>
 __device__ __forceinline__ void interleave()
 {
     constexpr int PRODUCT = 0x8, READ = 0x100, VALU = 0x2, TRANS = 0x400;
-    interleave_half();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(READ, 1, 0);
+    for (int i = 0; i < products; ++i) {
+        if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(READ, reads, 0);
         __builtin_amdgcn_sched_group_barrier(PRODUCT, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(VALU, 4, 0);
-        __builtin_amdgcn_sched_group_barrier(TRANS, 1, 0);
+        if constexpr (valu > 0) __builtin_amdgcn_sched_group_barrier(VALU, valu, 0);
+        if constexpr (exps > 0) __builtin_amdgcn_sched_group_barrier(TRANS, exps, 0);
     }
 }
 
-// The reference and the sum of a lane's row.  ref is a whole number, so that what was weighed against an older one is rescaled exactly,
-// bf16 weights included; lim = ref + PA_SLACK, -inf while the row has seen nothing.
+// The reference and the sum of a lane's row.  ref is a whole number; lim = ref + PA_SLACK where there is a running maximum, -inf while the row has
+// seen nothing.
 struct RowState {
     float ref, lim, l;
 };
@@ -278,23 +273,26 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         for (int i = 0; i < 16; ++i) top = fmaxf(top, S[i]);
         return fmaxf(top, other_half(top)) * PA_SCALE;
     };
-    auto weights = [&](f32x16& S, bf16x8 (&P)[2]) {
+    // keys 8 s .. 8 s + 7 of a lane's 16
+    auto weigh = [&](f32x16& S, bf16x8 (&P)[2], int s) {
+        u32x4 x;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], PA_SCALE, -row.ref));
-        float sum[2] = {S[0], S[1]};
+        for (int i = 8 * s; i < 8 * s + 8; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], PA_SCALE, -row.ref));
+        float sum[2] = {S[8 * s], S[8 * s + 1]};
 #pragma unroll
-        for (int i = 2; i < 16; ++i) sum[i & 1] += S[i];
+        for (int i = 8 * s + 2; i < 8 * s + 8; ++i) sum[i & 1] += S[i];
         row.l += sum[0] + sum[1];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            u32x4 x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = pack2(S[8 * s + 2 * e], S[8 * s + 2 * e + 1]);
-            P[s] = __builtin_bit_cast(bf16x8, x);
-        }
+        for (int e = 0; e < 4; ++e) x[e] = pack2(S[8 * s + 2 * e], S[8 * s + 2 * e + 1]);
+        P[s] = __builtin_bit_cast(bf16x8, x);
     };
-    // Before weights are taken of logits up to `top`; P: weights against the reference so far that O does not hold yet.
-    auto settle = [&](float top, bf16x8 (&P)[2]) {
+    auto weights = [&](f32x16& S, bf16x8 (&P)[2]) {
+        weigh(S, P, 0);
+        weigh(S, P, 1);
+    };
+    auto start = [&](float top) { row.ref = top == -INFINITY ? 0.f : ceilf(top); };
+    // The running maximum of the second try, before weights are taken of logits up to `top`.
+    auto settle = [&](float top) {
         if (!__builtin_amdgcn_ballot_w64(top > row.lim)) return;
         const float ref = row.lim == -INFINITY ? ceilf(top) : fmaxf(row.ref, ceilf(top));
         const bool none = top == -INFINITY && row.lim == -INFINITY;
@@ -308,13 +306,6 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[d][i] *= f;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            u32x4 x = __builtin_bit_cast(u32x4, P[s]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = pack2(__uint_as_float(x[e] << 16) * f, __uint_as_float(x[e] & 0xffff0000u) * f);
-            P[s] = __builtin_bit_cast(bf16x8, x);
-        }
     };
 
     auto clear = [&] {
@@ -324,8 +315,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
     };
-    // The logits of half a tile, -inf where a row does not see the key, and what follows from them.
-    auto masked = [&](const char* tile_k, const char* tile_v, int key, int k) {
+    // The logits of half a tile, -inf where a row does not see the key, and what follows from them; careful: with the running maximum;
+    // otherwise `first` says whether these are the unit's first keys.
+    auto masked = [&](const char* tile_k, const char* tile_v, int key, int k, bool first, auto careful) {
         f32x16 S;
         bf16x8 P[2]{}, F[8];
         read_k(tile_k, k, F);
@@ -335,7 +327,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (8 * (i / 4) + i % 4 > see) S[i] = -INFINITY;
-        settle(largest(S), P);
+        if constexpr (careful()) settle(largest(S));
+        else if (first) start(largest(S));
         weights(S, P);
         values(F, P);
     };
@@ -361,10 +354,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 read_k(sm_k0, 0, K);
                 logits(K, S0);
                 read_k(sm_k0, 1, K);
-                settle(largest(S0), P0);
+                start(largest(S0));
                 logits(K, S1);
                 weights(S0, P0);
-                settle(largest(S1), P0);
                 tile_ready();
                 if (n_tiles > 1) load_v(1, B1{});
                 if (n_tiles > 2) load_k(2, B0{});
@@ -379,19 +371,21 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                     weights(S1, P1);
                     read_k(tile_k, 1, K);
                     values(V, P0);
-                    const float top0 = largest(S0);
-                    interleave();
-                    settle(top0, P1);
+                    interleave<8, 2, 4, 2>();
+                    interleave<8, 1, 4, 0>();
+                    __builtin_amdgcn_sched_barrier(0);
                     read_v(tile_v, 1, V);
                     logits(K, S1);
-                    weights(S0, P0);
-                    interleave_half();
+                    weigh(S0, P0, 0);
+                    interleave<8, 2, 3, 1>();
                     tile_ready();
                     if (t + 3 < n_tiles) load(kb, t + 3, tile_k);
                     if (t + 2 < n_tiles) load(vb, t + 2, tile_v);
                     read_k(next_k, 0, K);
                     values(V, P1);
-                    settle(largest(S1), P0);
+                    weigh(S0, P0, 1);
+                    interleave<8, 1, 3, 1>();
+                    __builtin_amdgcn_sched_barrier(0);
                 };
                 int t = 0;
                 for (; t + 2 < n_full; t += 2) {
@@ -420,27 +414,29 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 }
                 read_k(sm_k0, 0, K);
                 logits(K, S0);
-                settle(largest(S0), P0);
+                start(largest(S0));
                 tile_ready();
                 if (n_tiles > 2) load_k(2, B0{});
                 read_k(sm_k1, 0, K);
-                auto body = [&](int t, auto odd, auto start) {
+                auto body = [&](int t, auto odd, auto begin) {
                     f32x16 &S_now = odd() ? S1 : S0, &S_next = odd() ? S0 : S1;
                     bf16x8(&P_now)[2] = odd() ? P1 : P0;
                     bf16x8(&P_last)[2] = odd() ? P0 : P1;
                     char* const tile_k = odd() ? sm_k1 : sm_k0;          // of K t + 2
                     char* const spent_k = odd() ? sm_k0 : sm_k1;
                     char* const tile_v = odd() ? sm_v0 : sm_v1;          // of V t - 1
-                    if (!start()) read_v(tile_v, 0, V);
+                    if (!begin()) read_v(tile_v, 0, V);
                     logits(K, S_next);
-                    weights(S_now, P_now);
-                    interleave_half();
+                    weigh(S_now, P_now, 0);
+                    interleave<8, 2, 3, 1>();
                     tile_ready();
                     if (t + 3 < n_tiles) load(kb, t + 3, spent_k);
-                    if (!start() && t + 1 < n_tiles) load(vb, t + 1, tile_v);
+                    if (!begin() && t + 1 < n_tiles) load(vb, t + 1, tile_v);
                     read_k(tile_k, 0, K);
-                    if (!start()) values(V, P_last);
-                    settle(largest(S_next), P_now);
+                    if (!begin()) values(V, P_last);
+                    weigh(S_now, P_now, 1);
+                    interleave<8, 1, 3, 1>();
+                    __builtin_amdgcn_sched_barrier(0);
                 };
                 int t = 0;
                 if (n_full > 1) body(t++, B0{}, std::true_type{});
@@ -468,8 +464,15 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 k_next = n_full + 2;
                 v_next = n_full + 1;
             }
+            tile_ready();
+        } else if (n_tiles > 1) {
+            load_k(1, B1{});
+            load_v(1, B1{});
+            k_next = v_next = 2;
+            tile_ready<8>();
+        } else {
+            tile_ready();
         }
-        tile_ready();
         // The tiles behind them, in which some row sees only the first keys.
         auto step = [&](int t, auto buf) {
             const int key = key_begin + t * PA_KEYS;
@@ -479,7 +482,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             }
             if (!idle && key < wave_end) {
 #pragma unroll
-                for (int k = 0; k < 2 / KS; ++k) masked(buf() ? sm_k1 : sm_k0, buf() ? sm_v1 : sm_v0, key, k);
+                for (int k = 0; k < 2 / KS; ++k) masked(buf() ? sm_k1 : sm_k0, buf() ? sm_v1 : sm_v0, key, k, t == 0 && k == 0, std::false_type{});
             }
             tile_ready();
         };
@@ -493,10 +496,12 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z = fmaf(O[d][i], 0.f, z);
-        if (n_full < n_tiles && __syncthreads_or(z != 0.f)) {
-            // Some sum is not finite: what a masked weight of zero makes of an infinity or a NaN in V must not count.  Once more, tile
-            // by tile: such values leave the tile, and are added by hand to the rows that see them.
+            for (int i = 0; i < 16; ++i) z += fabsf(O[d][i]);
+        const float sum = row.l + other_half(row.l);
+        const bool sees = !idle && limit >= key_begin + 32 * wk;                 // any of its wave's keys
+        if (__syncthreads_or(sees && !(z < PA_LARGEST && sum > PA_LEAST && sum < PA_MOST))) {
+            // Once more, tile by tile, with a running maximum.  What a masked weight of zero makes of an infinity or a NaN in V must not count:
+            // such values leave the tile, and are added by hand to the rows that see them.
             clear();
             for (t = 0; t < n_tiles; ++t) {
                 const int key = key_begin + t * PA_KEYS;
@@ -521,7 +526,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 __syncthreads();
                 if (!idle && key < wave_end) {
 #pragma unroll 1
-                    for (int k = 0; k < 2 / KS; ++k) masked(sm_k0, sm_v0, key, k);
+                    for (int k = 0; k < 2 / KS; ++k) masked(sm_k0, sm_v0, key, k, false, std::true_type{});
                     for (unsigned long long bad = KS == 1 ? sm_bad : sm_bad & (0xffffffffull << (32 * wk)); bad; bad &= bad - 1) {
                         const int j = __builtin_ctzll(bad), at = min(key + j, key_end - 1);
                         const uint16_t* from = (const uint16_t*)(vb + (size_t)(at - key_begin) * (HC_D * 2)) + 4 * hh;
@@ -556,12 +561,11 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         __syncthreads();
         if (wk) return;
         const RowState x = *other;
-        const bool mine = row.lim != -INFINITY, has = x.lim != -INFINITY;
+        const bool mine = l != 0.f, has = x.l != 0.f;
         const float ref = mine && has ? fmaxf(row.ref, x.ref) : mine ? row.ref : x.ref;
         const float f = mine ? __builtin_amdgcn_exp2f(row.ref - ref) : 0.f, g = has ? __builtin_amdgcn_exp2f(x.ref - ref) : 0.f;
         l = l * f + x.l * g;
         row.ref = ref;
-        row.lim = fmaxf(row.lim, x.lim);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const f32x4 y = o[i * 64];
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         f32x4* to = reinterpret_cast<f32x4*>(a.part_acc) + ((size_t)unit * (PA_ROWS / 32) + wr) * 1024 + (late & 63);
 #pragma unroll
         for (int i = 0; i < 16; ++i) to[i * 64] = f32x4{O[i / 4][4 * (i % 4)], O[i / 4][4 * (i % 4) + 1], O[i / 4][4 * (i % 4) + 2], O[i / 4][4 * (i % 4) + 3]};
-        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((size_t)unit * PA_ROWS + r) * 2) = f32x2{row.lim == -INFINITY ? -INFINITY : row.ref, l};
+        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((size_t)unit * PA_ROWS + r) * 2) = f32x2{l == 0.f ? -INFINITY : row.ref, l};
     }
 }
 

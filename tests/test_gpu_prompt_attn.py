@@ -109,6 +109,70 @@ def test_growing_logits():
     c.close()
 
 
+# one tile of rows, tiles with and without whole ones in front, pieces of the keys, both tile heights, one row
+SHAPES = [([0], [40], 2, 4), ([0], [700], 2, 1), ([0], [2500], 8, 4), ([9000], [2], 2, 8), ([9000], [64], 8, 4), ([40000], [400], 8, 1), ([20000, 0, 300], [1, 1500, 70], 2, 2)]
+
+
+def per_key(c, offsets, value):
+    """value(position) of every key into the rows at offsets."""
+    for b, (f, n) in enumerate(zip(c.first, c.count)):
+        for h in range(c.Hkv):
+            o = offsets[b * c.Hkv + h]
+            rows = c.kv[o:o + (f + n) * D].view(f + n, D)
+            rows.copy_(value(torch.arange(f + n, device=DEV, dtype=torch.float64), rows))
+
+
+@pytest.mark.parametrize("first,count,Hkv,G", SHAPES)
+@pytest.mark.parametrize("rise", [-0.75, 0.25, 4.0])
+def test_logits_that_rise_with_the_position(first, count, Hkv, G, rise):
+    """By `rise` from key to key (up to 2^17 in all): far beyond what weights against the first keys' largest could hold.  q . K = position * rise * sqrt(128)
+    but for what the other elements bring, each product exact: bf16 steps of the position make two keys of the same logit, as in the oracle."""
+    c = Call(first, count, Hkv, G, seed=5)
+    c.q[..., 1:] = 0
+    c.q[..., 0] = 1
+    per_key(c, c.k_off, lambda at, rows: torch.cat([(at * (rise * math.sqrt(D)))[:, None], rows[:, 1:].double()], 1).to(torch.bfloat16))
+    c.run()
+    torch.cuda.synchronize()
+    o, lse, pv, p2 = c.want()
+    # one product a logit: a weight is off by the rounding of t = s log2(e) / sqrt(128) and of t - ref, 2^-23 |t|, below 2^-4.7 for |t| up to 2^18.3; twice in a ratio.
+    # The keys that count have t within a few binary orders of the row's largest, and errors of the factor are common to all of them
+    # where their logits are equal; what is left is held to the 2^-10 that check_attention gives, plus 2^-22 |s| for unequal ones.
+    tol = 2.0 ** -8 * (pv + o.abs()) + (2.0 ** -10 + 2.0 ** -22 * lse.abs())[..., None] * pv
+    err = (c.out[:c.T].double() - o).abs()
+    assert (err <= tol).all(), float((err - tol).max())
+    assert ((c.lse[:c.T].double() - lse).abs() <= 1e-4 + 1e-6 * lse.abs()).all()
+    c.close()
+
+
+@pytest.mark.parametrize("first,count,Hkv,G", SHAPES)
+def test_first_keys_that_count_for_nothing(first, count, Hkv, G):
+    """Logits of minus infinity at the first 100 keys: rows that see others have these, the rest is 0 / 0."""
+    c = Call(first, count, Hkv, G, seed=6)
+    c.q[..., 3] = 1
+    per_key(c, c.k_off, lambda at, rows: torch.where((torch.arange(D, device=DEV) == 3)[None] & (at < 100)[:, None], -math.inf, rows.double()).to(torch.bfloat16))
+    c.run()
+    torch.cuda.synchronize()
+    o, lse, pv, p2 = c.want()
+    at = torch.cat([torch.arange(f, f + n, device=DEV) for f, n in zip(first, count)])
+    sees = at >= 100
+    assert torch.isnan(c.out[:c.T][~sees].float()).all() and (c.lse[:c.T][~sees] == -math.inf).all()
+    if sees.any():
+        P.check_attention(c.out[:c.T][sees], c.lse[:c.T][sees], tuple(x[sees] for x in (o, lse, pv, p2)), "")
+    c.close()
+
+
+@pytest.mark.parametrize("first,count,Hkv,G", SHAPES)
+def test_the_largest_values(first, count, Hkv, G):
+    """V of up to 2^90, and logits that rise by 60 binary orders at key 200."""
+    c = Call(first, count, Hkv, G, seed=7)
+    c.q[..., 3] = 1
+    per_key(c, c.v_off, lambda at, rows: (rows.double().clamp(-1, 1) * 2.0 ** 90).to(torch.bfloat16))
+    per_key(c, c.k_off, lambda at, rows: torch.where((torch.arange(D, device=DEV) == 3)[None] & (at >= 200)[:, None], 472.0, rows.double()).to(torch.bfloat16))
+    c.run()
+    c.check()
+    c.close()
+
+
 @pytest.mark.parametrize("big", [-2.0 ** 60, 2.0 ** 60])
 def test_logits_far_from_zero(big):
     """A single key far below (above) everything: the running maximum starts there."""
@@ -255,3 +319,48 @@ def test_same_results_every_time():
         torch.cuda.synchronize()
         assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
     c.close()
+
+
+def test_a_long_list_of_sequences_captured():
+    """More sequences than a launch's arguments hold: what a replay needs of them is in the graph and the work buffer."""
+    first, count = [700 * (i % 9) for i in range(90)], [1 + 40 * (i % 4) for i in range(90)]
+    c = Call(first, count, 2, 4)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run()
+    first, count = list(first), list(count)
+    for i in range(3):
+        c.q.copy_(torch.randn_like(c.q.float()).to(torch.bfloat16))
+        c.work.fill_(255)
+        graph.replay()
+        c.check(i)
+        got = c.out.clone()
+        c.run()                                  # eager between the replays, in the same work buffer
+        torch.cuda.synchronize()
+        assert torch.equal(got, c.out)
+    c.close()
+
+
+def test_two_calls_at_once():
+    """Of one context on two streams, a work buffer each; pieces in both."""
+    a, b = Call([30000, 4], [3, 400], 4, 4, seed=1), Call([100, 25000], [900, 70], 4, 4, seed=2)
+    hc.hc_destroy(b.ctx)
+    b.ctx = a.ctx                                # a's room is the larger
+    a.run(), b.run()
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for c in (a, b):
+            c.out.fill_(7)
+            c.work.fill_(255)
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for _ in range(4):
+            a.run(stream=streams[0])
+            b.run(stream=streams[1])
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+    a.check("a")
+    b.check("b")
+    a.close()
