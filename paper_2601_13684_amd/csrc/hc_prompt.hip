@@ -43,6 +43,8 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int PA_BLK = 256;                       // four waves, 32 query rows to each
 constexpr int PA_PER_CU = 2;                      // workgroups that a compute unit holds
+constexpr int PA_DIES = 8;                        // with an L2 each; workgroups go to them in turn
+constexpr int PA_ROOM = 4;                        // tiles of 128 rows of partial results to each of these workgroups
 constexpr int PA_KEYS = 64;                       // keys of a tile in LDS
 constexpr int PA_TILE = PA_KEYS * HC_D * 2;       // its bytes
 constexpr float PA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
@@ -57,14 +59,18 @@ struct PromptSeq {
     int unit_end;          // of the launch's work units, sequence by sequence
     int first, count;      // positions before the chunk, tokens of the chunk
     int tok0;              // its first token among the packed ones
-    int tiles, splits;     // tiles of query rows of a KV head; pieces of the keys
+    int tiles;             // tiles of query rows of a KV head
     int tile_end;          // tiles of all heads up to here
+    uint32_t cut;          // pieces of the keys (low bits), tiles of 64 keys of a piece
+    __host__ __device__ int splits() const { return cut & 0xfff; }
+    __host__ __device__ int chunk() const { return (cut >> 12) * 64; }
 };
 struct PromptArgs {
     const uint16_t *q, *kv;
     uint16_t* out;
     float *lse, *part_acc, *part_ml;
-    int Hkv, n_seq, chunk;                        // chunk: keys of a piece
+    int Hkv, n_seq;
+    int together;                                 // pieces whose tiles alternate, so that one piece of one head stays with one of the eight dies
     int n_cu, mirror;                             // compute units; units of the second round, which is dealt out backwards (0: it is not)
     // what is to be done, and where K and V are: here, or, of more sequences and heads than there is room for here, in the work buffer
     const PromptSeq* table;
@@ -84,7 +90,7 @@ __device__ __forceinline__ PromptSeq seq_of(const PromptArgs& a, int i)
 {
     if (!a.table) return a.seq[i];
     const PromptSeq s = a.table[i];
-    return PromptSeq{uniform(s.unit_end), uniform(s.first), uniform(s.count), uniform(s.tok0), uniform(s.tiles), uniform(s.splits), uniform(s.tile_end)};
+    return PromptSeq{uniform(s.unit_end), uniform(s.first), uniform(s.count), uniform(s.tok0), uniform(s.tiles), uniform(s.tile_end), (uint32_t)uniform((int)s.cut)};
 }
 // First sequence whose `end` is past x, 64 of them looked at at a time.
 template <class End>
@@ -165,6 +171,18 @@ __device__ __forceinline__ int mirrored(int block, int n_cu, int second, int Hkv
     return r >= second ? block : n_cu + (second / Hkv - 1 - r / Hkv) * Hkv + r % Hkv;
 }
 
+// The last pieces of a sequence's tiles have all lengths.  Counted from the last tile, `per` tiles have their ends in one piece's length of keys, and the
+// first of them has the longest: one of every such run in turn.
+__device__ __forceinline__ int last_tile(int i, int tiles, int per)
+{
+    const int runs = (tiles + per - 1) / per;
+    if (runs == 1) return i;
+    const int whole = (tiles - (runs - 1) * per) * runs;         // what comes before the last run, a shorter one, is used up
+    if (i < whole) return i % runs * per + i / runs;
+    i -= whole;
+    return i % (runs - 1) * per + whole / runs + i / (runs - 1);
+}
+
 // KS = 1: a tile has 128 rows, a wave takes all keys of its 32.  KS = 2: a tile has 64 rows, two waves share 32 of them, one half of every 64
 // keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the traffic into LDS.
 template <int KS>
@@ -179,20 +197,40 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, hh = lane >> 5;
 
-    // which tile, which piece of its keys, which head: the longest sequence's last tiles first, heads fastest, so that the workgroups
-    // that stream the same K and V land on the same die
+    // which piece of the keys, which tile, which head: the longest sequence first, its whole pieces and then the last ones of its tiles, heads
+    // fastest, so that the workgroups that stream the same K and V do so at the same time on the same die
     const int unit = a.mirror > 0 && (int)blockIdx.x >= a.n_cu ? mirrored(blockIdx.x, a.n_cu, a.mirror, a.Hkv) : blockIdx.x;
     const int si = find_seq(a, unit, lane, [&](int i) { return a.table ? a.table[i].unit_end : a.seq[i].unit_end; });
     const PromptSeq sq = seq_of(a, si);
-    int u = unit - (sq.unit_end - sq.tiles * sq.splits * a.Hkv);
-    const int h = u % a.Hkv;
-    u /= a.Hkv;
-    const int split = u % sq.splits, tile = sq.tiles - 1 - u / sq.splits;
+    const int unit0 = sq.unit_end - sq.tiles * sq.splits() * a.Hkv;
+    int u = (unit - unit0) / a.Hkv;
+    const int h = unit - unit0 - u * a.Hkv;
+    int split = 0;
+    bool whole = false;
+    if (sq.splits() > 1) {
+        const int left = u - (sq.splits() - 1) * sq.tiles, per = sq.chunk() * G / PA_ROWS;
+        whole = left < 0;
+        if (whole) {
+            // `together` pieces at a time, their tiles in turn; one, where the tiles have different numbers of pieces (dies would get more than others)
+            const int some = sq.tiles <= per ? a.together : 1, at = u / (sq.tiles * some) * some, n_at = min(some, sq.splits() - 1 - at);
+            u -= at * sq.tiles;
+            split = at + u % n_at;
+            u /= n_at;
+        } else {
+            u = last_tile(left, sq.tiles, per);
+        }
+    }
+    const int tile = sq.tiles - 1 - u;
     const int m0 = tile * PA_ROWS;
     const int last_tok = min((m0 + PA_ROWS - 1) / G, sq.count - 1);
-    const int key_begin = split * a.chunk;
-    const int key_end = min(sq.first + last_tok + 1, key_begin + a.chunk);        // one behind the last key of this unit
-    if (key_begin >= key_end) return;
+    if (sq.splits() > 1) {
+        const int ends_in = (sq.first + last_tok) / sq.chunk();
+        if (whole && split >= ends_in) return;
+        if (!whole) split = ends_in;
+    }
+    const int place = unit0 + (split * sq.tiles + sq.tiles - 1 - tile) * a.Hkv + h;         // of partial results
+    const int key_begin = split * sq.chunk();
+    const int key_end = min(sq.first + last_tok + 1, key_begin + sq.chunk());     // one behind the last key of this unit
     const int n_tiles = (key_end - key_begin + PA_KEYS - 1) / PA_KEYS;
     const int n_full = max(0, min(key_end, sq.first + m0 / G + 1) - key_begin) / PA_KEYS;      // tiles that every row sees whole
 
@@ -577,7 +615,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     asm volatile("" : "+v"(late));
     const int r = wr * 32 + (late & 31), half = (late >> 5) & 1;
     if (m0 + r >= sq.count * G) return;
-    if (sq.splits == 1) {
+    if (sq.splits() == 1) {
         const float f = 1.0f / l;
         const size_t row_out = row_of(m0 + r);
         uint16_t* to = a.out + row_out * HC_D + 8 * half;
@@ -594,10 +632,10 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         if (a.lse && half == 0) a.lse[row_out] = (row.ref + __builtin_amdgcn_logf(l)) * PA_LN2;
     } else {
         // as the registers lie: 1 KB to a store
-        f32x4* to = reinterpret_cast<f32x4*>(a.part_acc) + ((size_t)unit * (PA_ROWS / 32) + wr) * 1024 + (late & 63);
+        f32x4* to = reinterpret_cast<f32x4*>(a.part_acc) + ((size_t)place * (PA_ROWS / 32) + wr) * 1024 + (late & 63);
 #pragma unroll
         for (int i = 0; i < 16; ++i) to[i * 64] = f32x4{O[i / 4][4 * (i % 4)], O[i / 4][4 * (i % 4) + 1], O[i / 4][4 * (i % 4) + 2], O[i / 4][4 * (i % 4) + 3]};
-        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((size_t)unit * PA_ROWS + r) * 2) = f32x2{l == 0.f ? -INFINITY : row.ref, l};
+        if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((size_t)place * PA_ROWS + r) * 2) = f32x2{l == 0.f ? -INFINITY : row.ref, l};
     }
 }
 
@@ -615,14 +653,14 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a
     const int dims = blockIdx.x % 4, block = blockIdx.x / 4 % (PA_ROWS / 32);
     int u = blockIdx.x / 4 / (PA_ROWS / 32);                 // tile by tile, as the units but for the pieces
     const PromptSeq sq = seq_of(a, find_seq(a, u, lane, [&](int i) { return a.table ? a.table[i].tile_end : a.seq[i].tile_end; }));
-    if (sq.splits == 1) return;
+    if (sq.splits() == 1) return;
     u -= sq.tile_end - sq.tiles * a.Hkv;
-    int unit0 = sq.unit_end - sq.tiles * sq.splits * a.Hkv;
+    int unit0 = sq.unit_end - sq.tiles * sq.splits() * a.Hkv;
     const int h = u % a.Hkv, tile = u / a.Hkv, w0 = tile * PA_ROWS + block * 32;
     if (w0 >= sq.count * G) return;
     const int last_tok = min((tile * PA_ROWS + PA_ROWS - 1) / G, sq.count - 1);
-    const int pieces = (sq.first + last_tok + a.chunk) / a.chunk;          // those that have a key of the tile
-    unit0 += (sq.tiles - 1 - tile) * sq.splits * a.Hkv + h;
+    const int pieces = (sq.first + last_tok + sq.chunk()) / sq.chunk();    // those that have a key of the tile
+    unit0 += (sq.tiles - 1 - tile) * a.Hkv + h;
     const bool row = w0 + n < sq.count * G;
     float ref = -INFINITY, l = 0.f;
     f32x4 o[4];
@@ -635,7 +673,7 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a
 #pragma unroll
             for (int k = 0; k < PJ_AHEAD; ++k) {
                 const int s = s0 + k * PJ_WAVES;
-                const size_t unit = unit0 + (size_t)min(s, pieces - 1) * a.Hkv;
+                const size_t unit = unit0 + (size_t)min(s, pieces - 1) * sq.tiles * a.Hkv;
                 ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + (unit * PA_ROWS + block * 32 + n) * 2);
                 if (s >= pieces) ml[k] = f32x2{-INFINITY, 0.f};
                 const f32x4* from = reinterpret_cast<const f32x4*>(a.part_acc) + (unit * (PA_ROWS / 32) + block) * 1024 + dims * 256 + lane;
@@ -690,43 +728,60 @@ void launch(const PromptArgs& a, int units, bool join, int tiles, hipStream_t st
     if (join) prompt_join_kernel<G, KS><<<dim3(tiles * (pa_rows<KS> / 32) * 4), dim3(PJ_WAVES * 64), 0, st>>>(a);
 }
 
-struct PromptPlan {
-    int ks, chunk;         // waves to 32 rows, keys of a piece
+// Keys of a sequence's pieces: about `chunk`, all of one length but for the last.
+struct Cut {
+    int pieces, tiles;     // and tiles of 64 keys of a piece
 };
-// How long a call takes, in microseconds, if 128 / ks rows make a tile and `chunk` keys a piece; < 0: that is more units than are worth looking
-// at, or than the work buffer has room for.  What a tile of 64 keys takes a compute unit (0.94 us for 128 rows, 0.55 for 64, 15 %
-// more if it has one workgroup alone) and a workgroup (0.93 and 0.60), what memory gives (5.4 TB/s to 256 workgroups and more), what a workgroup needs before its first product (4 us),
-// and what the join costs, are measured.
+Cut cut_of(int keys, int chunk)
+{
+    const int s = (keys + chunk - 1) / chunk, t = ((keys + s - 1) / s + PA_KEYS - 1) / PA_KEYS;
+    return Cut{(keys + t * PA_KEYS - 1) / (t * PA_KEYS), t};
+}
+struct PromptPlan {
+    int ks, chunk;         // waves to 32 rows; keys beyond which a sequence is cut, and about as many to a piece
+};
+// How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit to 640 drawn batches (1 to 12 sequences of 1 to 16K
+// tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each, whose times come out within 12 %; the plan with the
+// least is 1.5 % slower than the fastest of them on average.  What any one plan costs: without pieces 1.5 times as much for four heads and 2,199 tokens behind 59,264 (1420 us
+// against 960), with a piece for every place 1.25 times for four heads and 9,038 tokens (133 us against 106).
 float plan_cost(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int ks, int chunk, int slots)
 {
     const int rows = 128 / ks;
-    float work = 0.f, units = 0.f, longest = 0.f, kv = 0.f, parts = 0.f;
+    const float tile_us = ks == 1 ? 0.93f : 0.60f;       // 64 keys: of a compute unit with two workgroups, and of a workgroup that has one for itself
+    float work = 0.f, equal = 0.f, units = 0.f, longest = 0.f, kv = 0.f, parts = 0.f;
     long long room = 0;
-    bool split = false;
+    int pieces = 0;
     for (int i = 0; i < n; ++i) {
         const int b = order[i];
         const float f = (float)first[b], c = (float)count[b], mean = f + 0.5f * c;
-        const long long t = ((long long)count[b] * G + rows - 1) / rows * Hkv, s = ((long long)first[b] + count[b] + chunk - 1) / chunk;
-        room += t * s;
+        const long long t = ((long long)count[b] * G + rows - 1) / rows * Hkv;
+        const Cut cut = cut_of(first[b] + count[b], chunk);
         work += t * (mean / PA_KEYS + 0.5f);
-        const float active = s > 1 ? t * std::min((float)s, std::max(1.f, mean / chunk + 0.5f)) : (float)t;
-        units += active;
-        longest = std::max(longest, std::min((float)chunk, f + c) / PA_KEYS);
-        kv += (f + c) * Hkv * 512.f;
-        if (s > 1) {
-            split = true;
+        float active = (float)t;
+        if (cut.pieces > 1) {
+            room += t * cut.pieces;
+            active *= std::min((float)cut.pieces, std::max(1.f, mean / (cut.tiles * PA_KEYS) + 0.5f));
             parts += active * std::min(rows, count[b] * G) * 520.f;
         }
+        equal += t * (mean - 0.5f * std::min(c, (float)cut.tiles * PA_KEYS)) / PA_KEYS;
+        pieces = std::max(pieces, cut.pieces);
+        units += active;
+        longest = std::max(longest, (float)cut.tiles);
+        kv += (f + c) * Hkv * 512.f;
     }
-    if (split && (room * rows > (long long)2 * slots * 128 || units > 2.5f * slots)) return -1.f;
-    // pieces are of one length, so that compute units have one more or one less of them; and those beyond what the GPU holds at a time
-    // come when the others have ended, to a GPU that is otherwise idle
-    const float cus = 0.5f * slots, last = units - floorf((units - 1.f) / slots) * slots;
-    const float uneven = split ? ceilf(units / cus) / (units / cus) : 1.f;
-    const float arithmetic = std::max(work * (ks == 1 ? 0.94f : 0.55f) / cus * uneven * (units <= cus ? 1.15f : 1.f), longest * (ks == 1 ? 0.93f : 0.60f));
+    if (room * rows > (long long)PA_ROOM * slots * 128) return -1.f;
+    // units of one length (whole pieces, tiles of a chunk behind many keys) leave some compute units one more than others; a prompt's tiles and
+    // last pieces are of all lengths and even out, the pieces less well.  The longest unit shares its compute unit as long as there are others;
+    // and what comes beyond what the GPU holds at a time finds an otherwise idle one.
+    const float cus = 0.5f * slots, more = units > slots ? 1.f - slots / units : 0.f, last = units - floorf((units - 1.f) / slots) * slots;
+    const float uneven = units > cus || room > 0 ? 1.f + (ceilf(units / cus) / (units / cus) - 1.f) * equal / work : 1.f;
+    const float ragged = room > 0 ? 0.25f * std::min(1.f, 3.f * (1.f - equal / work)) : 0.f;
+    const float alone = longest * tile_us, shared = work * tile_us / cus;
+    const float arithmetic = std::max(shared * uneven * (units <= cus ? 1.2f : 1.f) + ragged * alone, alone + 0.45f * more * shared);
     const float read = kv / 5.4e6f * (1.f + 0.12f * (uneven - 1.f));
-    const float memory = units > slots ? read * (1.f - last / units) + std::max(read * last / units, longest * 0.9f) : read / std::min(1.f, units / cus);
-    return std::max(arithmetic, memory) + (units > slots ? 8.f : 4.f) + (split ? 6.f + parts * (2.f / 4.5e6f) : 0.f);
+    const float memory = units > slots ? read * (1.f - last / units) + std::max(read * last / units, longest * 0.45f * equal / work)
+                                       : read / std::min(1.f, powf(units / cus, 0.3f));
+    return std::max(arithmetic, memory) + (units > slots ? 5.5f : 3.5f) + (room > 0 ? 4.5f + 0.03f * pieces + parts / 3.0e6f : 0.f);
 }
 PromptPlan make_plan(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int slots)
 {
@@ -735,7 +790,7 @@ PromptPlan make_plan(int n, const int* order, const int32_t* first, const int32_
     const int longest = first[order[0]] + count[order[0]];
     for (int ks = 1; ks <= 2; ++ks)
         for (int pieces = 1; pieces <= 1024 && longest / pieces >= 128; pieces += 1 + pieces / 12) {
-            const int chunk = pieces == 1 ? 1 << 30 : ((longest + pieces - 1) / pieces + PA_KEYS - 1) / PA_KEYS * PA_KEYS;
+            const int chunk = pieces == 1 ? 1 << 30 : (longest + pieces - 1) / pieces;
             const float c = plan_cost(n, order, first, count, G, Hkv, ks, chunk, slots);
             if (c < 0.f) break;
             if (c < cost) {
@@ -746,8 +801,8 @@ PromptPlan make_plan(int n, const int* order, const int32_t* first, const int32_
     return best;
 }
 
-// Rows of partial results that there is room for: two tiles of 128 for every workgroup that the GPU holds at a time.
-size_t part_rows(const hc_ctx* ctx) { return (size_t)2 * PA_PER_CU * ctx->n_cu * 128; }
+// Rows of partial results that there is room for: PA_ROOM tiles of 128 for every workgroup that the GPU holds at a time.
+size_t part_rows(const hc_ctx* ctx) { return (size_t)PA_ROOM * PA_PER_CU * ctx->n_cu * 128; }
 
 }   // namespace
 
@@ -787,8 +842,7 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
     std::sort(order, order + n, [&](int x, int y) { return first[x] + count[x] != first[y] + count[y] ? first[x] + count[x] > first[y] + count[y] : x < y; });
     const PromptPlan plan = make_plan(n, order, first, count, G, c.Hkv, slots);
     const int rows = 128 / plan.ks;
-    long long units = 0, tiles = 0;
-    bool join = false;
+    long long units = 0, tiles = 0, joined = 0;              // joined: units that leave partial results; they come first
     for (int i = 0; i < n; ++i) {
         const int b = order[i];
         PromptSeq& s = seq[i];
@@ -796,13 +850,16 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
         s.count = count[b];
         s.tok0 = tok0[b];
         s.tiles = (int)(((long long)count[b] * G + rows - 1) / rows);
-        s.splits = (int)(((long long)first[b] + count[b] + plan.chunk - 1) / plan.chunk);
-        join |= s.splits > 1;
+        const Cut cut = cut_of(first[b] + count[b], plan.chunk);
+        s.cut = (uint32_t)cut.tiles << 12 | (uint32_t)cut.pieces;
         tiles += (long long)s.tiles * c.Hkv;
-        units += (long long)s.tiles * s.splits * c.Hkv;
+        units += (long long)s.tiles * cut.pieces * c.Hkv;
+        if (cut.pieces > 1) joined = units;
         s.unit_end = (int)units;
         s.tile_end = (int)tiles;
     }
+    if (joined * rows > (long long)part_rows(ctx)) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: partial results without room");       // (the plan sees to it)
+    const bool join = joined > 0;
     PromptArgs a{};
     a.q = (const uint16_t*)q;
     a.kv = (const uint16_t*)kv;
@@ -812,7 +869,7 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
     a.part_ml = (float*)((char*)work + lay.ml);
     a.Hkv = c.Hkv;
     a.n_seq = n;
-    a.chunk = plan.chunk;
+    a.together = std::max(1, PA_DIES / c.Hkv);
     a.n_cu = ctx->n_cu;
     a.mirror = !join && ctx->n_cu % c.Hkv == 0 && units > ctx->n_cu ? (int)std::min<long long>(units - ctx->n_cu, ctx->n_cu) : 0;
     a.table_rows = n * c.Hkv;

@@ -76,6 +76,18 @@ def test_packed(first, count, Hkv, G):
     c.close()
 
 
+@pytest.mark.parametrize("first,count,Hkv,G", [
+    ([0], [8777], 1, 1), ([0], [4100], 2, 1), ([300], [6001], 1, 2),           # a prompt in pieces: its tiles have different numbers of them
+    ([60001], [52], 1, 8), ([62133, 0], [42, 14], 2, 4), ([50001], [150], 4, 1), ([33000], [301], 3, 4),      # a chunk: pieces of one head alternate
+    ([20000, 3000, 0], [1, 5000, 700], 1, 4),
+])
+def test_pieces_of_few_heads(first, count, Hkv, G):
+    c = Call(first, count, Hkv, G)
+    c.run()
+    c.check()
+    c.close()
+
+
 def test_nothing_to_do():
     c = Call([5, 0], [0, 0], 2, 4)
     c.run()
