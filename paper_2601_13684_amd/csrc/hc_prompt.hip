@@ -11,7 +11,13 @@
 // A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights, sums and bf16 are
 // floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.  A workgroup
 // that finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that keeps masked infinities
-// and NaNs of V out): what that costs is paid by inputs that need it.
+// and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by inputs that need it; all others save the running
+// maximum's 2 %.
+//
+// Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.0 ms, 1.19 PFLOP/s, 86 % of what
+// a bf16 product of 16384^3 reaches on the same card (1.39); in the loop the clock falls from 2.4 to 1.7 GHz, and changes of the schedule that
+// leave the matrix cores idle less let it fall further.  8,192 tokens 488 us, 1.13 PFLOP/s.  Few rows behind many keys are bound by memory: 17 tokens behind four contexts
+// of 20K to 90K 166 us, 5.5 TB/s.  Below about 2,000 tokens: the loads before the first product, and too few units (200 tokens 8 us, 1,024 18.5).
 //
 // P is rounded to bf16 for the matrix cores, to the nearest: the error of an output is that of its 2^-9 per weight, independent
 // from key to key, about what the output's own rounding to bf16 adds.  Sum, maximum, lse and accumulators are 32-bit, the sum
@@ -70,7 +76,8 @@ struct PromptArgs {
     uint16_t* out;
     float *lse, *part_acc, *part_ml;
     int Hkv, n_seq;
-    int together;                                 // pieces whose tiles alternate, so that one piece of one head stays with one of the eight dies
+    int together;                                 // pieces whose tiles alternate, so that one piece of one head stays with one of the dies (52 tokens of
+                                                  // eight heads behind 115,286, one KV head, seven tiles: 70 us without, the tiles on seven dies; 42 with)
     int n_cu, mirror;                             // compute units; units of the second round, which is dealt out backwards (0: it is not)
     // what is to be done, and where K and V are: here, or, of more sequences and heads than there is room for here, in the work buffer
     const PromptSeq* table;
@@ -164,27 +171,17 @@ struct RowState {
 };
 
 // A unit is the work of a workgroup.  The first n_cu workgroups go to a compute unit each, the next n_cu beside them: these are dealt out
-// backwards, the lightest beside the heaviest (head by head, so that a head stays with its die).
+// backwards, the lightest beside the heaviest (head by head, so that a head stays with its die): 2,048 tokens of eight heads 42.9 us against 44.7, 4,096
+// 132.5 against 136, 8,192 no difference.
 __device__ __forceinline__ int mirrored(int block, int n_cu, int second, int Hkv)
 {
     const int r = block - n_cu;
     return r >= second ? block : n_cu + (second / Hkv - 1 - r / Hkv) * Hkv + r % Hkv;
 }
 
-// The last pieces of a sequence's tiles have all lengths.  Counted from the last tile, `per` tiles have their ends in one piece's length of keys, and the
-// first of them has the longest: one of every such run in turn.
-__device__ __forceinline__ int last_tile(int i, int tiles, int per)
-{
-    const int runs = (tiles + per - 1) / per;
-    if (runs == 1) return i;
-    const int whole = (tiles - (runs - 1) * per) * runs;         // what comes before the last run, a shorter one, is used up
-    if (i < whole) return i % runs * per + i / runs;
-    i -= whole;
-    return i % (runs - 1) * per + whole / runs + i / (runs - 1);
-}
-
 // KS = 1: a tile has 128 rows, a wave takes all keys of its 32.  KS = 2: a tile has 64 rows, two waves share 32 of them, one half of every 64
-// keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the traffic into LDS.
+// keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the traffic into LDS.  Eight KV heads,
+// groups of four, KS = 1 against 2: 512 tokens 13.4 us against 11.4, 1,024 22.3 against 18.6, 2,048 42.9 against 47.5, 8,192 490 against 565.
 template <int KS>
 constexpr int pa_rows = 128 / KS;
 template <int G, int KS>
@@ -208,16 +205,16 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     int split = 0;
     bool whole = false;
     if (sq.splits() > 1) {
-        const int left = u - (sq.splits() - 1) * sq.tiles, per = sq.chunk() * G / PA_ROWS;
+        const int left = u - (sq.splits() - 1) * sq.tiles;
         whole = left < 0;
         if (whole) {
             // `together` pieces at a time, their tiles in turn; one, where the tiles have different numbers of pieces (dies would get more than others)
-            const int some = sq.tiles <= per ? a.together : 1, at = u / (sq.tiles * some) * some, n_at = min(some, sq.splits() - 1 - at);
+            const int some = sq.tiles * PA_ROWS <= sq.chunk() * G ? a.together : 1, at = u / (sq.tiles * some) * some, n_at = min(some, sq.splits() - 1 - at);
             u -= at * sq.tiles;
             split = at + u % n_at;
             u /= n_at;
         } else {
-            u = last_tile(left, sq.tiles, per);
+            u = left;
         }
     }
     const int tile = sq.tiles - 1 - u;
@@ -742,8 +739,9 @@ struct PromptPlan {
 };
 // How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit to 640 drawn batches (1 to 12 sequences of 1 to 16K
 // tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each, whose times come out within 12 %; the plan with the
-// least is 1.5 % slower than the fastest of them on average.  What any one plan costs: without pieces 1.5 times as much for four heads and 2,199 tokens behind 59,264 (1420 us
-// against 960), with a piece for every place 1.25 times for four heads and 9,038 tokens (133 us against 106).
+// least is 1.5 % slower than the fastest of them on average.  Pieces against none: one token behind 131,072 102 us against 2185, 512 behind 120,001 900 against 1650
+// (eight KV heads, groups of four), 2,199 behind 59,264 of four heads 1007 against 1429; and where there are units enough, two pieces against none: 9,038 tokens of
+// four single heads 124 against 109.
 float plan_cost(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int ks, int chunk, int slots)
 {
     const int rows = 128 / ks;
