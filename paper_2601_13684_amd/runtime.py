@@ -11,6 +11,7 @@ bytes per position, so that one retrieved position is one contiguous host read.
 """
 from __future__ import annotations
 
+import contextlib
 from array import array
 from typing import Dict, List, Optional, Tuple
 
@@ -229,7 +230,8 @@ class LayerRuntime:
         if prompt.length != spec.ctx:
             raise ValueError("the prompt's sequences have other lengths than the layer's")
         self.kv_prefill, self._k_src, self._v_src = prompt.kv, prompt.k_off, prompt.v_off
-        self.prefill_work = torch.zeros((hc.hc_prefill_work_bytes(self.ctx.handle, self.handle),), dtype=torch.uint8, device=self.ctx.device)
+        with _on(stream, self.ctx.device):
+            self.prefill_work = torch.zeros((hc.hc_prefill_work_bytes(self.ctx.handle, self.handle),), dtype=torch.uint8, device=self.ctx.device)
         self.prefill_init(None, q_last, pool, stream)
 
     def prefill_scores(self) -> dict:
@@ -275,7 +277,8 @@ class LayerRuntime:
         """The decode token's projected heads (q [B, Hq, D], k and v [B, Hkv, D], bf16 or f32): norm, rotation and append in one
         launch (hc_append_rope).  Returns the queries for ``attn``."""
         if q_out is None:
-            q_out = torch.empty((self.spec.B, self.spec.Hq, D), dtype=torch.bfloat16, device=self.ctx.device)
+            with _on(stream, self.ctx.device):
+                q_out = torch.empty((self.spec.B, self.spec.Hq, D), dtype=torch.bfloat16, device=self.ctx.device)
         hc.hc_append_rope(self.ctx.handle, self.handle, rope, q, k, v, q_out, self.arena, self.tier, stream)
         return q_out
 
@@ -323,6 +326,13 @@ class LayerRuntime:
             self.handle = None
 
 
+def _on(stream, device):
+    """What is allocated under it belongs to the stream that a call is given (None: the current one), so that its memory is not in another's use."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device))
+
+
 class Prompt:
     """The prompt stage of one layer: a buffer with a K and a V block for every (sequence, KV head), room[b] rows each, that takes the
     prompt in one or several chunks and attends over what is there."""
@@ -347,9 +357,10 @@ class Prompt:
         if any(n + c > r for n, c, r in zip(self.length, count, self.room)):
             raise ValueError("a sequence has no room for its chunk")
         T, Hq, dev = q.shape[0], self.ctx.cfg.Hq, self.ctx.device
-        qr = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
-        out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        with _on(stream, dev):
+            qr = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
+            out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
         hc.hc_prefill_rope(self.ctx.handle, rope, q, k, v, self.length, count, qr, self.kv, self.k_off, self.v_off, stream)
         hc.hc_prefill_attn(self.ctx.handle, qr, self.kv, self.k_off, self.v_off, self.length, count, out, lse, self.work, self.work.numel(), stream)
         self.length = [n + c for n, c in zip(self.length, count)]

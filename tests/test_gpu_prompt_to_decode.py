@@ -76,3 +76,22 @@ def layer_from(ctx, spec, prompt, q_last, growth):
     lay = R.LayerRuntime(ctx, spec, data, None, None, growth=growth, prefill=(q_last, 1))
     lay.prefill_from(prompt, q_last)
     return lay
+
+
+def test_chunks_on_another_stream():
+    """Everything that a chunk allocates and launches is the given stream's: as on the current one, with the current one's work around it."""
+    Hkv, G, ctx_lens = 2, 4, [300, 1100]
+    spec = I.LayerSpec(B=2, Hq=Hkv * G, Hkv=Hkv, D=D, ctx=ctx_lens, heads=[[I.HeadSpec(I.ROLE_FULL)] * 2] * 2)
+    ctx = R.Context(R.make_config(spec), DEV)
+    rope = hc.hc_rope_init(hc.HC_ROPE_HALF, 64, 10000.0)
+    x = torch.randn((sum(ctx_lens), Hkv * (G + 2), D), device=DEV).to(torch.bfloat16)
+    qkv = x[:, :Hkv * G], x[:, Hkv * G:-Hkv], x[:, -Hkv:]
+    want = R.Prompt(ctx, ctx_lens).chunk(rope, *qkv, ctx_lens)
+    for make in (lambda s: s, lambda s: s.cuda_stream):
+        prompt, side = R.Prompt(ctx, ctx_lens), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = prompt.chunk(rope, *qkv, ctx_lens, stream=make(side))
+        noise = [torch.full_like(t, 3.0) for t in want]          # the current stream's next allocations are not the chunk's memory
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all((n == 3).all() for n in noise)
