@@ -443,7 +443,7 @@ typedef struct {
 hc_status hc_rope_init(hc_rope* out, int32_t layout, int32_t rot_dim, double theta, const hc_rope_scaling* scaling);
 
 /* The tokens of a call are packed: sequence b brings count[b] >= 0 of them, at positions first[b] .. first[b] + count[b] - 1 (HOST arrays
- * of B; first + count <= max_ctx), sequence after sequence without gaps; T is their sum (T Hq below 2^31; 0: nothing happens).  first[b] > 0: a chunk behind
+ * of B; first + count <= max_ctx), sequence after sequence without gaps; T is their sum (at most 2^25, T Hq at most 2^29; 0: nothing happens).  first[b] > 0: a chunk behind
  * what earlier calls brought.  At most 128 KV heads.
  *   q, k, v       dev, in_type HC_BF16 or HC_F32; token t's heads, [Hq][128] or [Hkv][128], at element t * q_stride (k_stride, v_stride):
  *                 views of one [T][(Hq + 2 Hkv) * 128] product, or tensors of their own.  16-byte aligned, strides multiples of 8

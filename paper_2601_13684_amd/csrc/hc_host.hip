@@ -1091,7 +1091,7 @@ static hc_status chunk_check(hc_ctx* ctx, const char* who, const void* kv_prefil
             return hc_fail(ctx, HC_ESHAPE, "%s: sequence %d: %d tokens behind %d are more than max_ctx %d", who, b, (int)count[b], (int)first[b], (int)c.max_ctx);
         t += count[b];
     }
-    if (t > INT_MAX / c.Hq) return hc_fail(ctx, HC_ESHAPE, "%s: %lld tokens of %d query heads are more than one call takes", who, t, (int)c.Hq);
+    if (t > HC_PROMPT_TOKENS || t > HC_PROMPT_ROWS / c.Hq) return hc_fail(ctx, HC_ESHAPE, "%s: %lld tokens of %d query heads are more than one call takes", who, t, (int)c.Hq);
     for (int i = 0; i < c.B * c.Hkv; ++i)
         if (count[i / c.Hkv] > 0 && (k_off[i] < 0 || v_off[i] < 0 || (k_off[i] & 7) || (v_off[i] & 7)))
             return hc_fail(ctx, HC_EINVAL, "%s: head %d: offsets must be non-negative multiples of 8 elements", who, i);

@@ -397,6 +397,7 @@ struct hc_append_call {
 };
 hc_status hc_launch_append(hc_ctx* ctx, int n, const hc_append_call* calls, hipStream_t st);
 constexpr double HC_ROPE_MAX_FREQ = 1.0e6;      // radians a position: keeps position * frequency far from the ends of 64 bits
+constexpr int HC_PROMPT_TOKENS = 1 << 25, HC_PROMPT_ROWS = 1 << 29;      // of a call: its launches stay below 2^32 threads
 constexpr int HC_PROMPT_SEQS = 64, HC_PROMPT_HEADS = 128;   // sequences and (sequence, KV head) pairs that a launch over packed tokens has room for
 // Projected rows as a caller hands them in: elements from token to token (from sequence to sequence), 32-bit or bf16.
 struct hc_rows_in {

@@ -650,7 +650,6 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a
     const int dims = blockIdx.x % 4, block = blockIdx.x / 4 % (PA_ROWS / 32);
     int u = blockIdx.x / 4 / (PA_ROWS / 32);                 // tile by tile, as the units but for the pieces
     const PromptSeq sq = seq_of(a, find_seq(a, u, lane, [&](int i) { return a.table ? a.table[i].tile_end : a.seq[i].tile_end; }));
-    if (sq.splits() == 1) return;
     u -= sq.tile_end - sq.tiles * a.Hkv;
     int unit0 = sq.unit_end - sq.tiles * sq.splits() * a.Hkv;
     const int h = u % a.Hkv, tile = u / a.Hkv, w0 = tile * PA_ROWS + block * 32;
@@ -719,10 +718,10 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a
 }
 
 template <int G, int KS>
-void launch(const PromptArgs& a, int units, bool join, int tiles, hipStream_t st)
+void launch(const PromptArgs& a, int units, int tiles, hipStream_t st)
 {
     prompt_attn_kernel<G, KS><<<dim3(units), dim3(PA_BLK), 0, st>>>(a);
-    if (join) prompt_join_kernel<G, KS><<<dim3(tiles * (pa_rows<KS> / 32) * 4), dim3(PJ_WAVES * 64), 0, st>>>(a);
+    if (tiles) prompt_join_kernel<G, KS><<<dim3(tiles * (pa_rows<KS> / 32) * 4), dim3(PJ_WAVES * 64), 0, st>>>(a);
 }
 
 // Keys of a sequence's pieces: about `chunk`, all of one length but for the last.
@@ -840,7 +839,7 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
     std::sort(order, order + n, [&](int x, int y) { return first[x] + count[x] != first[y] + count[y] ? first[x] + count[x] > first[y] + count[y] : x < y; });
     const PromptPlan plan = make_plan(n, order, first, count, G, c.Hkv, slots);
     const int rows = 128 / plan.ks;
-    long long units = 0, tiles = 0, joined = 0;              // joined: units that leave partial results; they come first
+    long long units = 0, tiles = 0, joined = 0, joined_tiles = 0;          // joined: those that leave partial results; they come first
     for (int i = 0; i < n; ++i) {
         const int b = order[i];
         PromptSeq& s = seq[i];
@@ -852,12 +851,14 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
         s.cut = (uint32_t)cut.tiles << 12 | (uint32_t)cut.pieces;
         tiles += (long long)s.tiles * c.Hkv;
         units += (long long)s.tiles * cut.pieces * c.Hkv;
-        if (cut.pieces > 1) joined = units;
+        if (cut.pieces > 1) {
+            joined = units;
+            joined_tiles = tiles;
+        }
         s.unit_end = (int)units;
         s.tile_end = (int)tiles;
     }
     if (joined * rows > (long long)part_rows(ctx)) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: partial results without room");       // (the plan sees to it)
-    const bool join = joined > 0;
     PromptArgs a{};
     a.q = (const uint16_t*)q;
     a.kv = (const uint16_t*)kv;
@@ -869,7 +870,7 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
     a.n_seq = n;
     a.together = std::max(1, PA_DIES / c.Hkv);
     a.n_cu = ctx->n_cu;
-    a.mirror = !join && ctx->n_cu % c.Hkv == 0 && units > ctx->n_cu ? (int)std::min<long long>(units - ctx->n_cu, ctx->n_cu) : 0;
+    a.mirror = joined == 0 && ctx->n_cu % c.Hkv == 0 && units > ctx->n_cu ? (int)std::min<long long>(units - ctx->n_cu, ctx->n_cu) : 0;
     a.table_rows = n * c.Hkv;
     const bool in_table = n > PA_SEQS || a.table_rows > PA_HEADS;
     const int most = std::max(1, std::min(PA_SEQS, PA_HEADS / c.Hkv));          // sequences of an upload
@@ -892,14 +893,14 @@ hc_status hc_launch_prefill_attn(hc_ctx* ctx, const void* q, const void* kv, con
         a.table_off = (const int64_t*)((char*)work + lay.off);
     }
     switch (G * 4 + plan.ks) {
-    case 5: launch<1, 1>(a, (int)units, join, (int)tiles, st); break;
-    case 6: launch<1, 2>(a, (int)units, join, (int)tiles, st); break;
-    case 9: launch<2, 1>(a, (int)units, join, (int)tiles, st); break;
-    case 10: launch<2, 2>(a, (int)units, join, (int)tiles, st); break;
-    case 17: launch<4, 1>(a, (int)units, join, (int)tiles, st); break;
-    case 18: launch<4, 2>(a, (int)units, join, (int)tiles, st); break;
-    case 33: launch<8, 1>(a, (int)units, join, (int)tiles, st); break;
-    default: launch<8, 2>(a, (int)units, join, (int)tiles, st); break;
+    case 5: launch<1, 1>(a, (int)units, (int)joined_tiles, st); break;
+    case 6: launch<1, 2>(a, (int)units, (int)joined_tiles, st); break;
+    case 9: launch<2, 1>(a, (int)units, (int)joined_tiles, st); break;
+    case 10: launch<2, 2>(a, (int)units, (int)joined_tiles, st); break;
+    case 17: launch<4, 1>(a, (int)units, (int)joined_tiles, st); break;
+    case 18: launch<4, 2>(a, (int)units, (int)joined_tiles, st); break;
+    case 33: launch<8, 1>(a, (int)units, (int)joined_tiles, st); break;
+    default: launch<8, 2>(a, (int)units, (int)joined_tiles, st); break;
     }
     HC_HIP(ctx, hipGetLastError());
     return HC_OK;

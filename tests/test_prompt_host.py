@@ -142,6 +142,13 @@ assert attn(many, 129) == S and rope(many, 129) == S
 big = cfg(2, 1, 8, 1 << 24)
 fake.fake_reset(0)
 assert attn(big, 2, first=[0, 0], count=[1 << 24, 1 << 24]) == 0 and len(log()) == 1           # 2^28 rows of queries
+n = 1 << 24
+more = cfg(3, 1, 1, n)
+fake.fake_reset(0)
+assert attn(more, 3, first=[0] * 3, count=[n, n, 1]) == S and rope(more, 3, first=[0] * 3, count=[n, 1, n]) == S and not log()      # 2^25 tokens
+wide = cfg(9, 4, 8, n)
+fake.fake_reset(0)
+assert attn(wide, 36, first=[0] * 9, count=[n] + [1] + [0] * 7) == S and rope(wide, 36, first=[0] * 9, count=[0] * 8 + [n]) == 0      # 2^29 rows
 huge = cfg(64, 1, 8, 1 << 24)
 fake.fake_reset(0)
 assert attn(huge, 64, first=[0] * 64, count=[1 << 24] * 64) == S
