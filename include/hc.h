@@ -419,8 +419,8 @@ enum { HC_ROPE_HALF = 0,          /* pairs (i, i + rot_dim/2)                   
 enum { HC_ROPE_LINEAR = 0,        /* every frequency divided by factor (positions interpolated)            */
        HC_ROPE_BASE = 1,          /* theta multiplied by factor^(rot_dim / (rot_dim - 2))                  */
        HC_ROPE_BANDS = 2 };       /* by full turns inside `original` positions: at most low: divided by factor; at least
-                                     high: kept; between them the two mixed linearly (low 1, high 4: Llama 3.1;
-                                     low 1, high 32 with gain 0.1 ln(factor) + 1: YaRN)                    */
+                                     high: kept; between them the two mixed linearly (usual: low 1, high 4; or low 1,
+                                     high 32 and a gain of 0.1 ln(factor) + 1)                             */
 /* What happens to a query or key head: y = x (mean(x^2) + eps)^(-1/2) w over its 128 elements (only where w is given), then the pairs of
  * its first rot_dim elements turn by position * freq[i]:  (u, v) -> gain (u cos - v sin, v cos + u sin).  The elements behind
  * rot_dim are not turned and not multiplied by gain.  A plain struct: set or change any field. */
@@ -449,7 +449,7 @@ hc_status hc_rope_init(hc_rope* out, int32_t layout, int32_t rot_dim, double the
  *                 views of one [T][(Hq + 2 Hkv) * 128] product, or tensors of their own.  16-byte aligned, strides multiples of 8
  *   q_out         dev bf16 [T][Hq][128]: the queries, through norm and rotation
  *   kv_prefill    dev bf16: K row of position p of head (b, h) at element k_off[b*Hkv+h] + p * 128, through norm and rotation; V row,
- *                 as it is, at v_off[..] + p * 128 (HOST arrays of B*Hkv, multiples of 8).  Nothing else in it is written
+ *                 as it is, at v_off[..] + p * 128 (HOST arrays of B*Hkv, multiples of 8).  Nothing else in it is written; rows that a call writes must not overlap
  * Angles are formed in 64 bits, norms and rotation in 32; one rounding, to bf16.  q_out and kv_prefill must not overlap the inputs. */
 hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
                           int64_t v_stride, int32_t in_type, const int32_t* first, const int32_t* count, void* q_out, void* kv_prefill,

@@ -3,23 +3,25 @@
 //     s_j = q . K_h[j] / sqrt(128),  j = 0 .. p;   out = sum_j exp(s_j - lse) V_h[j],   lse = log sum_j exp(s_j)
 //
 // Work is cut into tiles of PA_ROWS query rows of one KV head, the group's G heads of a token side by side: a tile spans PA_ROWS / G
-// tokens, the group shares its K and V, and the diagonal is met in fine steps.  A wave holds 32 rows.  It forms the transposed
-// product S^T = K Q^T on the matrix cores (v_mfma_f32_32x32x16_bf16), keys along the registers and a query to each lane, so that a
-// row's maximum and sum stay inside a lane but for one exchange between the halves of the wave; and the registers that hold P^T
-// are, rounded to bf16, the second product's operand as they are: O^T = V^T P^T may take the keys of a step in any order as long
-// as both operands do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
-// A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights, sums and bf16 are
-// floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.  A workgroup
-// that finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that keeps masked infinities
-// and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by inputs that need it; all others save the running
-// maximum's 2 %.
+// tokens, the group shares its K and V, and the diagonal is met in fine steps.  A wave holds 32 rows.  It forms the transposed product
+// S^T = K Q^T on the matrix cores (v_mfma_f32_32x32x16_bf16), keys along the registers and a query to each lane, so that a row's
+// maximum and sum stay inside a lane but for one exchange between the halves of the wave; and the registers that hold P^T are, rounded
+// to bf16, the second product's operand as they are: O^T = V^T P^T may take the keys of a step in any order as long as both operands
+// do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
+// A row's weights
+// are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights, sums and bf16 are
+// floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.  A workgroup that
+// finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that keeps masked
+// infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by inputs that
+// need it; all others save the running maximum's 2 %.
 //
-// Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.0 ms, 1.19 PFLOP/s, 86 % of what
-// a bf16 product of 16384^3 reaches on the same card (1.39); in the loop the clock falls from 2.4 to 1.7 GHz, and changes of the schedule that
-// leave the matrix cores idle less let it fall further.  8,192 tokens 488 us, 1.13 PFLOP/s.  Few rows behind many keys are bound by memory: 17 tokens behind four contexts
-// of 20K to 90K 166 us, 5.5 TB/s.  Below about 2,000 tokens: the loads before the first product, and too few units (200 tokens 8 us, 1,024 18.5).
+// Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.0 ms, 1.19
+// PFLOP/s, 86 % of what a bf16 product of 16384^3 reaches on the same card (1.39); in the loop the clock falls from 2.4 to 1.7 GHz,
+// and changes of the schedule that leave the matrix cores idle less let it fall further.  8,192 tokens 488 us, 1.13 PFLOP/s.  Few rows
+// behind many keys are bound by memory: 17 tokens behind four contexts of 20K to 90K 166 us, 5.5 TB/s.  Below about 2,000 tokens: the
+// loads before the first product, and too few units (200 tokens 8 us, 1,024 18.5).
 //
-// P is rounded to bf16 for the matrix cores, to the nearest: the error of an output is that of its 2^-9 per weight, independent
+// P is rounded to bf16 for the matrix cores, to the nearest: the error of an output is that of at most 2^-8 per weight, independent
 // from key to key, about what the output's own rounding to bf16 adds.  Sum, maximum, lse and accumulators are 32-bit, the sum
 // from the unrounded weights.
 //
@@ -56,8 +58,8 @@ constexpr int PA_TILE = PA_KEYS * HC_D * 2;       // its bytes
 constexpr float PA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
 constexpr float PA_LN2 = 0.6931471805599453f;
 constexpr float PA_SLACK = 8.0f;                  // log2 units: where there is a running maximum, a weight is at most 2^8 before the reference moves
-// Where there is none: what a row's sum of weights lies between (below 2^-60 weights that are lost as denormals might count: 2^24 of 2^-126), and what the
-// magnitudes of a lane's 64 sums add up to (the join adds up to 2^11 of them, of at most 2^24 weights).
+// Where there is none: what a row's sum of weights lies between (below 2^-60 weights that are lost as denormals might count: 2^24 of
+// 2^-126), and what the magnitudes of a lane's 64 sums add up to (the join adds up to 2^11 of them, of at most 2^24 weights).
 constexpr float PA_LEAST = 0x1p-60f, PA_MOST = 0x1p100f, PA_LARGEST = 0x1p112f;
 
 constexpr int PA_SEQS = HC_PROMPT_SEQS, PA_HEADS = HC_PROMPT_HEADS;
@@ -76,8 +78,9 @@ struct PromptArgs {
     uint16_t* out;
     float *lse, *part_acc, *part_ml;
     int Hkv, n_seq;
-    int together;                                 // pieces whose tiles alternate, so that one piece of one head stays with one of the dies (52 tokens of
-                                                  // eight heads behind 115,286, one KV head, seven tiles: 70 us without, the tiles on seven dies; 42 with)
+    // pieces whose tiles alternate, so that one piece of one head stays with one of the dies (52 tokens behind 115,286, one KV head of eight
+    // query heads: 42 us; with the seven tiles of every piece on seven dies 70)
+    int together;
     int n_cu, mirror;                             // compute units; units of the second round, which is dealt out backwards (0: it is not)
     // what is to be done, and where K and V are: here, or, of more sequences and heads than there is room for here, in the work buffer
     const PromptSeq* table;
@@ -149,8 +152,8 @@ __device__ __forceinline__ void tile_ready()
     __syncthreads();
 }
 
-// How the instructions of eight products are to follow each other: behind each of them operand reads for later ones and a share of the weights'
-// arithmetic.
+// How the instructions of eight products are to follow each other: behind each of them operand reads for later ones and a share of the
+// weights' arithmetic.
 template <int products, int reads, int valu, int exps>
 __device__ __forceinline__ void interleave()
 {
@@ -164,24 +167,25 @@ __device__ __forceinline__ void interleave()
     }
 }
 
-// The reference and the sum of a lane's row.  ref is a whole number; lim = ref + PA_SLACK where there is a running maximum, -inf while the row has
-// seen nothing.
+// The reference and the sum of a lane's row.  ref is a whole number; lim = ref + PA_SLACK where there is a running maximum, -inf while
+// the row has seen nothing.
 struct RowState {
     float ref, lim, l;
 };
 
-// A unit is the work of a workgroup.  The first n_cu workgroups go to a compute unit each, the next n_cu beside them: these are dealt out
-// backwards, the lightest beside the heaviest (head by head, so that a head stays with its die): 2,048 tokens of eight heads 42.9 us against 44.7, 4,096
-// 132.5 against 136, 8,192 no difference.
+// A unit is the work of a workgroup.  The first n_cu workgroups go to a compute unit each, the next n_cu beside them: these are dealt
+// out backwards, the lightest beside the heaviest (head by head, so that a head stays with its die): 2,048 tokens of eight heads 42.9
+// us against 44.7, 4,096 132.5 against 136, 8,192 no difference.
 __device__ __forceinline__ int mirrored(int block, int n_cu, int second, int Hkv)
 {
     const int r = block - n_cu;
     return r >= second ? block : n_cu + (second / Hkv - 1 - r / Hkv) * Hkv + r % Hkv;
 }
 
-// KS = 1: a tile has 128 rows, a wave takes all keys of its 32.  KS = 2: a tile has 64 rows, two waves share 32 of them, one half of every 64
-// keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the traffic into LDS.  Eight KV heads,
-// groups of four, KS = 1 against 2: 512 tokens 13.4 us against 11.4, 1,024 22.3 against 18.6, 2,048 42.9 against 47.5, 8,192 490 against 565.
+// KS = 1: a tile has 128 rows, a wave takes all keys of its 32.  KS = 2: a tile has 64 rows, two waves share 32 of them, one half of
+// every 64 keys to each, and what they have comes together in LDS at the end: twice the workgroups of half the length, for twice the
+// traffic into LDS.  Eight KV heads, groups of four, KS = 1 against 2: 512 tokens 13.4 us against 11.4, 1,024 22.3 against 18.6, 2,048
+// 42.9 against 47.5, 8,192 490 against 565.
 template <int KS>
 constexpr int pa_rows = 128 / KS;
 template <int G, int KS>
@@ -194,8 +198,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, hh = lane >> 5;
 
-    // which piece of the keys, which tile, which head: the longest sequence first, its whole pieces and then the last ones of its tiles, heads
-    // fastest, so that the workgroups that stream the same K and V do so at the same time on the same die
+    // which piece of the keys, which tile, which head: the longest sequence first, its whole pieces and then the last ones of its
+    // tiles, heads fastest, so that the workgroups that stream the same K and V do so at the same time on the same die
     const int unit = a.mirror > 0 && (int)blockIdx.x >= a.n_cu ? mirrored(blockIdx.x, a.n_cu, a.mirror, a.Hkv) : blockIdx.x;
     const int si = find_seq(a, unit, lane, [&](int i) { return a.table ? a.table[i].unit_end : a.seq[i].unit_end; });
     const PromptSeq sq = seq_of(a, si);
@@ -208,7 +212,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         const int left = u - (sq.splits() - 1) * sq.tiles;
         whole = left < 0;
         if (whole) {
-            // `together` pieces at a time, their tiles in turn; one, where the tiles have different numbers of pieces (dies would get more than others)
+            // `together` pieces at a time, their tiles in turn; one, where the tiles have different numbers of pieces
+            // (dies would get more than others)
             const int some = sq.tiles * PA_ROWS <= sq.chunk() * G ? a.together : 1, at = u / (sq.tiles * some) * some, n_at = min(some, sq.splits() - 1 - at);
             u -= at * sq.tiles;
             split = at + u % n_at;
@@ -535,8 +540,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         const float sum = row.l + other_half(row.l);
         const bool sees = !idle && limit >= key_begin + 32 * wk;                 // any of its wave's keys
         if (__syncthreads_or(sees && !(z < PA_LARGEST && sum > PA_LEAST && sum < PA_MOST))) {
-            // Once more, tile by tile, with a running maximum.  What a masked weight of zero makes of an infinity or a NaN in V must not count:
-            // such values leave the tile, and are added by hand to the rows that see them.
+            // Once more, tile by tile, with a running maximum.  What a masked weight of zero makes of an infinity or a NaN
+            // in V must not count: such values leave the tile, and are added by hand to the rows that see them.
             clear();
             for (t = 0; t < n_tiles; ++t) {
                 const int key = key_begin + t * PA_KEYS;
@@ -636,9 +641,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     }
 }
 
-// The pieces of the keys together, for 32 rows of a tile and 32 of their dimensions: wave v takes pieces v, v + PJ_WAVES, ..., PJ_AHEAD of them at a
-// time (what bounds this kernel is how long a read takes, not how much there is to read), a lane what the same lane of the attention kernel's wave
-// left: row lane % 32, four times four dimensions.  The waves' sums meet in LDS.
+// The pieces of the keys together, for 32 rows of a tile and 32 of their dimensions: wave v takes pieces v, v + PJ_WAVES, ...,
+// PJ_AHEAD of them at a time (what bounds this kernel is how long a read takes, not how much there is to read), a lane what the same
+// lane of the attention kernel's wave left: row lane % 32, four times four dimensions.  The waves' sums meet in LDS.
 constexpr int PJ_WAVES = 8, PJ_AHEAD = 4;
 template <int G, int KS>
 __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a)
@@ -736,11 +741,11 @@ Cut cut_of(int keys, int chunk)
 struct PromptPlan {
     int ks, chunk;         // waves to 32 rows; keys beyond which a sequence is cut, and about as many to a piece
 };
-// How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit to 640 drawn batches (1 to 12 sequences of 1 to 16K
-// tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each, whose times come out within 12 %; the plan with the
-// least is 1.5 % slower than the fastest of them on average.  Pieces against none: one token behind 131,072 102 us against 2185, 512 behind 120,001 900 against 1650
-// (eight KV heads, groups of four), 2,199 behind 59,264 of four heads 1007 against 1429; and where there are units enough, two pieces against none: 9,038 tokens of
-// four single heads 124 against 109.
+// How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit to 640 drawn batches (1 to
+// 12 sequences of 1 to 16K tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each, whose times come out
+// within 12 %; the plan with the least is 1.5 % slower than the fastest of them on average.  Pieces against none: one token behind
+// 131,072 102 us against 2185, 512 behind 120,001 900 against 1650 (eight KV heads, groups of four), 2,199 behind 59,264 of four heads
+// 1007 against 1429; and where there are units enough, two pieces against none: 9,038 tokens of four single heads 124 against 109.
 float plan_cost(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int ks, int chunk, int slots)
 {
     const int rows = 128 / ks;
@@ -767,9 +772,9 @@ float plan_cost(int n, const int* order, const int32_t* first, const int32_t* co
         kv += (f + c) * Hkv * 512.f;
     }
     if (room * rows > (long long)PA_ROOM * slots * 128) return -1.f;
-    // units of one length (whole pieces, tiles of a chunk behind many keys) leave some compute units one more than others; a prompt's tiles and
-    // last pieces are of all lengths and even out, the pieces less well.  The longest unit shares its compute unit as long as there are others;
-    // and what comes beyond what the GPU holds at a time finds an otherwise idle one.
+    // units of one length (whole pieces, tiles of a chunk behind many keys) leave some compute units one more than others; a
+    // prompt's tiles and last pieces are of all lengths and even out, the pieces less well.  The longest unit shares its compute
+    // unit as long as there are others; and what comes beyond what the GPU holds at a time finds an otherwise idle one.
     const float cus = 0.5f * slots, more = units > slots ? 1.f - slots / units : 0.f, last = units - floorf((units - 1.f) / slots) * slots;
     const float uneven = units > cus || room > 0 ? 1.f + (ceilf(units / cus) / (units / cus) - 1.f) * equal / work : 1.f;
     const float ragged = room > 0 ? 0.25f * std::min(1.f, 3.f * (1.f - equal / work)) : 0.f;
