@@ -8,12 +8,11 @@
 // maximum and sum stay inside a lane but for one exchange between the halves of the wave; and the registers that hold P^T are, rounded
 // to bf16, the second product's operand as they are: O^T = V^T P^T may take the keys of a step in any order as long as both operands
 // do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
-// A row's weights
-// are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights, sums and bf16 are
-// floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.  A workgroup that
-// finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that keeps masked
-// infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by inputs that
-// need it; all others save the running maximum's 2 %.
+// A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights,
+// sums and bf16 are floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.
+// A workgroup that finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that
+// keeps masked infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by
+// inputs that need it; all others save the running maximum's 2 %.
 //
 // Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.0 ms, 1.19
 // PFLOP/s, 86 % of what a bf16 product of 16384^3 reaches on the same card (1.39); in the loop the clock falls from 2.4 to 1.7 GHz,
