@@ -162,6 +162,7 @@ class LayerRuntime:
         if cfg.window_mode == hc.HC_WINDOW_RESCORED:
             self.q_window = torch.zeros((cfg.window, B, spec.Hq, D), dtype=torch.bfloat16, device=dev)
             self.rescore_work = torch.zeros((hc.hc_rescore_work_bytes(ctx.handle, self.handle),), dtype=torch.uint8, device=dev)
+        self.made = _Made(dev, self.arena, self.topk_idx, self.base_idx, self.ring, *(() if self.slot_pos is None else (self.slot_pos,)))
         if prefill is not None:
             self.prefill_init(data, prefill[0], prefill[1])
         # torch creates the HIP event lazily at the first record: do it now, the C ABI needs the handle
@@ -230,8 +231,11 @@ class LayerRuntime:
         if prompt.length != spec.ctx:
             raise ValueError("the prompt's sequences have other lengths than the layer's")
         self.kv_prefill, self._k_src, self._v_src = prompt.kv, prompt.k_off, prompt.v_off
+        prompt.made.used_on(stream)
+        self.made.used_on(stream)
         with _on(stream, self.ctx.device):
             self.prefill_work = torch.zeros((hc.hc_prefill_work_bytes(self.ctx.handle, self.handle),), dtype=torch.uint8, device=self.ctx.device)
+            q_last = q_last.to(self.ctx.device)
         self.prefill_init(None, q_last, pool, stream)
 
     def prefill_scores(self) -> dict:
@@ -330,12 +334,45 @@ def _on(stream, device):
     """What is allocated under it belongs to the stream that a call is given (None: the current one), so that its memory is not in another's use."""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device))
+    return torch.cuda.stream(_as_stream(stream, device))
+
+
+def _as_stream(stream, device):
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
+
+
+class _Made:
+    """Buffers that were allocated on the then current stream and may be used on another: that one waits for what was queued before they were
+    there (their fill, and the last use of their memory), and their memory is not given away before its work is through.  (While a graph is
+    captured neither is possible; a capture begins on an idle device, and its buffers have to outlive its replays.)"""
+
+    def __init__(self, device, *buffers: torch.Tensor):
+        self.device, self.buffers = device, buffers
+        self.stream = torch.cuda.current_stream(device)
+        self.event = None
+        if not torch.cuda.is_current_stream_capturing():
+            self.event = torch.cuda.Event()
+            self.event.record(self.stream)
+
+    def used_on(self, stream) -> None:
+        """Before a call on this stream (None: the current one)."""
+        s = _as_stream(stream, self.device)
+        if self.event is None or s.cuda_stream == self.stream.cuda_stream:
+            return
+        with torch.cuda.stream(s):
+            if torch.cuda.is_current_stream_capturing():
+                return
+        s.wait_event(self.event)
+        for x in self.buffers:
+            x.record_stream(s)
 
 
 class Prompt:
     """The prompt stage of one layer: a buffer with a K and a V block for every (sequence, KV head), room[b] rows each, that takes the
-    prompt in one or several chunks and attends over what is there."""
+    prompt in one or several chunks and attends over what is there.  Chunks may be put on any stream (one that is given as a bare handle has
+    to live as long as the Prompt does); chunks on different streams are put in order by the caller."""
 
     def __init__(self, ctx: Context, room: List[int]):
         self.ctx = ctx
@@ -349,7 +386,8 @@ class Prompt:
                 off += 2 * rows * D
         self.k_off, self.v_off = array("q", self.k_off), array("q", self.v_off)      # as the library takes them
         self.kv = torch.zeros((off,), dtype=torch.bfloat16, device=ctx.device)
-        self.work = torch.zeros((hc.hc_prefill_attn_work_bytes(ctx.handle),), dtype=torch.uint8, device=ctx.device)
+        self.work = torch.empty((hc.hc_prefill_attn_work_bytes(ctx.handle),), dtype=torch.uint8, device=ctx.device)
+        self.made = _Made(ctx.device, self.kv, self.work)
 
     def chunk(self, rope: hc.hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, count: List[int], stream=None):
         """The next count[b] tokens of every sequence, packed (q [T, Hq, D], k and v [T, Hkv, D], bf16 or f32): norm and rotation, rows to the
@@ -357,6 +395,7 @@ class Prompt:
         if any(n + c > r for n, c, r in zip(self.length, count, self.room)):
             raise ValueError("a sequence has no room for its chunk")
         T, Hq, dev = q.shape[0], self.ctx.cfg.Hq, self.ctx.device
+        self.made.used_on(stream)
         with _on(stream, dev):
             qr = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
             out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
