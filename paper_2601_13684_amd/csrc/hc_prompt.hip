@@ -10,7 +10,7 @@
 // do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
 // A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights,
 // sums and bf16 are floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.
-// A workgroup that finds a row outside of that, or a sum that is not finite, starts again with a running maximum (and in a form that
+// A workgroup that finds a row outside of that, a sum that is not finite or logits beyond 2^23, starts again with a running maximum (and in a form that
 // keeps masked infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by
 // inputs that need it; all others save the running maximum's 2 %.
 //
@@ -60,6 +60,11 @@ constexpr float PA_SLACK = 8.0f;                  // log2 units: where there is 
 // Where there is none: what a row's sum of weights lies between (below 2^-60 weights that are lost as denormals might count: 2^24 of
 // 2^-126), and what the magnitudes of a lane's 64 sums add up to (the join adds up to 2^11 of them, of at most 2^24 weights).
 constexpr float PA_LEAST = 0x1p-60f, PA_MOST = 0x1p100f, PA_LARGEST = 0x1p112f;
+
+// A weight's fused product and difference has only the difference's rounding.  Where the product is so large that rounding it moves it by more than half a
+// binary order, the reference, made from a rounded product, may lie any number of them from the product that it was made from: there (only in the second try) the
+// weights are taken of products rounded like it, and the row's largest weight is 1 again.
+constexpr float PA_FAR = 0x1p23f;
 
 constexpr int PA_SEQS = HC_PROMPT_SEQS, PA_HEADS = HC_PROMPT_HEADS;
 struct PromptSeq {
@@ -139,6 +144,13 @@ __device__ __forceinline__ float other_half(float x)
 __device__ __forceinline__ uint32_t pack2(float x, float y)
 {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+}
+
+// A logit in binary orders, as a number of its own (not part of a fused operation).
+__device__ __forceinline__ float rounded(float s)
+{
+#pragma clang fp contract(off)
+    return s * PA_SCALE;
 }
 
 // Every wave's loads to LDS have arrived, and every wave is through with the tile before.  (The barrier alone does not wait for them.)
@@ -310,13 +322,17 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, S[i]);
-        return fmaxf(top, other_half(top)) * PA_SCALE;
+        return rounded(fmaxf(top, other_half(top)));
     };
     // keys 8 s .. 8 s + 7 of a lane's 16
-    auto weigh = [&](f32x16& S, bf16x8 (&P)[2], int s) {
+    auto weigh = [&](f32x16& S, bf16x8 (&P)[2], int s, auto careful) {
         u32x4 x;
 #pragma unroll
-        for (int i = 8 * s; i < 8 * s + 8; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], PA_SCALE, -row.ref));
+        for (int i = 8 * s; i < 8 * s + 8; ++i) {
+            float t = fmaf(S[i], PA_SCALE, -row.ref);
+            if constexpr (careful()) t = fabsf(row.ref) < PA_FAR ? t : rounded(S[i]) - row.ref;
+            S[i] = __builtin_amdgcn_exp2f(t);
+        }
         float sum[2] = {S[8 * s], S[8 * s + 1]};
 #pragma unroll
         for (int i = 8 * s + 2; i < 8 * s + 8; ++i) sum[i & 1] += S[i];
@@ -325,9 +341,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         for (int e = 0; e < 4; ++e) x[e] = pack2(S[8 * s + 2 * e], S[8 * s + 2 * e + 1]);
         P[s] = __builtin_bit_cast(bf16x8, x);
     };
-    auto weights = [&](f32x16& S, bf16x8 (&P)[2]) {
-        weigh(S, P, 0);
-        weigh(S, P, 1);
+    auto weights = [&](f32x16& S, bf16x8 (&P)[2], auto careful) {
+        weigh(S, P, 0, careful);
+        weigh(S, P, 1, careful);
     };
     auto start = [&](float top) { row.ref = top == -INFINITY ? 0.f : ceilf(top); };
     // The running maximum of the second try, before weights are taken of logits up to `top`.
@@ -368,7 +384,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             if (8 * (i / 4) + i % 4 > see) S[i] = -INFINITY;
         if constexpr (careful()) settle(largest(S));
         else if (first) start(largest(S));
-        weights(S, P);
+        weights(S, P, careful);
         values(F, P);
     };
     {
@@ -395,7 +411,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 read_k(sm_k0, 1, K);
                 start(largest(S0));
                 logits(K, S1);
-                weights(S0, P0);
+                weights(S0, P0, std::false_type{});
                 tile_ready();
                 if (n_tiles > 1) load_v(1, B1{});
                 if (n_tiles > 2) load_k(2, B0{});
@@ -407,7 +423,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                     char* const tile_v = vbuf() ? sm_v1 : sm_v0;
                     read_v(tile_v, 0, V);
                     logits(K, S0);
-                    weights(S1, P1);
+                    weights(S1, P1, std::false_type{});
                     read_k(tile_k, 1, K);
                     values(V, P0);
                     interleave<8, 2, 4, 2>();
@@ -415,14 +431,14 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                     __builtin_amdgcn_sched_barrier(0);
                     read_v(tile_v, 1, V);
                     logits(K, S1);
-                    weigh(S0, P0, 0);
+                    weigh(S0, P0, 0, std::false_type{});
                     interleave<8, 2, 3, 1>();
                     tile_ready();
                     if (t + 3 < n_tiles) load(kb, t + 3, tile_k);
                     if (t + 2 < n_tiles) load(vb, t + 2, tile_v);
                     read_k(next_k, 0, K);
                     values(V, P1);
-                    weigh(S0, P0, 1);
+                    weigh(S0, P0, 1, std::false_type{});
                     interleave<8, 1, 3, 1>();
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -437,7 +453,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 }
                 const char* tile_v = t & 1 ? sm_v1 : sm_v0;
                 read_v(tile_v, 0, V);
-                weights(S1, P1);
+                weights(S1, P1, std::false_type{});
                 values(V, P0);
                 read_v(tile_v, 1, V);
                 values(V, P1);
@@ -466,14 +482,14 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                     char* const tile_v = odd() ? sm_v0 : sm_v1;          // of V t - 1
                     if (!begin()) read_v(tile_v, 0, V);
                     logits(K, S_next);
-                    weigh(S_now, P_now, 0);
+                    weigh(S_now, P_now, 0, std::false_type{});
                     interleave<8, 2, 3, 1>();
                     tile_ready();
                     if (t + 3 < n_tiles) load(kb, t + 3, spent_k);
                     if (!begin() && t + 1 < n_tiles) load(vb, t + 1, tile_v);
                     read_k(tile_k, 0, K);
                     if (!begin()) values(V, P_last);
-                    weigh(S_now, P_now, 1);
+                    weigh(S_now, P_now, 1, std::false_type{});
                     interleave<8, 1, 3, 1>();
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -494,8 +510,8 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                     if (t & 1) values(V, P0);
                     else values(V, P1);
                 }
-                if (t & 1) weights(S1, P1);
-                else weights(S0, P1);
+                if (t & 1) weights(S1, P1, std::false_type{});
+                else weights(S0, P1, std::false_type{});
                 tile_ready();
                 if (t > 0 && t + 1 < n_tiles) load(vb, t + 1, other_v);
                 read_v(tile_v, 0, V);
@@ -538,7 +554,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
             for (int i = 0; i < 16; ++i) z += fabsf(O[d][i]);
         const float sum = row.l + other_half(row.l);
         const bool sees = !idle && limit >= key_begin + 32 * wk;                 // any of its wave's keys
-        if (__syncthreads_or(sees && !(z < PA_LARGEST && sum > PA_LEAST && sum < PA_MOST))) {
+        if (__syncthreads_or(sees && !(z < PA_LARGEST && sum > PA_LEAST && sum < PA_MOST && fabsf(row.ref) < PA_FAR))) {
             // Once more, tile by tile, with a running maximum.  What a masked weight of zero makes of an infinity or a NaN
             // in V must not count: such values leave the tile, and are added by hand to the rows that see them.
             clear();
