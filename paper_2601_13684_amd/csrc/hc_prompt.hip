@@ -345,7 +345,9 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         weigh(S, P, 0, careful);
         weigh(S, P, 1, careful);
     };
-    auto start = [&](float top) { row.ref = top == -INFINITY ? 0.f : ceilf(top); };
+    // (Nothing but minus infinities: there is nothing to take weights against.  No weight is then larger than zero, and where the row sees other keys that
+    // sum sends it to the second try: with a reference made up here, what these keys' sum comes to might lie too far from it for the sums of other parts.)
+    auto start = [&](float top) { row.ref = top == -INFINITY ? INFINITY : ceilf(top); };
     // The running maximum of the second try, before weights are taken of logits up to `top`.
     auto settle = [&](float top) {
         if (!__builtin_amdgcn_ballot_w64(top > row.lim)) return;
