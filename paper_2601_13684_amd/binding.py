@@ -204,13 +204,19 @@ def _check(st: int, where: str, ctx=None):
         raise HcError(st, where, detail)
 
 
+# (B, Hq, Hkv) of the contexts made here, for the calls that are handed tensors with these dimensions
+_made = {}
+
+
 def hc_create(cfg: hc_config) -> int:
     h = C.c_void_p()
     _check(lib().hc_create(C.byref(cfg), C.byref(h)), "hc_create")
+    _made[h.value] = cfg.B, cfg.Hq, cfg.Hkv
     return h.value
 
 
 def hc_destroy(ctx: int) -> None:
+    _made.pop(ctx, None)
     _check(lib().hc_destroy(ctx), "hc_destroy")
 
 
@@ -404,25 +410,43 @@ def hc_rope_init(layout: int, rot_dim: int, theta: float, scaling: Optional[hc_r
     return r
 
 
-def _heads(x: torch.Tensor):
-    """(address, elements from token to token, tokens) of x [tokens, heads, 128], whose heads lie side by side."""
+def _row(x: torch.Tensor):
+    """(address, elements from token to token, tokens, heads) of x [tokens, heads, 128], whose heads lie side by side."""
     tokens, heads, width = x.shape
     step, between, one = x.stride()
     if width != 128 or one != 1 or (between != 128 and heads > 1):
         raise ValueError("projected heads are [tokens, heads, 128], a token's heads side by side")
-    return x.data_ptr(), step if tokens > 1 else 0, tokens
+    return x.data_ptr(), step if tokens > 1 else 0, tokens, heads
 
 
-def _qkv(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
+def _heads(x: torch.Tensor):
+    return _row(x)[:3]
+
+
+def _qkv(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, made=None):
+    """As the library takes them; made: (B, Hq, Hkv) of the context, which the heads have to be as many as (None, for one that was made elsewhere: its maker
+    sees to that)."""
     kind = q.dtype
-    (qp, qs, nq), (kp, ks, nk), (vp, vs, nv) = _heads(q), _heads(k), _heads(v)
+    (qp, qs, nq, hq), (kp, ks, nk, hk), (vp, vs, nv, hv) = _row(q), _row(k), _row(v)
     if kind is not k.dtype or kind is not v.dtype or nk != nq or nv != nq:
         raise ValueError("q, k and v are of one type and of as many tokens")
+    if made is not None and (hq != made[1] or hk != made[2] or hv != made[2]):
+        raise ValueError(f"{hq} query, {hk} key and {hv} value heads; the context (B, Hq, Hkv) has {made}")
     if kind is torch.bfloat16:
         return qp, kp, vp, qs, ks, vs, HC_BF16
     if kind is torch.float32:
         return qp, kp, vp, qs, ks, vs, HC_F32
     raise ValueError("projected heads are bf16 or f32")
+
+
+def _sized(x: Ptr, nbytes: int, what: str) -> Optional[int]:
+    """As _p, of a tensor of at least nbytes."""
+    if isinstance(x, torch.Tensor):
+        assert x.is_contiguous(), "tensors handed to the C ABI must be contiguous"
+        if x.nbytes < nbytes:
+            raise ValueError(f"{what} has {x.nbytes} bytes, the call's tokens {nbytes}")
+        return x.data_ptr()
+    return _p(x)
 
 
 def _ints(x: Sequence[int], code: str) -> array:
@@ -447,7 +471,12 @@ def hc_prefill_rope(ctx: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v
     first, count, k_off, v_off = _chunks(first, count, k_off, v_off)
     if sum(count) != len(q) or k.shape[1] * len(first) != len(k_off):
         raise ValueError("hc_prefill_rope: q has another number of tokens than count adds up to, or k_off another than first's sequences and k's heads")
-    _check(lib().hc_prefill_rope(ctx, C.byref(rope), *_qkv(q, k, v), _at(first), _at(count), _p(q_out), _p(kv_prefill), _at(k_off), _at(v_off),
+    made = _made.get(ctx)
+    if made is not None and len(first) != made[0]:
+        raise ValueError(f"hc_prefill_rope: {len(first)} sequences; the context (B, Hq, Hkv) has {made}")
+    rows = _qkv(q, k, v, made)
+    q_out = _sized(q_out, q.shape[0] * q.shape[1] * 256, "hc_prefill_rope: q_out")
+    _check(lib().hc_prefill_rope(ctx, C.byref(rope), *rows, _at(first), _at(count), q_out, _p(kv_prefill), _at(k_off), _at(v_off),
                                  _stream(stream)), "hc_prefill_rope", ctx)
 
 
@@ -457,15 +486,27 @@ def hc_prefill_attn_work_bytes(ctx: int) -> int:
 
 def hc_prefill_attn(ctx: int, q: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], first: Sequence[int], count: Sequence[int], out: Ptr,
                     lse: Ptr, work: Ptr, work_bytes: int, stream=None) -> None:
+    """q and out [T, Hq, 128] bf16, lse [T, Hq] f32 or None, T what count adds up to."""
     first, count, k_off, v_off = _chunks(first, count, k_off, v_off)
-    _check(lib().hc_prefill_attn(ctx, _p(q), _p(kv_prefill), _at(k_off), _at(v_off), _at(first), _at(count), _p(out), _p(lse), _p(work), work_bytes,
+    made, rows = _made.get(ctx), 0
+    if made is not None:
+        if len(first) != made[0] or len(k_off) != made[0] * made[2]:
+            raise ValueError(f"hc_prefill_attn: {len(first)} sequences and {len(k_off)} heads; the context (B, Hq, Hkv) has {made}")
+        rows = sum(count) * made[1]
+    q, out, lse = _sized(q, rows * 256, "hc_prefill_attn: q"), _sized(out, rows * 256, "hc_prefill_attn: out"), _sized(lse, rows * 4, "hc_prefill_attn: lse")
+    _check(lib().hc_prefill_attn(ctx, q, _p(kv_prefill), _at(k_off), _at(v_off), _at(first), _at(count), out, lse, _p(work), work_bytes,
                                  _stream(stream)), "hc_prefill_attn", ctx)
 
 
 def hc_append_rope(ctx: int, layer: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Ptr, kv_arena: Ptr,
                    host_tier: Ptr = None, stream=None) -> None:
     """q [B, Hq, 128], k and v [B, Hkv, 128]: tensors or views with any stride from sequence to sequence."""
-    _check(lib().hc_append_rope(ctx, layer, C.byref(rope), *_qkv(q, k, v), _p(q_out), _p(kv_arena), _p(host_tier), _stream(stream)), "hc_append_rope", ctx)
+    made, tokens = _made.get(ctx), q.shape
+    if made is not None and tokens[0] != made[0]:                 # (a row a sequence; from a single one nothing says how far the next is)
+        raise ValueError(f"hc_append_rope: rows of {tokens[0]} sequences; the context (B, Hq, Hkv) has {made}")
+    rows = _qkv(q, k, v, made)
+    q_out = _sized(q_out, tokens[0] * tokens[1] * 256, "hc_append_rope: q_out")
+    _check(lib().hc_append_rope(ctx, layer, C.byref(rope), *rows, q_out, _p(kv_arena), _p(host_tier), _stream(stream)), "hc_append_rope", ctx)
 
 
 def hc_layer_window_slot(layer: int) -> int:
