@@ -459,7 +459,7 @@ hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const void* q, const
  *     out[t,a,:] = softmax_j( q[t,a,:] . K_{b,h}[j,:] / sqrt(D) ) V_{b,h}[j,:],  h = a / G;   lse[t,a]: log-sum-exp of these logits.
  *   q      dev bf16 [T][Hq][128] (q_out of hc_prefill_rope);  kv_prefill, k_off, v_off, first, count: as there, rows 0 .. first + count - 1
  *          of every head present
- *   out    dev bf16 [T][Hq][128], not q itself;  lse  dev f32 [T][Hq] or NULL
+ *   out    dev bf16 [T][Hq][128], must not overlap q;  lse  dev f32 [T][Hq] or NULL
  *   work   dev, at least hc_prefill_attn_work_bytes(ctx) bytes (enough for every call of this context), 256-byte aligned, scratch:
  *          two calls that may overlap, captured ones among them, need one each
  * bf16 products on the matrix cores, everything else 32-bit, the logits too (any that 32 bits hold); the weights are rounded to bf16 for the second

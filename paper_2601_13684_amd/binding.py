@@ -494,6 +494,8 @@ def hc_prefill_attn(ctx: int, q: Ptr, kv_prefill: Ptr, k_off: Sequence[int], v_o
             raise ValueError(f"hc_prefill_attn: {len(first)} sequences and {len(k_off)} heads; the context (B, Hq, Hkv) has {made}")
         rows = sum(count) * made[1]
     q, out, lse = _sized(q, rows * 256, "hc_prefill_attn: q"), _sized(out, rows * 256, "hc_prefill_attn: out"), _sized(lse, rows * 4, "hc_prefill_attn: lse")
+    if rows and q and out and abs(q - out) < rows * 256:          # workgroups read queries while others' results are written
+        raise ValueError("hc_prefill_attn: out overlaps q")
     _check(lib().hc_prefill_attn(ctx, q, _p(kv_prefill), _at(k_off), _at(v_off), _at(first), _at(count), out, lse, _p(work), work_bytes,
                                  _stream(stream)), "hc_prefill_attn", ctx)
 

@@ -87,3 +87,15 @@ def test_larger_tensors_than_the_call_needs(calls):
     rope(q_out=heads(6, Hq))
     append(q_out=B * Hq + 1)
     assert len(calls) == 4
+
+
+def test_outputs_over_the_queries(calls):
+    """Parts of the keys are read against q until the last of them is through."""
+    x, off = heads(9, Hq), [8 * i for i in range(B * Hkv)]
+    for q, out in ((x[:5], x[:5]), (x[:5], x[4:]), (x[4:], x[:5]), (x.data_ptr(), x)):
+        with pytest.raises(ValueError, match="overlaps"):
+            hc.hc_prefill_attn(CTX, q, 4096, off, off, [0] * 3, [2, 0, 3], out, None, 4096, 1 << 40)
+    assert not calls
+    hc.hc_prefill_attn(CTX, x[:5], 4096, off, off, [0] * 3, [1, 0, 3], x[4:], None, 4096, 1 << 40)
+    hc.hc_prefill_attn(CTX, x, 4096, off, off, [0] * 3, [0] * 3, x, None, 4096, 1 << 40)             # nothing is read or written
+    assert len(calls) == 2
