@@ -69,7 +69,7 @@ static hc_status check_config(const hc_config* cfg)
     if (cfg->D != HC_D) return HC_ESHAPE;
     if (cfg->B < 1 || cfg->Hkv < 1 || cfg->Hq < 1 || cfg->Hq % cfg->Hkv != 0) return HC_EINVAL;
     const int G = cfg->Hq / cfg->Hkv;
-    if (G != 1 && G != 2 && G != 4 && G != 8) return HC_ESHAPE;
+    if (G > HC_MAX_G || (G & (G - 1)) != 0) return HC_ESHAPE;
     if (cfg->max_ctx < 64 || cfg->max_ctx % 64 != 0 || cfg->max_ctx > (1 << 24)) return HC_ESHAPE;
     if (cfg->max_k < 1 || cfg->max_k > cfg->max_ctx) return HC_EINVAL;
     if (cfg->window < 1 || cfg->window > HC_MAX_WINDOW) return HC_EINVAL;

@@ -11,6 +11,7 @@
 #include "../../include/hc.h"
 
 constexpr int HC_D = 128;            // head dimension the kernels are written for
+constexpr int HC_MAX_G = 8;          // query heads of a KV head: a power of two up to this
 constexpr int HC_UNIT_ROWS = 32;     // split-K granule: 4 waves x 8 rows
 constexpr int HC_SEL_CHUNK = 1024;   // candidates a workgroup or wave of the monitor's first passes takes at a time
 constexpr int HC_RADIX_BINS = 2048;  // bins of the monitor's histograms: 11 bits of a key, or of its distance from the smallest

@@ -197,7 +197,8 @@ __global__ __launch_bounds__(PR_BLK) void prefill_rope_kernel(RopeArgs r, Prompt
 
 // ---- the decode token ------------------------------------------------------------------------------------------------------
 
-constexpr int AR_MAX_BLK = (16 * (HC_MAX_GROUP + 2) + 63) / 64 * 64;     // (groups have up to eight heads)
+// Threads of a workgroup: 16 for each of the K row, the V row and the G query rows, whole waves.
+__host__ __device__ constexpr int append_threads(int G) { return (16 * (G + 2) + 63) / 64 * 64; }
 
 struct AppendRows {
     const void *q, *k, *v;
@@ -213,7 +214,7 @@ struct AppendRows {
 // One workgroup per KV head and sequence takes the token's K row, V row and the G query rows of the head's group: the position
 // is the head's length in the device's table, which the same workgroup moves on once all of it has read it.
 template <bool F32>
-__global__ __launch_bounds__(AR_MAX_BLK) void append_rope_kernel(RopeArgs r, AppendRows a)
+__global__ __launch_bounds__(append_threads(HC_MAX_G)) void append_rope_kernel(RopeArgs r, AppendRows a)
 {
     __shared__ float2 sm_turn[HC_D / 2];
     const int bh = blockIdx.x, b = bh / a.Hkv, h = bh - b * a.Hkv, tid = threadIdx.x;
@@ -337,7 +338,7 @@ hc_status hc_launch_append_rope(hc_ctx* ctx, const hc_layer* L, const hc_rope* r
     const RopeArgs r = rope_args(rope);
     const AppendRows a{in.q, in.k, in.v, in.q_stride, in.k_stride, in.v_stride, (uint16_t*)q_out, (uint16_t*)arena, (uint16_t*)tier,
                        L->heads, L->segs, L->blks, L->reps, ctx->cfg.Hkv, ctx->G};
-    const dim3 grid((unsigned)L->n_heads), block((unsigned)((16 * (ctx->G + 2) + 63) / 64 * 64));
+    const dim3 grid((unsigned)L->n_heads), block((unsigned)append_threads(ctx->G));
     if (in.f32) append_rope_kernel<true><<<grid, block, 0, st>>>(r, a);
     else append_rope_kernel<false><<<grid, block, 0, st>>>(r, a);
     HC_HIP(ctx, hipGetLastError());
