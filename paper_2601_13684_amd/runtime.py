@@ -13,7 +13,7 @@ from __future__ import annotations
 
 import contextlib
 from array import array
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Tuple, Union
 
 import torch
 
@@ -91,12 +91,13 @@ class Context:
 
 
 class LayerRuntime:
-    def __init__(self, ctx: Context, spec: LayerSpec, data: LayerData,
+    def __init__(self, ctx: Context, spec: LayerSpec, data: Union[LayerData, "Prompt"],
                  retrieved: Dict[Tuple[int, int], torch.Tensor], base: Dict[Tuple[int, int], torch.Tensor],
                  host_tier: bool = True, own_scratch: bool = False, delta_gather: bool = True, growth: int = 0,
                  prefill: Optional[Tuple[torch.Tensor, int]] = None):
         """``prefill = (q_last, pool)``: ``retrieved`` and ``base`` are ignored (may be None) and the library builds
-        the initial state itself from ``data`` and the last prompt token's queries (hc_prefill_init)."""
+        the initial state itself from ``data`` and the last prompt token's queries (hc_prefill_init); ``data`` may then be the
+        Prompt that has taken the layer's tokens."""
         self.ctx, self.spec = ctx, spec
         cfg, dev = ctx.cfg, ctx.device
         B, Hkv = spec.B, spec.Hkv
@@ -164,7 +165,10 @@ class LayerRuntime:
             self.rescore_work = torch.zeros((hc.hc_rescore_work_bytes(ctx.handle, self.handle),), dtype=torch.uint8, device=dev)
         self.made = _Made(dev, self.arena, self.topk_idx, self.base_idx, self.ring, *(() if self.slot_pos is None else (self.slot_pos,)))
         if prefill is not None:
-            self.prefill_init(data, prefill[0], prefill[1])
+            if isinstance(data, Prompt):
+                self.prefill_from(data, prefill[0], prefill[1])
+            else:
+                self.prefill_init(data, prefill[0], prefill[1])
         # torch creates the HIP event lazily at the first record: do it now, the C ABI needs the handle
         self.ev_topk = torch.cuda.Event()
         self.ev_done = torch.cuda.Event()
