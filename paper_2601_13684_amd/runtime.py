@@ -232,8 +232,8 @@ class LayerRuntime:
     def prefill_from(self, prompt: "Prompt", q_last: torch.Tensor, pool: int = 1, stream=None) -> None:
         """The same from a Prompt that has taken all of its tokens; q_last [B, Hq, 128]: the last tokens' rows of its queries."""
         spec = self.spec
-        if prompt.length != spec.ctx:
-            raise ValueError("the prompt's sequences have other lengths than the layer's")
+        if prompt.length != spec.ctx or len(prompt.k_off) != spec.B * spec.Hkv:
+            raise ValueError("the prompt's sequences have other lengths, or other heads, than the layer's")
         self.kv_prefill, self._k_src, self._v_src = prompt.kv, prompt.k_off, prompt.v_off
         prompt.made.used_on(stream)
         self.made.used_on(stream)

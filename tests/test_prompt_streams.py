@@ -111,7 +111,7 @@ def test_the_work_buffer_is_not_filled(prompt):
 @pytest.mark.parametrize("stream", [Stream(7), 7])
 def test_initialisation_on_another_stream(prompt, stream):
     lay = R.LayerRuntime.__new__(R.LayerRuntime)
-    lay.ctx, lay.spec, lay.handle = prompt.ctx, types.SimpleNamespace(ctx=[0]), 2
+    lay.ctx, lay.spec, lay.handle = prompt.ctx, types.SimpleNamespace(ctx=[0], B=1, Hkv=1), 2
     lay.arena = R.torch.zeros((5,))
     lay.made = R._Made("cuda:0", lay.arena)
     lay.prefill_init = lambda data, q, pool, stream: log.append(("init", stream, q))
@@ -122,3 +122,15 @@ def test_initialisation_on_another_stream(prompt, stream):
     assert after[-1] == ("init", stream, "q") and where == [7]                 # a copy of the queries is that stream's
     assert [e[1] for e in after if e[0] == "wait"] == [7, 7] and max(e[2] for e in after if e[0] == "wait") == at
     assert {id(e[2]) for e in after if e[0] == "keep"} == {id(prompt.kv), id(prompt.work), id(lay.arena)}
+
+
+@pytest.mark.parametrize("spec", [dict(ctx=[0], B=1, Hkv=2), dict(ctx=[1], B=1, Hkv=1), dict(ctx=[0, 0], B=2, Hkv=1)])
+def test_a_prompt_of_another_shape(prompt, spec):
+    """Its lists of offsets are as long as it has heads."""
+    lay = R.LayerRuntime.__new__(R.LayerRuntime)
+    lay.ctx, lay.spec = prompt.ctx, types.SimpleNamespace(**spec)
+    lay.prefill_init = lambda *a: pytest.fail("taken")
+    lay.made = R._Made("cuda:0")
+    lay.handle = 2
+    with pytest.raises(ValueError):
+        lay.prefill_from(prompt, types.SimpleNamespace(to=lambda device: "q"))
