@@ -419,8 +419,11 @@ enum { HC_ROPE_HALF = 0,          /* pairs (i, i + rot_dim/2)                   
 enum { HC_ROPE_LINEAR = 0,        /* every frequency divided by factor (positions interpolated)            */
        HC_ROPE_BASE = 1,          /* theta multiplied by factor^(rot_dim / (rot_dim - 2))                  */
        HC_ROPE_BANDS = 2 };       /* by full turns inside `original` positions: at most low: divided by factor; at least
-                                     high: kept; between them the two mixed linearly (usual: low 1, high 4; or low 1,
-                                     high 32 and a gain of 0.1 ln(factor) + 1)                             */
+                                     high: kept; between them the two mixed, linearly in the number of turns (usual: low
+                                     1, high 4).  Where a model mixes linearly in the pair's index i between two bounds
+                                     instead, as most that state bounds of 1 and 32 turns and a gain of 0.1 ln(factor) + 1
+                                     do, this is not its rule (frequencies up to 2.3 times off at factor 8): fill freq[]
+                                     with its own, and set gain                                            */
 /* What happens to a query or key head: y = x (mean(x^2) + eps)^(-1/2) w over its 128 elements (only where w is given), then the pairs of
  * its first rot_dim elements turn by position * freq[i]:  (u, v) -> gain (u cos - v sin, v cos + u sin).  The elements behind
  * rot_dim are not turned and not multiplied by gain.  A plain struct: set or change any field. */
