@@ -14,11 +14,12 @@
 // keeps masked infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by
 // inputs that need it; all others save the running maximum's 2 %.
 //
-// Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.0 ms, 1.19
-// PFLOP/s, 86 % of what a bf16 product of 16384^3 reaches on the same card (1.39); in the loop the clock falls from 2.4 to 1.7 GHz,
-// and changes of the schedule that leave the matrix cores idle less let it fall further.  8,192 tokens 488 us, 1.13 PFLOP/s.  Few rows
-// behind many keys are bound by memory: 17 tokens behind four contexts of 20K to 90K 166 us, 5.5 TB/s.  Below about 2,000 tokens: the
-// loads before the first product, and too few units (200 tokens 8 us, 1,024 18.5).
+// Bound: the matrix cores at the clock that their power leaves.  32,003 tokens (eight KV heads, groups of four) take 7.1 ms, 1.18
+// PFLOP/s, 86 % of what a bf16 product of 16384^3 reaches on the same card (1.37; from card to card 6.9 to 7.4 ms); in the loop the
+// clock falls from 2.4 to 1.7 GHz, and changes of the schedule that leave the matrix cores idle less let it fall further.  8,192 tokens
+// 494 us, 1.11 PFLOP/s (476 to 502).  Few rows behind many keys are bound by memory: 17 tokens behind four contexts of 20K to 90K 166
+// us, 5.5 TB/s.  Prompts of a few hundred to about 6,000 tokens are two to eight times above either bound: the loads before the first product, units
+// too few or of unequal length, and a second launch where keys are cut (200 tokens 8 us, 1,024 18.5).
 //
 // P is rounded to bf16 for the matrix cores, to the nearest: the error of an output is that of at most 2^-8 per weight, independent
 // from key to key, about what the output's own rounding to bf16 adds.  Sum, maximum, lse and accumulators are 32-bit, the sum
@@ -758,9 +759,10 @@ Cut cut_of(int keys, int chunk)
 struct PromptPlan {
     int ks, chunk;         // waves to 32 rows; keys beyond which a sequence is cut, and about as many to a piece
 };
-// How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit to 640 drawn batches (1 to
-// 12 sequences of 1 to 16K tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each, whose times come out
-// within 12 %; the plan with the least is 1.5 % slower than the fastest of them on average.  Pieces against none: one token behind
+// How long a call takes, in microseconds; < 0: the partial results have no room.  The constants are a fit on one card to 640 drawn
+// batches (1 to 12 sequences of 1 to 16K tokens behind up to 128K, 1 to 8 KV heads, groups of 1 to 8) under 5 to 28 plans each.  Over 780
+// batches measured with the plans made from it, the plan with the least was 3 % slower than the fastest of them on average, at worst 1.6
+// times; times come out 11 % off on average, a third of them more than 12 %, and calls below 10 us too short.  Pieces against none: one token behind
 // 131,072 102 us against 2185, 512 behind 120,001 900 against 1650 (eight KV heads, groups of four), 2,199 behind 59,264 of four heads
 // 1007 against 1429; and where there are units enough, two pieces against none: 9,038 tokens of four single heads 124 against 109.
 float plan_cost(int n, const int* order, const int32_t* first, const int32_t* count, int G, int Hkv, int ks, int chunk, int slots)
