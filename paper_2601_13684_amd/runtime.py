@@ -163,7 +163,7 @@ class LayerRuntime:
         if cfg.window_mode == hc.HC_WINDOW_RESCORED:
             self.q_window = torch.zeros((cfg.window, B, spec.Hq, D), dtype=torch.bfloat16, device=dev)
             self.rescore_work = torch.zeros((hc.hc_rescore_work_bytes(ctx.handle, self.handle),), dtype=torch.uint8, device=dev)
-        self.made = _Made(dev, self.arena, self.topk_idx, self.base_idx, self.ring, *(() if self.slot_pos is None else (self.slot_pos,)))
+        self.made = _Made(dev)
         if prefill is not None:
             if isinstance(data, Prompt):
                 self.prefill_from(data, prefill[0], prefill[1])
@@ -235,8 +235,8 @@ class LayerRuntime:
         if prompt.length != spec.ctx or len(prompt.k_off) != spec.B * spec.Hkv:
             raise ValueError("the prompt's sequences have other lengths, or other heads, than the layer's")
         self.kv_prefill, self._k_src, self._v_src = prompt.kv, prompt.k_off, prompt.v_off
-        prompt.made.used_on(stream)
-        self.made.used_on(stream)
+        prompt.made.used_on(stream, prompt.kv)
+        self.made.used_on(stream, self.arena, self.topk_idx, self.base_idx, self.ring, *(() if self.slot_pos is None else (self.slot_pos,)))
         with _on(stream, self.ctx.device):
             self.prefill_work = torch.zeros((hc.hc_prefill_work_bytes(self.ctx.handle, self.handle),), dtype=torch.uint8, device=self.ctx.device)
             q_last = q_last.to(self.ctx.device)
@@ -348,19 +348,19 @@ def _as_stream(stream, device):
 
 
 class _Made:
-    """Buffers that were allocated on the then current stream and may be used on another: that one waits for what was queued before they were
-    there (their fill, and the last use of their memory), and their memory is not given away before its work is through.  (While a graph is
-    captured neither is possible; a capture begins on an idle device, and its buffers have to outlive its replays.)"""
+    """When and where an object's buffers were allocated, on the then current stream.  Another one that they are used on waits for what was queued
+    before they were there (their fill, and the last use of their memory), and their memory is not given away before its work is through.  (While a
+    graph is captured neither is possible; a capture begins on an idle device, and its buffers have to outlive its replays.)"""
 
-    def __init__(self, device, *buffers: torch.Tensor):
-        self.device, self.buffers = device, buffers
+    def __init__(self, device):
+        self.device = device
         self.stream = torch.cuda.current_stream(device)
         self.event = None
         if not torch.cuda.is_current_stream_capturing():
             self.event = torch.cuda.Event()
             self.event.record(self.stream)
 
-    def used_on(self, stream) -> None:
+    def used_on(self, stream, *buffers: torch.Tensor) -> None:
         """Before a call on this stream (None: the current one)."""
         s = _as_stream(stream, self.device)
         if self.event is None or s.cuda_stream == self.stream.cuda_stream:
@@ -369,7 +369,7 @@ class _Made:
             if torch.cuda.is_current_stream_capturing():
                 return
         s.wait_event(self.event)
-        for x in self.buffers:
+        for x in buffers:
             x.record_stream(s)
 
 
@@ -391,7 +391,7 @@ class Prompt:
         self.k_off, self.v_off = array("q", self.k_off), array("q", self.v_off)      # as the library takes them
         self.kv = torch.zeros((off,), dtype=torch.bfloat16, device=ctx.device)
         self.work = torch.empty((hc.hc_prefill_attn_work_bytes(ctx.handle),), dtype=torch.uint8, device=ctx.device)
-        self.made = _Made(ctx.device, self.kv, self.work)
+        self.made = _Made(ctx.device)
 
     def chunk(self, rope: hc.hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, count: List[int], stream=None):
         """The next count[b] tokens of every sequence, packed (q [T, Hq, D], k and v [T, Hkv, D], bf16 or f32): norm and rotation, rows to the
@@ -399,7 +399,7 @@ class Prompt:
         if any(n + c > r for n, c, r in zip(self.length, count, self.room)):
             raise ValueError("a sequence has no room for its chunk")
         T, Hq, dev = q.shape[0], self.ctx.cfg.Hq, self.ctx.device
-        self.made.used_on(stream)
+        self.made.used_on(stream, self.kv, self.work)
         with _on(stream, dev):
             qr = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)
             out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev)

@@ -63,3 +63,53 @@ def test_a_chunk_captured():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, eager))
     ctx.close()
+
+
+@pytest.mark.parametrize("where", [0, "current"])
+def test_a_chunk_on_the_default_stream(where):
+    """By its handle, or as the current one of another stream's context."""
+    lens = [200]
+    spec = I.LayerSpec(B=1, Hq=4, Hkv=1, D=D, ctx=lens, heads=[[I.HeadSpec(I.ROLE_FULL)]])
+    ctx = R.Context(R.make_config(spec), DEV)
+    rope = hc.hc_rope_init(hc.HC_ROPE_HALF, 128, 10000.0)
+    x = torch.randn((200, 6, D), device=DEV).to(torch.bfloat16)
+    qkv = x[:, :4], x[:, 4:5], x[:, 5:]
+    want = R.Prompt(ctx, lens).chunk(rope, *qkv, lens)
+    torch.cuda.synchronize()
+    if where == 0:
+        got = R.Prompt(ctx, lens).chunk(rope, *qkv, lens, stream=0)
+    else:
+        prompt = R.Prompt(ctx, lens)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = prompt.chunk(rope, *qkv, lens)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ctx.close()
+
+
+def test_a_layer_made_on_another_stream():
+    """prefill_from on a side stream, the current one busy in front of the layer's own fills: the layer is what it is on the current stream."""
+    Hkv, G, lens = 2, 4, [900]
+    heads = [[I.HeadSpec(I.ROLE_FULL), I.HeadSpec(I.ROLE_SATELLITE, rep=0, sink=4, recent=16, budget=120)]]
+    spec = I.LayerSpec(B=1, Hq=Hkv * G, Hkv=Hkv, D=D, ctx=lens, heads=heads)
+    ctx = R.Context(R.make_config(spec), DEV)
+    rope = hc.hc_rope_init(hc.HC_ROPE_HALF, 128, 10000.0)
+    x = torch.randn((900, Hkv * (G + 2), D), device=DEV).to(torch.bfloat16)
+    prompt = R.Prompt(ctx, lens)
+    q, _, _ = prompt.chunk(rope, x[:, :Hkv * G], x[:, Hkv * G:-Hkv], x[:, -Hkv:], lens)
+    want = R.LayerRuntime(ctx, spec, prompt, None, None, prefill=(q[-1:], 1))
+    busy, side = torch.empty((1 << 28,), device=DEV), torch.cuda.Stream()
+    zeros = {(0, h): torch.zeros((900, D), dtype=torch.bfloat16) for h in range(2)}
+    for _ in range(3):
+        torch.cuda.synchronize()
+        for _ in range(40):
+            busy.fill_(1.0)
+        lay = R.LayerRuntime(ctx, spec, I.LayerData(zeros, zeros, {}), {(0, 1): torch.arange(4, 104)}, {})
+        lay.prefill_from(prompt, q[-1:].cpu(), 1, side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        for name in ("arena", "tier", "topk_idx", "base_idx", "slot_pos", "ring"):
+            assert torch.equal(getattr(lay, name), getattr(want, name)), name
+        lay.close()
+    want.close()
+    ctx.close()

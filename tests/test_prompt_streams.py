@@ -113,7 +113,8 @@ def test_initialisation_on_another_stream(prompt, stream):
     lay = R.LayerRuntime.__new__(R.LayerRuntime)
     lay.ctx, lay.spec, lay.handle = prompt.ctx, types.SimpleNamespace(ctx=[0], B=1, Hkv=1), 2
     lay.arena = R.torch.zeros((5,))
-    lay.made = R._Made("cuda:0", lay.arena)
+    lay.topk_idx, lay.base_idx, lay.ring, lay.slot_pos = (R.torch.zeros((5,)) for _ in range(4))
+    lay.made = R._Made("cuda:0")
     lay.prefill_init = lambda data, q, pool, stream: log.append(("init", stream, q))
     at = len(log)
     where = []
@@ -121,7 +122,7 @@ def test_initialisation_on_another_stream(prompt, stream):
     after = log[at:]
     assert after[-1] == ("init", stream, "q") and where == [7]                 # a copy of the queries is that stream's
     assert [e[1] for e in after if e[0] == "wait"] == [7, 7] and max(e[2] for e in after if e[0] == "wait") == at
-    assert {id(e[2]) for e in after if e[0] == "keep"} == {id(prompt.kv), id(prompt.work), id(lay.arena)}
+    assert {id(e[2]) for e in after if e[0] == "keep"} == {id(x) for x in (prompt.kv, lay.arena, lay.topk_idx, lay.base_idx, lay.ring, lay.slot_pos)}
 
 
 @pytest.mark.parametrize("spec", [dict(ctx=[0], B=1, Hkv=2), dict(ctx=[1], B=1, Hkv=1), dict(ctx=[0, 0], B=2, Hkv=1)])
@@ -134,3 +135,12 @@ def test_a_prompt_of_another_shape(prompt, spec):
     lay.handle = 2
     with pytest.raises(ValueError):
         lay.prefill_from(prompt, types.SimpleNamespace(to=lambda device: "q"))
+
+
+def test_buffers_that_are_let_go(prompt):
+    """Nothing but the attributes holds them."""
+    import weakref
+    gone = weakref.ref(prompt.kv)
+    log.clear()
+    prompt.kv = None
+    assert gone() is None
