@@ -466,7 +466,7 @@ hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const void* q, const
  *   work   dev, at least hc_prefill_attn_work_bytes(ctx) bytes (enough for every call of this context), 256-byte aligned, scratch:
  *          two calls that may overlap, captured ones among them, need one each
  * bf16 products on the matrix cores, everything else 32-bit, the logits too (any that 32 bits hold); the weights are rounded to bf16 for the second
- * product.  Sums over the keys are divided at the end: finite values of V beyond 2^90 may come out as infinities.  A value of V that is
+ * product.  Sums over the keys are divided at the end: finite values of V beyond 2^90 (2^75 where logits pass 2^22) may come out as infinities.  A value of V that is
  * not finite reaches the rows that see it and no others.  One token a sequence is a call like any other: its keys are split over the GPU. */
 size_t hc_prefill_attn_work_bytes(const hc_ctx* ctx);
 hc_status hc_prefill_attn(hc_ctx* ctx, const void* q, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,

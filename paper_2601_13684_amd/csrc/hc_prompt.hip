@@ -10,7 +10,7 @@
 // do, and V is read from LDS transposed (ds_read_b64_tr_b16) in the order that S^T leaves.  One pass over the keys.
 // A row's weights are 2^(t - ref), t the scaled logit, ref the largest of its first 32 keys rounded up to a whole number: weights,
 // sums and bf16 are floating point, so that ref need not be the row's maximum to the end, only within a hundred binary orders of it.
-// A workgroup that finds a row outside of that, a sum that is not finite or logits beyond 2^23, starts again with a running maximum (and in a form that
+// A workgroup that finds a row outside of that, a sum that is not finite or logits beyond 2^29, starts again with a running maximum (and in a form that
 // keeps masked infinities and NaNs of V out): what that costs, 2.1 to 2.3 times a call's time where every workgroup does, is paid by
 // inputs that need it; all others save the running maximum's 2 %.
 //
@@ -62,10 +62,12 @@ constexpr float PA_SLACK = 8.0f;                  // log2 units: where there is 
 // 2^-126), and what the magnitudes of a lane's 64 sums add up to (the join adds up to 2^11 of them, of at most 2^24 weights).
 constexpr float PA_LEAST = 0x1p-60f, PA_MOST = 0x1p100f, PA_LARGEST = 0x1p112f;
 
-// A weight's fused product and difference has only the difference's rounding.  Where the product is so large that rounding it moves it by more than half a
-// binary order, the reference, made from a rounded product, may lie any number of them from the product that it was made from: there (only in the second try) the
-// weights are taken of products rounded like it, and the row's largest weight is 1 again.
-constexpr float PA_FAR = 0x1p23f;
+// A weight's fused product and difference has only the difference's rounding, but its reference comes from a rounded product, and may lie up to half a step
+// of that from the product that it was made from.  As far as here that is 16 binary orders, and a row's largest weight 2^16 at most before slack; from 2^31 on
+// it is more than the exponents hold.  Beyond (only in the second try) references are logits as they leave the first product, not scaled: their steps are at least
+// 32 binary orders, so that logits are equal or nothing to each other.  A logit is larger than its scaled value, so that references of both kinds have one order, and
+// whenever two of them differ and one is of the second kind, by more than the exponents hold: f = exp2(difference) serves both.
+constexpr float PA_FAR = 0x1p29f;
 
 constexpr int PA_SEQS = HC_PROMPT_SEQS, PA_HEADS = HC_PROMPT_HEADS;
 struct PromptSeq {
@@ -147,11 +149,15 @@ __device__ __forceinline__ uint32_t pack2(float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
 }
 
-// A logit in binary orders, as a number of its own (not part of a fused operation).
-__device__ __forceinline__ float rounded(float s)
+// What a row's weights are taken against, of its largest logit.
+__device__ __forceinline__ float reference(float s)
 {
-#pragma clang fp contract(off)
-    return s * PA_SCALE;
+    const float t = s * PA_SCALE;
+    return fabsf(t) < PA_FAR ? ceilf(t) : s;
+}
+__device__ __forceinline__ float lse_of(float ref, float l)
+{
+    return ((fabsf(ref) < PA_FAR ? ref : ref * PA_SCALE) + __builtin_amdgcn_logf(l)) * PA_LN2;
 }
 
 // Every wave's loads to LDS have arrived, and every wave is through with the tile before.  (The barrier alone does not wait for them.)
@@ -323,7 +329,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, S[i]);
-        return rounded(fmaxf(top, other_half(top)));
+        return fmaxf(top, other_half(top));
     };
     // keys 8 s .. 8 s + 7 of a lane's 16
     auto weigh = [&](f32x16& S, bf16x8 (&P)[2], int s, auto careful) {
@@ -331,7 +337,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
 #pragma unroll
         for (int i = 8 * s; i < 8 * s + 8; ++i) {
             float t = fmaf(S[i], PA_SCALE, -row.ref);
-            if constexpr (careful()) t = fabsf(row.ref) < PA_FAR ? t : rounded(S[i]) - row.ref;
+            if constexpr (careful()) t = fabsf(row.ref) < PA_FAR ? t : S[i] - row.ref;
             S[i] = __builtin_amdgcn_exp2f(t);
         }
         float sum[2] = {S[8 * s], S[8 * s + 1]};
@@ -348,11 +354,12 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
     };
     // (Nothing but minus infinities: there is nothing to take weights against.  No weight is then larger than zero, and where the row sees other keys that
     // sum sends it to the second try: with a reference made up here, what these keys' sum comes to might lie too far from it for the sums of other parts.)
-    auto start = [&](float top) { row.ref = top == -INFINITY ? INFINITY : ceilf(top); };
+    auto start = [&](float top) { row.ref = top == -INFINITY ? INFINITY : ceilf(top * PA_SCALE); };
     // The running maximum of the second try, before weights are taken of logits up to `top`.
     auto settle = [&](float top) {
-        if (!__builtin_amdgcn_ballot_w64(top > row.lim)) return;
-        const float ref = row.lim == -INFINITY ? ceilf(top) : fmaxf(row.ref, ceilf(top));
+        const float next = reference(top);
+        if (!__builtin_amdgcn_ballot_w64(next > row.lim)) return;
+        const float ref = row.lim == -INFINITY ? next : fmaxf(row.ref, next);
         const bool none = top == -INFINITY && row.lim == -INFINITY;
         const float f = row.lim == -INFINITY ? 0.f : ref == row.ref ? 1.f : __builtin_amdgcn_exp2f(row.ref - ref);
         if (!none) {
@@ -649,7 +656,7 @@ __global__ __launch_bounds__(PA_BLK, 2) void prompt_attn_kernel(PromptArgs a)
                 swap_halves32(x1, y1);
                 *reinterpret_cast<u32x4*>(to + 32 * d + 16 * i) = u32x4{x0, x1, y0, y1};
             }
-        if (a.lse && half == 0) a.lse[row_out] = (row.ref + __builtin_amdgcn_logf(l)) * PA_LN2;
+        if (a.lse && half == 0) a.lse[row_out] = lse_of(row.ref, l);
     } else {
         // as the registers lie: 1 KB to a store
         f32x4* to = reinterpret_cast<f32x4*>(a.part_acc) + ((size_t)place * (PA_ROWS / 32) + wr) * 1024 + (late & 63);
@@ -737,7 +744,7 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void prompt_join_kernel(PromptArgs a
     const float inv = 1.0f / l;
     const size_t at = ((size_t)(sq.tok0 + (w0 + n) / G) * a.Hkv + h) * G + (w0 + n) % G;
     *reinterpret_cast<u32x2*>(a.out + at * HC_D + dims * 32 + v * 8 + 4 * half) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
-    if (a.lse && half == 0 && v == 0 && dims == 0) a.lse[at] = (zero + __builtin_amdgcn_logf(l)) * PA_LN2;
+    if (a.lse && half == 0 && v == 0 && dims == 0) a.lse[at] = lse_of(zero, l);
 }
 
 template <int G, int KS>

@@ -71,3 +71,26 @@ def test_one_key_far_from_zero(k, e):
     torch.cuda.synchronize()
     P.check_attention(c.out[:200], c.lse[:200], want(c), (k, e))
     c.close()
+
+
+@pytest.mark.parametrize("first,count,Hkv,G", SHAPES)
+@pytest.mark.parametrize("e", [20, 24, 26, 28, 30, 31, 32, 33, 34, 36, 40, 60, 100, 124])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_neighbouring_logits(first, count, Hkv, G, e, sign):
+    """Logits one step of 32 bits apart (two products, their sum exact): by e the step is nothing, a few binary orders, or all the difference there is.  Half of the
+    heads have their logits just below a power of two, where a step of the logit is less than one of the logit in binary orders."""
+    c = Call(first, count, Hkv, G, seed=e)
+    c.q.zero_()
+    q = c.q.view(c.T, Hkv, G, P.D)
+    q[..., 9], q[..., 10] = sign * 2.0 ** (e // 2), 2.0 ** (e // 2 - 20)
+    for b, (f, n) in enumerate(zip(first, count)):
+        step = (torch.arange(f + n, device=DEV) * 7 % 11 - 5).to(torch.bfloat16)
+        for h in range(Hkv):
+            rows = c.kv[c.k_off[b * Hkv + h]:][:(f + n) * P.D].view(f + n, P.D)
+            rows.zero_()
+            rows[:, 9] = (1.984375 if h % 2 == 0 else 1.40625) * 2.0 ** (e - e // 2)
+            rows[:, 10] = step * 2.0 ** (e - e // 2 - 3)
+    c.run()
+    torch.cuda.synchronize()
+    P.check_attention(c.out[:c.T], c.lse[:c.T], want(c), (first, count, e))
+    c.close()
