@@ -1,0 +1,539 @@
+"""The operators of a KV cache held in 4 bits, as measurable cases: rows into it and back, decode attention over it, eviction by accumulated weight.
+
+Kinds of case:
+  store   hc_kv4_store, then hc_kv4_load: a prompt's (or a chunk's) K and V rows into the cache, and the rows as the cache holds them
+  append  hc_kv4_append, then hc_kv4_load: norm and rotation of the decode token, its rows into the cache, and the rows as the cache holds them
+  attn    hc_kv4_attn: attention of the decode token over the cache; with ``acc`` every row's share of the weights is added to what it had
+  evict   hc_kv4_evict, then hc_kv4_load: the rows that keep their place by accumulated weight go to a smaller cache, and what it then holds
+
+A row of 128 values is 64 bytes of codes (element i in bits 4 (i % 8) .. of word i / 8: sign, then one of 0 .5 1 1.5 2 3 4 6) and four scale bytes s,
+one per 32 values, for the factor 2^(s - 127): the smallest power of two, at least 2^-125, of which no value is more than 7 times.  A head's block of
+``cap`` rows: codes of K, scales of K, codes of V, scales of V.
+
+``rows`` of a case: what every head holds before the call, a number a sequence or a number a (sequence, KV head).
+"""
+import math
+
+import torch
+
+own = False
+DEV = "cuda:0"
+D = 128
+EPS = 1e-6
+GROW = 98304         # decode tokens that a measured cache has room for
+SCALING = dict(bands=dict(factor=8.0, low=1.0, high=4.0, original=8192))
+MOST_PADDED = 2_200_000     # heads times rows of the longest: what a drawn case may cost
+
+
+def _case(name, kind, rows, B, Hkv=8, G=4, **more):
+    c = dict(kind=kind, rows=rows, B=B, Hkv=Hkv, G=G)
+    if name:
+        c["name"] = name
+    c.update(more)
+    return c
+
+
+def _list(values):
+    return ",".join(str(int(v)) for v in values)
+
+
+def listed():
+    ragged = [8 + 517 * i for i in range(64)]
+    return [
+        # A short chunk behind a prefix that stays (several answers to one prompt), small layer: launch latency.
+        _case("store_17", "store", "4001", 1, Hkv=2, count="17"),
+        # The prompt of the 32K configuration, one layer.
+        _case("store_32k", "store", "0", 1, count="32003"),
+        # A serving batch's ragged prompts, new ones and chunks behind what is there.
+        _case("store_batch", "store", "0,777,2048,0,1500,1,0,2049", 8, count="8192,1024,0,5001,640,4096,1,12000"),
+        # The decode token of one small layer.
+        _case("append_1", "append", "4096", 1, Hkv=2, rot=128, pairs="half", scaling="none", norm=True, type="bf16", theta=10000.0),
+        # The decode tokens of a large serving batch.
+        _case("append_64", "append", _list(2048 + 517 * i for i in range(64)), 64, rot=128, pairs="interleaved", scaling="bands", norm=True, type="bf16",
+              theta=500000.0),
+        # One short context on a small layer: latency.
+        _case("attn_500", "attn", "500", 1, Hkv=2, acc=False, decay=1.0),
+        # The longest configuration's context, every head whole: what reading the cache costs.
+        _case("attn_224k", "attn", "229376", 1, acc=False, decay=1.0),
+        # The same context with two whole heads and six of fixed budgets, weights accumulated for the eviction.
+        _case("attn_hetero", "attn", "229376,229376,8192,4096,4096,2048,2048,1024", 1, acc=True, decay=1.0),
+        # A serving batch of very different lengths, eight query heads to a KV head; one sequence has nothing yet.
+        _case("attn_batch", "attn", "32001,1,8192,20011,0,4097,130,16384,257,12345,64,30000,9001,2500,700,27777", 16, Hkv=4, G=8, acc=True, decay=0.98),
+        # A small layer that has grown 256 tokens past its budget.
+        _case("evict_2k", "evict", "2304", 1, Hkv=2, budget="2048", sink=64, recent=128),
+        # The longest configuration's prompt brought to its budgets, every head to its own.
+        _case("evict_224k", "evict", "229376", 1, budget="65536,32768,8192,4096,4096,2048,2048,1024", sink=64, recent=128),
+        # A serving batch, where some sequences are below their budget.
+        _case("evict_batch", "evict", _list(ragged), 64, budget="4096", sink=4, recent=1000),
+    ]
+
+
+def _logint(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["store", "append", "attn", "attn", "attn", "evict", "evict"])
+    Hkv, G = rng.choice([1, 2, 4, 8, 8]), rng.choice([1, 2, 4, 4, 8])
+    if kind == "store":
+        B = rng.choice([1, 1, 2, 5, 9])
+        count = [_logint(rng, 1, 32768 // (1 if B == 1 else 4)) for _ in range(B)]
+        return _case(None, kind, _list(rng.choice([0, _logint(rng, 1, 8192)]) for _ in range(B)), B, Hkv, G, count=_list(count))
+    if kind == "append":
+        B = _logint(rng, 1, 64)
+        return _case(None, kind, _list(_logint(rng, 1, 32768) for _ in range(B)), B, Hkv, G, rot=rng.choice([128, 128, 64, 32, 96]),
+                     pairs=rng.choice(["half", "interleaved"]), scaling=rng.choice(["none", "bands"]), norm=rng.choice([True, False]),
+                     type=rng.choice(["bf16", "bf16", "f32"]), theta=rng.choice([10000.0, 500000.0]))
+    B = rng.choice([1, 1, 2, 5, 16, 40])
+    most = min(229376, MOST_PADDED // (B * Hkv))
+    if kind == "attn":
+        each = B * Hkv if rng.random() < 0.5 else B          # every head a length of its own
+        rows = [_logint(rng, 1, most) if rng.random() < 0.95 else 0 for _ in range(each)]
+        return _case(None, kind, _list(rows), B, Hkv, G, acc=rng.choice([True, False]), decay=rng.choice([1.0, 0.9, 0.99]))
+    rows = [_logint(rng, 1, most) for _ in range(B)]
+    budget = [_logint(rng, 160, 65536) for _ in range(rng.choice([1, B * Hkv]))]
+    return _case(None, kind, _list(rows), B, Hkv, G, budget=_list(budget), sink=rng.choice([0, 4, 64]), recent=rng.choice([1, 32, 96]))
+
+
+def _ints(s):
+    return [int(x) for x in str(s).split(",")]
+
+
+def _per_head(c, s):
+    """A number a (sequence, KV head)."""
+    v, n = _ints(s), c["B"] * c["Hkv"]
+    if len(v) == 1:
+        return v * n
+    return v if len(v) == n and n != c["B"] else [x for x in v for _ in range(c["Hkv"])]
+
+
+def _up(n):
+    return max(64, (n + 63) // 64 * 64)
+
+
+# ---- what a user's program holds ------------------------------------------------------------------------------------------------------
+
+class Table:
+    """Where every head's block is: byte offset in the cache, first element in the tables of a number a row, rows that it has room for."""
+
+    def __init__(self, caps):
+        self.caps, self.off, self.row_off, at, row = caps, [], [], 0, 0
+        for cap in caps:
+            self.off.append(at)
+            self.row_off.append(row)
+            at += 136 * cap
+            row += cap
+        self.bytes, self.rows = at, row
+        self.block, self.first, self.cap = (torch.tensor(x, dtype=torch.int64, device=DEV) for x in (self.off, self.row_off, caps))
+
+    def codes(self, v):
+        """Of K (v: V) row 0 of every head, in units of 64 bytes."""
+        return (self.block + (68 * self.cap if v else 0)) // 64
+
+    def scales(self, v):
+        """The same in units of 4 bytes."""
+        return (self.block + (132 * self.cap if v else 64 * self.cap)) // 4
+
+
+class Handle:
+    """A library object that lives as long as the state does."""
+
+    def __init__(self, value, close, after=None):
+        self.value, self.close, self.after = value, close, after
+
+    def __del__(self):
+        torch.cuda.synchronize()
+        self.close(self.value)
+
+
+def _cache(c, ctx, table, budget=None):
+    from paper_2601_13684_amd import binding as hc
+    heads = [hc.hc_kv4_head(off=table.off[i], row_off=table.row_off[i], cap=cap, budget=cap if budget is None else budget[i],
+                            sink=0 if budget is None else c["sink"], recent=0 if budget is None else c["recent"]) for i, cap in enumerate(table.caps)]
+    return Handle(hc.hc_kv4_create(ctx.value, heads), hc.hc_kv4_destroy, ctx)
+
+
+def _rope(s):
+    """The model's rotation and norms, as the library takes them."""
+    from paper_2601_13684_amd import binding as hc
+    c = s["c"]
+    scaling = hc.hc_rope_scaling(kind=hc.HC_ROPE_BANDS, **SCALING["bands"]) if c["scaling"] == "bands" else None
+    return hc.hc_rope_init(hc.HC_ROPE_HALF if c["pairs"] == "half" else hc.HC_ROPE_INTERLEAVED, c["rot"], c["theta"], scaling,
+                           q_norm=s["q_norm"], k_norm=s["k_norm"], eps=EPS)
+
+
+def _buffer(s, rooms):
+    """bf16 rows of K and V, rooms[i] of head i, and where they are."""
+    s["k_off"], s["v_off"], at = [], [], 0
+    for room in rooms:
+        s["k_off"].append(at)
+        s["v_off"].append(at + room * D)
+        at += 2 * room * D
+    return torch.zeros((at,), dtype=torch.bfloat16, device=DEV)
+
+
+def prepare(case, seed):
+    c = case
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    B, Hkv, G, BH = c["B"], c["Hkv"], c["G"], c["B"] * c["Hkv"]
+    rows = _per_head(c, c["rows"])
+    s = dict(c=c, held=rows)
+    more = _per_head(c, c["count"]) if c["kind"] == "store" else [GROW if c["kind"] == "append" else 0] * BH
+    t = s["table"] = Table([_up(n + m) for n, m in zip(rows, more)])
+    s["state"] = torch.tensor([[n, n] for n in rows], dtype=torch.int32, device=DEV)
+    if c["kind"] in ("store", "append"):
+        # (nothing of what is there is read: of zeros, so that what is written is what counts)
+        s["arena"] = torch.zeros((t.bytes,), dtype=torch.uint8, device=DEV)
+    if c["kind"] == "store":
+        s["start"] = s["state"].clone()
+        s["first"], s["count"] = [rows[b * Hkv] for b in range(B)], _ints(c["count"])
+        room = [_up(f + n) for f, n in zip(s["first"], s["count"]) for _ in range(Hkv)]
+        s["back"] = _buffer(s, room)
+        s["kv"] = torch.randn((s["back"].numel() // D, D), generator=g, device=DEV)
+        s["kv"] *= torch.exp(0.7 * torch.randn((D,), generator=g, device=DEV))          # channels differ in size
+        s["kv"] = s["kv"].to(torch.bfloat16).view(-1)
+        s["acc"] = torch.ones((t.rows + 1,), device=DEV)
+    elif c["kind"] == "append":
+        Hq = Hkv * G
+        x = torch.randn((B, Hq + 2 * Hkv, D), generator=g, device=DEV) * torch.exp(0.5 * torch.randn((Hq + 2 * Hkv, D), generator=g, device=DEV))
+        s["x"] = x.to(torch.bfloat16 if c["type"] == "bf16" else torch.float32)
+        s["q_norm"], s["k_norm"] = [1 + 0.2 * torch.randn((D,), generator=g, device=DEV) for _ in range(2)] if c["norm"] else (None, None)
+        s["q_out"] = torch.zeros((B, Hq, D), dtype=torch.bfloat16, device=DEV)
+        s["back"] = _buffer(s, [1] * BH)
+        s["step"], s["one"] = [rows[b * Hkv] for b in range(B)], [1] * B
+    elif c["kind"] == "attn":
+        # queries and keys as rotation leaves them: logits of standard deviation 1.5, one position in 50 that draws more than the rest
+        s["q"] = (1.5 * torch.randn((B, Hkv * G, D), generator=g, device=DEV) + 0.3).to(torch.bfloat16)
+        s["arena"] = torch.zeros((t.bytes,), dtype=torch.uint8, device=DEV)
+        for off, cap in zip(t.off, t.caps):
+            for v in (0, 1):
+                x = torch.randn((cap, D), generator=g, device=DEV)
+                if not v:
+                    x += 0.4 * (torch.rand((cap, 1), generator=g, device=DEV) < 0.02)
+                words, scales = _pack(x.to(torch.bfloat16))
+                at = off + 68 * cap * v
+                s["arena"][at:at + 64 * cap] = words.view(torch.uint8).view(-1)
+                s["arena"][at + 64 * cap:at + 68 * cap] = scales.view(-1)
+        if c["acc"]:
+            s["acc"] = torch.rand((t.rows + 1,), generator=g, device=DEV) ** 4
+    else:
+        # (any codes are rows; scales as those of values about 1)
+        s["arena"] = torch.randint(0, 256, (t.bytes,), generator=g, dtype=torch.uint8, device=DEV)
+        for off, cap in zip(t.off, t.caps):
+            for at in (off + 64 * cap, off + 132 * cap):
+                s["arena"][at:at + 4 * cap] = torch.randint(122, 130, (4 * cap,), generator=g, dtype=torch.uint8, device=DEV)
+        # weights of several steps: a few rows have most of it, some have had nothing
+        s["acc"] = torch.exp(2 * torch.randn((t.rows + 1,), generator=g, device=DEV)) * (torch.rand((t.rows + 1,), generator=g, device=DEV) > 0.1)
+        s["budget"] = [min(b, cap) for b, cap in zip(_per_head(c, c["budget"]), t.caps)]
+        s["budget"] = [max(b, min(cap, c["sink"] + c["recent"])) for b, cap in zip(s["budget"], t.caps)]
+        s["to"] = Table([_up(b) for b in s["budget"]])
+        s["to_arena"] = torch.zeros((s["to"].bytes,), dtype=torch.uint8, device=DEV)
+        s["to_state"] = torch.zeros((BH, 2), dtype=torch.int32, device=DEV)
+        s["to_acc"] = torch.zeros((s["to"].rows + 1,), device=DEV)
+        s["kept"] = torch.zeros((s["to"].rows + 1,), dtype=torch.int32, device=DEV)
+        s["back"] = _buffer(s, s["to"].caps)
+        s["first"], s["count"] = [0] * B, [max(s["to"].caps)] * B
+    if own:
+        from paper_2601_13684_amd import binding as hc
+        cfg = hc.hc_config(B=B, Hq=Hkv * G, Hkv=Hkv, D=D, max_ctx=max(t.caps + (s["to"].caps if c["kind"] == "evict" else [])), max_k=8, window=1, metric=0,
+                           tau_num=4, tau_den=5, agg=0, window_mode=0)
+        s["ctx"] = Handle(hc.hc_create(cfg), hc.hc_destroy)
+        s["kv4"] = _cache(c, s["ctx"], t)
+        if c["kind"] == "append":
+            s["rope"] = _rope(s)
+        if c["kind"] == "evict":
+            s["to_kv4"] = _cache(c, s["ctx"], s["to"], s["budget"])
+        if c["kind"] in ("attn", "evict"):
+            s["work"] = torch.zeros((hc.hc_kv4_work_bytes(s["ctx"].value, s["kv4"].value),), dtype=torch.uint8, device=DEV)
+        if c["kind"] == "attn":
+            s["out"] = torch.zeros((B, Hkv * G, D), dtype=torch.float32, device=DEV)
+            s["lse"] = torch.zeros((B, Hkv * G), dtype=torch.float32, device=DEV)
+    return s
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------------------------
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"store": _plain_store, "append": _plain_append, "attn": _plain_attn, "evict": _plain_evict}[state["c"]["kind"]](state)
+
+
+def _run_own(s):
+    from paper_2601_13684_amd import binding as hc
+    c = s["c"]
+    ctx, kv4 = s["ctx"].value, s["kv4"].value
+    if c["kind"] == "attn":
+        hc.hc_kv4_attn(ctx, kv4, s["arena"], s["state"], s["q"], s["out"], s["lse"], s["acc"] if c["acc"] else None, c["decay"], s["work"], s["work"].numel())
+        return (s["out"], s["lse"], s["acc"]) if c["acc"] else (s["out"], s["lse"])
+    if c["kind"] == "evict":
+        hc.hc_kv4_evict(ctx, kv4, s["arena"], s["state"], s["acc"], s["to_kv4"].value, s["to_arena"], s["to_state"], s["to_acc"], s["kept"], s["work"],
+                        s["work"].numel())
+        hc.hc_kv4_load(ctx, s["to_kv4"].value, s["to_arena"], s["to_state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
+        return s["to_state"], s["to_acc"], s["kept"], s["back"]
+    if c["kind"] == "store":
+        s["state"].copy_(s["start"])
+        hc.hc_kv4_store(ctx, kv4, s["kv"], s["k_off"], s["v_off"], s["first"], s["count"], s["arena"], s["state"], s["acc"])
+        hc.hc_kv4_load(ctx, kv4, s["arena"], s["state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
+        return s["state"], s["acc"], s["back"]
+    Hkv, Hq, x = c["Hkv"], c["Hkv"] * c["G"], s["x"]
+    hc.hc_kv4_append(ctx, kv4, s["rope"], x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], s["q_out"], s["arena"], s["state"], None)
+    hc.hc_kv4_load(ctx, kv4, s["arena"], s["state"], s["step"], s["one"], s["back"], s["k_off"], s["v_off"])
+    s["step"] = [n + 1 for n in s["step"]]
+    return s["q_out"], s["state"], s["back"]
+
+
+LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0)
+
+
+def _power(e):
+    """2^e of an int32 tensor, -126 .. 127."""
+    return ((e + 127) << 23).view(torch.float32)
+
+
+def _codes(x):
+    """Codes 0..15 [..., 4, 32] and exponents [..., 4, 1] of rows x [..., 128]."""
+    y = x.float().unflatten(-1, (4, 32))
+    top, e = torch.frexp(y.abs().amax(-1, keepdim=True))
+    e = torch.clamp(e - 3 + (top > 0.875), min=-125).to(torch.int32)
+    m = y.abs() * _power(-e)
+    code = (m > 0.25).int() + (m >= 0.75) + (m > 1.25) + (m >= 1.75) + (m > 2.5) + (m >= 3.5) + (m > 5)
+    return code + 8 * (y < 0), e
+
+
+def _pack(x):
+    """Words [..., 16] and scale bytes [..., 4] of rows x."""
+    code, e = _codes(x)
+    words = (code.flatten(-2).unflatten(-1, (16, 8)).long() << (4 * torch.arange(8, device=DEV))).sum(-1)
+    return torch.where(words >= 2 ** 31, words - 2 ** 32, words).to(torch.int32), (e[..., 0] + 127).to(torch.uint8)
+
+
+def _worth(code, e):
+    """What codes [..., 4, 32] and exponents [..., 4, 1] stand for, [..., 128]."""
+    return (torch.tensor(LEVELS, device=DEV)[code] * _power(e)).flatten(-2)
+
+
+def _rows(s, v, index):
+    """Rows [heads, n] of K (v: of V) as the cache holds them, 32 bits."""
+    t = s["table"]
+    words = s["arena"].view(torch.int32).view(-1, 16)[t.codes(v)[:, None] + index]
+    scales = s["arena"].view(-1, 4)[t.scales(v)[:, None] + index]
+    code = (words[..., None] >> (4 * torch.arange(8, dtype=torch.int32, device=DEV))) & 15
+    return _worth(code.flatten(-2).unflatten(-1, (4, 32)), scales.to(torch.int32)[..., None] - 127)
+
+
+def _write(s, v, head, row, x):
+    """Rows x of the heads `head` to their places; what they are then worth."""
+    t = s["table"]
+    code, e = _codes(x)
+    words, scales = _pack(x)
+    s["arena"].view(torch.int32).view(-1, 16)[t.codes(v)[head] + row] = words
+    s["arena"].view(-1, 4)[t.scales(v)[head] + row] = scales
+    return _worth(code, e).to(torch.bfloat16)
+
+
+def _plain_store(s):
+    c, t = s["c"], s["table"]
+    count = torch.tensor(_per_head(c, c["count"]), device=DEV)
+    s["state"].copy_(s["start"])
+    head = torch.repeat_interleave(torch.arange(len(t.caps), device=DEV), count, output_size=sum(s["count"]) * c["Hkv"])
+    i = torch.arange(head.numel(), device=DEV) - (count.cumsum(0) - count)[head]
+    row = s["state"][:, 0][head] + i
+    for v, off in ((0, s["k_off"]), (1, s["v_off"])):
+        at = torch.tensor(off, device=DEV)[head] // D
+        s["back"].view(-1, D)[at + i] = _write(s, v, head, row, s["kv"].view(-1, D)[at + s["start"][:, 1][head] + i])
+    s["acc"][t.first[head] + row] = 0
+    s["state"] += count[:, None]
+    return s["state"], s["acc"], s["back"]
+
+
+def _frequencies(c):
+    """Radians a position, 64 bits."""
+    f = c["theta"] ** -(torch.arange(0, c["rot"], 2, dtype=torch.float64, device=DEV) / c["rot"])
+    if c["scaling"] == "bands":
+        p = SCALING["bands"]
+        keep = ((p["original"] * f / (2 * math.pi) - p["low"]) / (p["high"] - p["low"])).clamp(0, 1)
+        return f * keep + f / p["factor"] * (1 - keep)
+    return f
+
+
+def _turn(c, x, weight, pos):
+    """Norm and rotation of x [B, heads, 128]; in 64 bits, for what lies next to a border between two codes."""
+    x = x.double()
+    if weight is not None:
+        x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS) * weight.double()
+    angle = pos[:, None, None].double() * _frequencies(c)
+    cos, sin, r = torch.cos(angle), torch.sin(angle), c["rot"]
+    if c["pairs"] == "half":
+        a, b = x[..., :r // 2], x[..., r // 2:r]
+        return torch.cat([a * cos - b * sin, b * cos + a * sin, x[..., r:]], -1).to(torch.bfloat16)
+    a, b = x[..., 0:r:2], x[..., 1:r:2]
+    return torch.cat([torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2), x[..., r:]], -1).to(torch.bfloat16)
+
+
+def _plain_append(s):
+    c = s["c"]
+    Hkv, Hq, x = c["Hkv"], c["Hkv"] * c["G"], s["x"]
+    row, pos = s["state"][:, 0], s["state"][::Hkv, 1]
+    head = torch.arange(row.numel(), device=DEV)
+    k, v = _turn(c, x[:, Hq:Hq + Hkv], s["k_norm"], pos), x[:, Hq + Hkv:].to(torch.bfloat16)
+    s["back"].view(-1, 2, D)[:, 0] = _write(s, 0, head, row, k.flatten(0, 1))
+    s["back"].view(-1, 2, D)[:, 1] = _write(s, 1, head, row, v.flatten(0, 1))
+    s["q_out"].copy_(_turn(c, x[:, :Hq], s["q_norm"], pos))
+    s["state"] += 1
+    return s["q_out"], s["state"], s["back"]
+
+
+def _plain_attn(s):
+    c, t = s["c"], s["table"]
+    BH, G = len(t.caps), c["G"]
+    n = s["state"][:, 0].long()
+    i = torch.arange(max(1, max(s["held"])), device=DEV)
+    there = i < n[:, None]
+    index = torch.minimum(i, t.cap[:, None] - 1)
+    x = torch.bmm(_rows(s, 0, index), (s["q"].float().view(BH, G, D) / math.sqrt(D)).transpose(1, 2).contiguous())       # [heads, rows, G]
+    x = x.masked_fill(~there[..., None], -math.inf)
+    top = x.amax(1, keepdim=True).clamp(min=-3e38)         # (of a head with no rows: weights of 0)
+    p = torch.exp(x - top)
+    total = p.sum(1, keepdim=True)
+    p = p / total.clamp(min=1e-38)
+    out = torch.bmm(p.transpose(1, 2).contiguous(), _rows(s, 1, index)).view(c["B"], -1, D)
+    lse = torch.where(total > 0, top + torch.log(total), -math.inf)[:, 0].reshape(c["B"], -1)
+    if not c["acc"]:
+        return out, lse
+    at = torch.where(there, t.first[:, None] + i, t.rows)         # (what is behind a head's rows goes to one place behind the last)
+    new = s["acc"][at] * c["decay"] + p.mean(-1)
+    s["acc"][at] = torch.where(there, new, s["acc"][-1])
+    return out, lse, s["acc"]
+
+
+def _plain_evict(s):
+    c, t, to = s["c"], s["table"], s["to"]
+    n = s["state"][:, 0].long()
+    m = torch.minimum(n, torch.tensor(s["budget"], device=DEV))
+    i, j = torch.arange(max(s["held"]), device=DEV), torch.arange(min(max(s["held"]), max(s["budget"])), device=DEV)
+    score = s["acc"][torch.minimum(t.first[:, None] + i, torch.tensor(t.rows, device=DEV))]
+    always = (i < c["sink"]) | (i >= n[:, None] - c["recent"])
+    score = score.masked_fill(always, math.inf).masked_fill(i >= n[:, None], -math.inf)
+    order = torch.sort(score, dim=-1, descending=True, stable=True).indices[:, :j.numel()]
+    stays = j < m[:, None]
+    kept = torch.sort(torch.where(stays, order, i.numel()), dim=-1).values
+    at, kept = torch.where(stays, to.first[:, None] + j, to.rows), torch.where(stays, kept, 0)
+    s["kept"][at] = torch.where(stays, kept, s["kept"][-1]).to(torch.int32)
+    s["to_acc"][at] = torch.where(stays, s["acc"][t.first[:, None] + kept], s["to_acc"][-1])
+    s["to_state"][:, 0], s["to_state"][:, 1] = m, s["state"][:, 1]
+    for v, off in ((0, s["k_off"]), (1, s["v_off"])):
+        rows = _rows(s, v, kept).to(torch.bfloat16)
+        at = torch.tensor(off, device=DEV)[:, None] // D + torch.minimum(j, m[:, None] - 1)
+        rows = rows.gather(1, torch.minimum(j, m[:, None] - 1)[..., None].expand(-1, -1, D))         # (the last row again, behind it)
+        s["back"].view(-1, D)[at] = rows
+    return s["to_state"], s["to_acc"], s["kept"], s["back"]
+
+
+# ---- the same in 64 bits --------------------------------------------------------------------------------------------------------------
+
+def _nearest(x):
+    """What rows x [n, 128] (64 bits, values of bf16) are worth in the cache."""
+    y = x.view(-1, 4, 32)
+    borders = 7 * 2.0 ** torch.arange(-125, 128, dtype=torch.float64, device=DEV)
+    unit = borders[torch.bucketize(y.abs().amax(-1, keepdim=True), borders)] / 7
+    m = y.abs() / unit
+    step = torch.where(m < 2, 0.5, torch.where(m < 4, 1.0, 2.0)).double()
+    return (torch.sign(y) * (torch.round(m / step) * step).clamp(max=6) * unit).view(-1, D)
+
+
+def _held(s, i, v, n):
+    """The first n rows of head i, 64 bits, from the cache's bytes."""
+    off, cap = s["table"].off[i] + 68 * s["table"].caps[i] * v, s["table"].caps[i]
+    b = s["arena"][off:off + 64 * n].view(n, 64).int()
+    code = torch.stack([b & 15, b >> 4], -1).view(n, D)
+    e, odd = (code & 7) >> 1, (code & 1).double()
+    size = torch.where(e > 0, (2 + odd) * 2.0 ** (e - 2).double(), odd / 2)
+    unit = 2.0 ** (s["arena"][off + 64 * cap:off + 64 * cap + 4 * n].view(n, 4).double() - 127)
+    return torch.where(code > 7, -size, size) * unit.repeat_interleave(32, dim=1)
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(c, seed)
+    B, Hkv, G, t = c["B"], c["Hkv"], c["G"], s["table"]
+    if c["kind"] == "attn":
+        out = torch.zeros((B * Hkv, G, D), dtype=torch.float64, device=DEV)
+        lse = torch.full((B * Hkv, G), -math.inf, dtype=torch.float64, device=DEV)
+        acc = s["acc"].double() if c["acc"] else None
+        for i, n in enumerate(s["held"]):
+            if n:
+                x = s["q"].view(B * Hkv, G, D)[i].double() @ _held(s, i, 0, n).t().contiguous() * D ** -0.5
+                lse[i] = torch.logsumexp(x, -1)
+                p = torch.exp(x - lse[i][:, None])
+                out[i] = p @ _held(s, i, 1, n)
+                if c["acc"]:
+                    acc[t.row_off[i]:t.row_off[i] + n] = acc[t.row_off[i]:t.row_off[i] + n] * c["decay"] + p.sum(0) / G
+        out, lse = out.view(B, -1, D), lse.view(B, -1)
+        return (out, lse, acc) if c["acc"] else (out, lse)
+    if c["kind"] == "store":
+        back, acc = s["back"].double().view(-1, D), s["acc"].double()
+        for i in range(B * Hkv):
+            f, n = s["first"][i // Hkv], s["count"][i // Hkv]
+            acc[t.row_off[i] + f:t.row_off[i] + f + n] = 0
+            for off in (s["k_off"], s["v_off"]):
+                at = off[i] // D
+                back[at:at + n] = _nearest(s["kv"].view(-1, D)[at + f:at + f + n].double()) if n else back[at:at + n]
+        return s["state"] + torch.tensor(_per_head(c, c["count"]), dtype=torch.int32, device=DEV)[:, None], acc, back.view(-1)
+    if c["kind"] == "evict":
+        kept, acc, back, state = s["kept"], s["to_acc"].double(), s["back"].double().view(-1, D), s["to_state"]
+        for i, n in enumerate(s["held"]):
+            row, score = list(range(n)), s["acc"][t.row_off[i]:t.row_off[i] + n].tolist()
+            m = min(n, s["budget"][i])
+            if m < n:
+                last = n - c["recent"]
+                between = sorted(range(c["sink"], last), key=lambda r: (-score[r], r))[:m - c["sink"] - c["recent"]]
+                row = list(range(c["sink"])) + sorted(between) + list(range(last, n))
+            state[i, 0], state[i, 1] = m, n
+            to, row = s["to"].row_off[i], torch.tensor(row, dtype=torch.int64, device=DEV)
+            kept[to:to + m] = row.to(torch.int32)
+            acc[to:to + m] = s["acc"][t.row_off[i] + row].double()
+            for v, off in ((0, s["k_off"]), (1, s["v_off"])):
+                back[off[i] // D:off[i] // D + m] = _held(s, i, v, n)[row]
+        return state, acc, kept, back.view(-1)
+    Hq, x = Hkv * G, s["x"].double()
+    # a pair is a complex number, turned by exp(i angle)
+    half = torch.arange(c["rot"] // 2, dtype=torch.float64, device=DEV)
+    f = torch.exp(-2 * half / c["rot"] * math.log(c["theta"]))
+    if c["scaling"] == "bands":
+        p = SCALING["bands"]
+        turns = p["original"] * f / (2 * math.pi)
+        part = (turns - p["low"]) / (p["high"] - p["low"])
+        f = torch.where(turns < p["low"], f / p["factor"], torch.where(turns > p["high"], f, (1 - part) * f / p["factor"] + part * f))
+    angle = torch.tensor(s["step"], dtype=torch.float64, device=DEV)[:, None, None] * f
+    e = torch.polar(torch.ones_like(angle), angle)
+    i = torch.arange(c["rot"] // 2, device=DEV)
+    one, two = (i, i + c["rot"] // 2) if c["pairs"] == "half" else (2 * i, 2 * i + 1)
+    done = []
+    for y, w in ((x[:, :Hq], s["q_norm"]), (x[:, Hq:Hq + Hkv], s["k_norm"])):
+        y = y.clone()
+        if w is not None:
+            y = y / torch.sqrt((y * y).sum(-1, keepdim=True) / D + EPS) * w.double()
+        z = torch.complex(y[..., one], y[..., two]) * e
+        y[..., one], y[..., two] = z.real, z.imag
+        done.append(y)
+    # (a row goes into the cache by way of bf16, so that it is the same whoever turned it)
+    k, v = (_nearest(y.to(torch.bfloat16).double().reshape(-1, D)) for y in (done[1], x[:, Hq + Hkv:]))
+    return done[0], s["state"] + 1, torch.stack([k, v], 1).view(-1)
+
+
+def work(case):
+    c = case
+    Hkv, G, rows = c["Hkv"], c["G"], _per_head(c, c["rows"])
+    pair, held = 2 * D * 2, 136         # bytes of a K row and a V row, in bf16 and in the cache
+    if c["kind"] == "store":
+        n = sum(_ints(c["count"])) * Hkv
+        return dict(bytes=n * (pair + held + 4 + held + pair), flops=n * 2 * D * 6)
+    if c["kind"] == "append":
+        n, size = c["B"] * Hkv, 2 if c["type"] == "bf16" else 4
+        return dict(bytes=n * ((G + 2) * D * size + G * D * 2 + held + held + pair), flops=n * ((G + 1) * (3 * c["rot"] + (4 * D if c["norm"] else 0)) + 2 * D * 6))
+    if c["kind"] == "attn":
+        return dict(bytes=sum(rows) * (held + (8 if c["acc"] else 0)) + len(rows) * G * (D * 2 + D * 4 + 4), flops=sum(rows) * G * 4 * D)
+    kept = sum(min(n, b) for n, b in zip(rows, _per_head(c, c["budget"])))
+    return dict(bytes=sum(rows) * 4 + kept * (2 * (held + 4) + 4 + held + pair), flops=sum(rows) * 8)
