@@ -1,10 +1,10 @@
 """The operators of a KV cache held in 4 bits, as measurable cases: rows into it and back, decode attention over it, eviction by accumulated weight.
 
 Kinds of case:
-  store   hc_kv4_store, then hc_kv4_load: a prompt's (or a chunk's) K and V rows into the cache, and the rows as the cache holds them
-  append  hc_kv4_append, then hc_kv4_load: norm and rotation of the decode token, its rows into the cache, and the rows as the cache holds them
-  attn    hc_kv4_attn: attention of the decode token over the cache; with ``acc`` every row's share of the weights is added to what it had
-  evict   hc_kv4_evict, then hc_kv4_load: the rows that keep their place by accumulated weight go to a smaller cache, and what it then holds
+  store   hc_kvq_store, then hc_kvq_load: a prompt's (or a chunk's) K and V rows into the cache, and the rows as the cache holds them
+  append  hc_kvq_append, then hc_kvq_load: norm and rotation of the decode token, its rows into the cache, and the rows as the cache holds them
+  attn    hc_kvq_attn: attention of the decode token over the cache; with ``acc`` every row's share of the weights is added to what it had
+  evict   hc_kvq_evict, then hc_kvq_load: the rows that keep their place by accumulated weight go to a smaller cache, and what it then holds
 
 A row of 128 values is 64 bytes of codes (element i in bits 4 (i % 8) .. of word i / 8: sign, then one of 0 .5 1 1.5 2 3 4 6) and four scale bytes s,
 one per 32 values, for the factor 2^(s - 127): the smallest power of two, at least 2^-125, of which no value is more than 7 times.  A head's block of
@@ -148,9 +148,9 @@ class Handle:
 
 def _cache(c, ctx, table, budget=None):
     from paper_2601_13684_amd import binding as hc
-    heads = [hc.hc_kv4_head(off=table.off[i], row_off=table.row_off[i], cap=cap, budget=cap if budget is None else budget[i],
+    heads = [hc.hc_kvq_head(off=table.off[i], row_off=table.row_off[i], cap=cap, budget=cap if budget is None else budget[i],
                             sink=0 if budget is None else c["sink"], recent=0 if budget is None else c["recent"]) for i, cap in enumerate(table.caps)]
-    return Handle(hc.hc_kv4_create(ctx.value, heads), hc.hc_kv4_destroy, ctx)
+    return Handle(hc.hc_kvq_create(ctx.value, heads), hc.hc_kvq_destroy, ctx)
 
 
 def _rope(s):
@@ -239,13 +239,13 @@ def prepare(case, seed):
         cfg = hc.hc_config(B=B, Hq=Hkv * G, Hkv=Hkv, D=D, max_ctx=max(t.caps + (s["to"].caps if c["kind"] == "evict" else [])), max_k=8, window=1, metric=0,
                            tau_num=4, tau_den=5, agg=0, window_mode=0)
         s["ctx"] = Handle(hc.hc_create(cfg), hc.hc_destroy)
-        s["kv4"] = _cache(c, s["ctx"], t)
+        s["kvq"] = _cache(c, s["ctx"], t)
         if c["kind"] == "append":
             s["rope"] = _rope(s)
         if c["kind"] == "evict":
-            s["to_kv4"] = _cache(c, s["ctx"], s["to"], s["budget"])
+            s["to_kvq"] = _cache(c, s["ctx"], s["to"], s["budget"])
         if c["kind"] in ("attn", "evict"):
-            s["work"] = torch.zeros((hc.hc_kv4_work_bytes(s["ctx"].value, s["kv4"].value),), dtype=torch.uint8, device=DEV)
+            s["work"] = torch.zeros((hc.hc_kvq_work_bytes(s["ctx"].value, s["kvq"].value),), dtype=torch.uint8, device=DEV)
         if c["kind"] == "attn":
             s["out"] = torch.zeros((B, Hkv * G, D), dtype=torch.float32, device=DEV)
             s["lse"] = torch.zeros((B, Hkv * G), dtype=torch.float32, device=DEV)
@@ -263,23 +263,23 @@ def run(state):
 def _run_own(s):
     from paper_2601_13684_amd import binding as hc
     c = s["c"]
-    ctx, kv4 = s["ctx"].value, s["kv4"].value
+    ctx, kvq = s["ctx"].value, s["kvq"].value
     if c["kind"] == "attn":
-        hc.hc_kv4_attn(ctx, kv4, s["arena"], s["state"], s["q"], s["out"], s["lse"], s["acc"] if c["acc"] else None, c["decay"], s["work"], s["work"].numel())
+        hc.hc_kvq_attn(ctx, kvq, s["arena"], s["state"], s["q"], s["out"], s["lse"], s["acc"] if c["acc"] else None, c["decay"], s["work"], s["work"].numel())
         return (s["out"], s["lse"], s["acc"]) if c["acc"] else (s["out"], s["lse"])
     if c["kind"] == "evict":
-        hc.hc_kv4_evict(ctx, kv4, s["arena"], s["state"], s["acc"], s["to_kv4"].value, s["to_arena"], s["to_state"], s["to_acc"], s["kept"], s["work"],
+        hc.hc_kvq_evict(ctx, kvq, s["arena"], s["state"], s["acc"], s["to_kvq"].value, s["to_arena"], s["to_state"], s["to_acc"], s["kept"], s["work"],
                         s["work"].numel())
-        hc.hc_kv4_load(ctx, s["to_kv4"].value, s["to_arena"], s["to_state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
+        hc.hc_kvq_load(ctx, s["to_kvq"].value, s["to_arena"], s["to_state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
         return s["to_state"], s["to_acc"], s["kept"], s["back"]
     if c["kind"] == "store":
         s["state"].copy_(s["start"])
-        hc.hc_kv4_store(ctx, kv4, s["kv"], s["k_off"], s["v_off"], s["first"], s["count"], s["arena"], s["state"], s["acc"])
-        hc.hc_kv4_load(ctx, kv4, s["arena"], s["state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
+        hc.hc_kvq_store(ctx, kvq, s["kv"], s["k_off"], s["v_off"], s["first"], s["count"], s["arena"], s["state"], s["acc"])
+        hc.hc_kvq_load(ctx, kvq, s["arena"], s["state"], s["first"], s["count"], s["back"], s["k_off"], s["v_off"])
         return s["state"], s["acc"], s["back"]
     Hkv, Hq, x = c["Hkv"], c["Hkv"] * c["G"], s["x"]
-    hc.hc_kv4_append(ctx, kv4, s["rope"], x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], s["q_out"], s["arena"], s["state"], None)
-    hc.hc_kv4_load(ctx, kv4, s["arena"], s["state"], s["step"], s["one"], s["back"], s["k_off"], s["v_off"])
+    hc.hc_kvq_append(ctx, kvq, s["rope"], x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], s["q_out"], s["arena"], s["state"], None)
+    hc.hc_kvq_load(ctx, kvq, s["arena"], s["state"], s["step"], s["one"], s["back"], s["k_off"], s["v_off"])
     s["step"] = [n + 1 for n in s["step"]]
     return s["q_out"], s["state"], s["back"]
 
