@@ -479,6 +479,65 @@ hc_status hc_prefill_attn(hc_ctx* ctx, const void* q, const void* kv_prefill, co
 hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
                          int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* kv_arena, void* host_tier, void* stream);
 
+/* ---- The cache held in 4 bits --------------------------------------------------------------------------------------------------
+ * A second kind of cache, beside the bf16 arena that the calls above read: 136 bytes for a K row and a V row in place of 512, every head of it with a
+ * capacity and a length of its own, and every row with the attention that it has drawn so far, by which heads are brought to a budget.
+ *     hc_kvq_store  (a prompt's rows, from the kv_prefill of hc_prefill_rope)  ->  then for every token
+ *     hc_kvq_append  ->  hc_kvq_attn,   and from time to time   hc_kvq_evict  into another cache.   hc_kvq_load gives rows back as bf16.
+ *
+ * A row of 128 values is 64 bytes of codes and 4 scale bytes s, one per 32 values.  Element i is bits 4 (i % 8) .. 4 (i % 8) + 3 of dword i / 8: the sign
+ * (bit 3) and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (0 .. 7), times 2^(s - 127).  s is the smallest, 2 at least, with no value beyond 7 of these units; codes are
+ * rounded to the nearest, ties to the even one, and what is beyond 5 to 6: a value is at most a unit off where it is beyond 4 units, half a unit between 2
+ * and 4, a quarter below.  s = 255, codes 0: a value of the 32 was not finite, and all 32 read as NaN.  (From 1.75 * 2^127 on, values may read as infinities.)
+ * A head's block in the cache is  K codes [cap][64], K scales [cap][4], V codes [cap][64], V scales [cap][4]  bytes.
+ *
+ * state: dev int32 [B*Hkv][2]: the rows that a head holds (a kernel that reads more than cap or less than 0 takes cap and 0), and the position of its
+ * sequence's next token.  Lengths live there alone: the calls take them from the device, so that every one of them may be captured and replayed while they
+ * grow.  acc: dev f32, a number a row (see row_off), or NULL where nothing is accumulated.  A cache, its state and its acc belong to the caller;
+ * the hc_kvq is the table of where its heads are, may serve any number of them (every layer's), and must outlive graphs that were captured with
+ * it.  All calls but create and destroy only enqueue, and neither allocate nor wait; calls that touch the same cache, state or acc are put in order by the
+ * caller, and so are two that are given the same work buffer. */
+typedef struct hc_kvq hc_kvq;
+typedef struct {
+    int64_t off;       /* byte offset of the head's block of 136 cap bytes in the cache; multiple of 64      */
+    int64_t row_off;   /* element of its row 0 in acc and kept                                               */
+    int32_t cap;       /* rows that it has room for: multiple of 16, 16 .. max_ctx                           */
+    int32_t budget;    /* rows that hc_kvq_evict leaves when it fills this head, 1 .. cap ...                */
+    int32_t sink;      /* ... of which the first `sink` ...                                                  */
+    int32_t recent;    /* ... and the last `recent` of the source always are                                 */
+} hc_kvq_head;
+/* Table of B*Hkv entries, row (b*Hkv + h), HOST memory.  Blocks must not overlap, nor rows in acc.  Allocates and synchronises. */
+hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads_host, hc_kvq** out);
+hc_status hc_kvq_destroy(hc_kvq* kvq);                 /* before its context                                 */
+/* Bytes of the work buffer of hc_kvq_attn and hc_kvq_evict (dev, 256-byte aligned, scratch): enough for either. */
+size_t hc_kvq_work_bytes(const hc_ctx* ctx, const hc_kvq* kvq);
+
+/* Rows of positions first[b] .. first[b] + count[b] - 1 of kv_prefill (arguments as hc_prefill_attn's) become the next rows of every head of sequence b;
+ * its next position becomes first[b] + count[b] (where count[b] > 0).  Their acc (if not NULL) becomes 0.  Rows that a head has no room for are dropped. */
+hc_status hc_kvq_store(hc_ctx* ctx, const hc_kvq* kvq, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                       const int32_t* count, void* arena, int32_t* state, float* acc, void* stream);
+/* Rows first[b] .. first[b] + count[b] - 1 of every head of sequence b, those of them that it holds, as bf16: row first[b] + i to row i of the K block
+ * at element k_off[b*Hkv+h] and the V block at v_off[..] of kv_out.  Nothing else in kv_out is written. */
+hc_status hc_kvq_load(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const int32_t* first, const int32_t* count,
+                      void* kv_out, const int64_t* k_off, const int64_t* v_off, void* stream);
+/* The decode token of sequence b, at its next position: norm and rotation of its query and key heads (arguments as hc_append_rope's; computed in 64 bits,
+ * rounded once to bf16), the queries to q_out (dev bf16 [B][Hq][128]), the K and V rows behind every head's last, with an acc (if not NULL) of 0; rows and
+ * position grow by one.  A head that is full keeps the rows that it has, and its position moves on. */
+hc_status hc_kvq_append(hc_ctx* ctx, const hc_kvq* kvq, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
+                        int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* arena, int32_t* state, float* acc, void* stream);
+/* hc_decode_attn over this cache: out (dev f32 [B][Hq][128]) and lse (dev f32 [B][Hq]) of q (dev bf16 [B][Hq][128]) over the rows that every head holds;
+ * of a head with none, 0 and minus infinity.  acc (if not NULL) of row j becomes  decay acc + (1/G) sum over the head's queries of its weight,
+ * decay in 0 .. 1 (not read where acc is NULL).  Rows' values are taken exactly, everything else is 32-bit.  Sums over the rows are divided at the end: finite values
+ * of V beyond 2^90 may come out as infinities. */
+hc_status hc_kvq_attn(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const void* q, float* out, float* lse, float* acc,
+                      float decay, void* work, size_t work_bytes, void* stream);
+/* Heads of `kvq` to those of another table of the same context: of a head's n rows, m = min(n, budget) go, in order, to rows 0 .. m - 1: where n is more than the
+ * budget, the first `sink`, the last `recent`, and of those between them the ones with the largest acc (NaN comes last; of equals the first).  budget,
+ * sink and recent are `to`'s, sink + recent at most the budget (or the budget at least the source's cap).  to_acc: their acc; kept (dev int32, indexed as to_acc; or NULL):
+ * which rows they were; to_state: m and the source's next position.  Nothing else of the target is written, nothing of the source.  The two caches, states and acc must not overlap. */
+hc_status hc_kvq_evict(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const float* acc, const hc_kvq* to, void* to_arena,
+                       int32_t* to_state, float* to_acc, int32_t* kept, void* work, size_t work_bytes, void* stream);
+
 /* ---- Algorithm 1, the loop over the window's buffered queries at t mod W = 0 (HC_WINDOW_RESCORED) ------
  * Call once per decode step and layer, after hc_decode_attn and BEFORE hc_rep_topk_drift, on the stream
  * of the monitor (hc_decode_step does).  The layer counts the steps of the window: slot = monitored

@@ -28,6 +28,7 @@ EXPORTS = ["hc_create", "hc_destroy", "hc_strerror", "hc_last_error", "hc_layer_
            "hc_layer_window_slot",
            "hc_layer_set_window_slot", "hc_layer_context",
            "hc_rope_init", "hc_prefill_rope", "hc_prefill_attn_work_bytes", "hc_prefill_attn", "hc_append_rope",
+           "hc_kvq_create", "hc_kvq_destroy", "hc_kvq_work_bytes", "hc_kvq_store", "hc_kvq_load", "hc_kvq_append", "hc_kvq_attn", "hc_kvq_evict",
            "hc_decode_step", "hc_taxonomy", "hc_budgets", "hc_probe_stream_read", "hc_probe_host_copy"]
 
 
@@ -67,6 +68,10 @@ class hc_rope(C.Structure):
 
 class hc_rope_scaling(C.Structure):
     _fields_ = [("kind", C.c_int32), ("original", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class hc_kvq_head(C.Structure):
+    _fields_ = [("off", C.c_int64), ("row_off", C.c_int64), ("cap", C.c_int32), ("budget", C.c_int32), ("sink", C.c_int32), ("recent", C.c_int32)]
 
 
 class HcError(RuntimeError):
@@ -141,13 +146,22 @@ def lib():
         L.hc_prefill_attn_work_bytes.restype = C.c_size_t
         L.hc_prefill_attn.argtypes = [vp] * 10 + [C.c_size_t, vp]
         L.hc_append_rope.argtypes = [vp] * 6 + [i64] * 3 + [i32] + [vp] * 4
+        L.hc_kvq_create.argtypes = [vp, vp, C.POINTER(vp)]
+        L.hc_kvq_destroy.argtypes = [vp]
+        L.hc_kvq_work_bytes.argtypes = [vp, vp]
+        L.hc_kvq_work_bytes.restype = C.c_size_t
+        L.hc_kvq_store.argtypes = [vp] * 11
+        L.hc_kvq_load.argtypes = [vp] * 10
+        L.hc_kvq_append.argtypes = [vp] * 6 + [i64] * 3 + [i32] + [vp] * 5
+        L.hc_kvq_attn.argtypes = [vp] * 8 + [C.c_float, vp, C.c_size_t, vp]
+        L.hc_kvq_evict.argtypes = [vp] * 11 + [C.c_size_t, vp]
         L.hc_layer_context.argtypes = [vp, i32]
         L.hc_layer_context.restype = i32
         L.hc_decode_step.argtypes = [vp, C.POINTER(hc_layer_io), i32, i32, vp, vp]
         for n in EXPORTS:
             if n not in ("hc_strerror", "hc_last_error", "hc_layer_num_reps", "hc_layer_rep_slot",
                          "hc_layer_num_workgroups", "hc_layer_num_partials", "hc_rescore_work_bytes", "hc_prefill_work_bytes",
-                         "hc_prefill_attn_work_bytes", "hc_layer_window_slot"):
+                         "hc_prefill_attn_work_bytes", "hc_kvq_work_bytes", "hc_layer_window_slot"):
                 getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -509,6 +523,97 @@ def hc_append_rope(ctx: int, layer: int, rope: hc_rope, q: torch.Tensor, k: torc
     rows = _qkv(q, k, v, made)
     q_out = _sized(q_out, tokens[0] * tokens[1] * 256, "hc_append_rope: q_out")
     _check(lib().hc_append_rope(ctx, layer, C.byref(rope), *rows, q_out, _p(kv_arena), _p(host_tier), _stream(stream)), "hc_append_rope", ctx)
+
+
+# (B, Hq, Hkv, bytes of the cache, rows in its tables) of the 4-bit caches' tables made here
+_tables = {}
+
+
+def hc_kvq_create(ctx: int, heads: Sequence[hc_kvq_head]) -> int:
+    """heads: one entry for every (sequence, KV head)."""
+    made = _made.get(ctx)
+    if made is not None and len(heads) != made[0] * made[2]:
+        raise ValueError(f"hc_kvq_create: {len(heads)} heads; the context (B, Hq, Hkv) has {made}")
+    arr = (hc_kvq_head * len(heads))(*heads)
+    h = C.c_void_p()
+    _check(lib().hc_kvq_create(ctx, arr, C.byref(h)), "hc_kvq_create", ctx)
+    if made is not None:
+        _tables[h.value] = *made, max(x.off + 136 * x.cap for x in heads), max(x.row_off + x.cap for x in heads)
+    return h.value
+
+
+def hc_kvq_destroy(kvq: int) -> None:
+    _tables.pop(kvq, None)
+    _check(lib().hc_kvq_destroy(kvq), "hc_kvq_destroy")
+
+
+def hc_kvq_work_bytes(ctx: int, kvq: int) -> int:
+    return int(lib().hc_kvq_work_bytes(ctx, kvq))
+
+
+def _typed(x: Ptr, kind: torch.dtype, nbytes: int, what: str) -> Optional[int]:
+    if isinstance(x, torch.Tensor) and x.dtype is not kind:
+        raise ValueError(f"{what} is {x.dtype}, not {kind}")
+    return _sized(x, nbytes, what)
+
+
+def _cache(kvq: int, arena: Ptr, state: Ptr, acc: Ptr, what: str):
+    """Addresses of a cache, its state and its weights, of the sizes that its table says."""
+    B, _, Hkv, size, rows = _tables.get(kvq, (0, 0, 0, 0, 0))
+    return (_sized(arena, size, what + ": the cache"), _typed(state, torch.int32, 8 * B * Hkv, what + ": state"),
+            _typed(acc, torch.float32, 4 * rows, what + ": acc"))
+
+
+def _kvq_chunks(kvq: int, first, count, k_off, v_off, what: str):
+    first, count, k_off, v_off = _chunks(first, count, k_off, v_off)
+    made = _tables.get(kvq)
+    if made is not None and (len(first) != made[0] or len(k_off) != made[0] * made[2]):
+        raise ValueError(f"{what}: {len(first)} sequences and {len(k_off)} heads; the context (B, Hq, Hkv) has {made[:3]}")
+    return first, count, k_off, v_off
+
+
+def hc_kvq_store(ctx: int, kvq: int, kv_prefill: Ptr, k_off: Sequence[int], v_off: Sequence[int], first: Sequence[int], count: Sequence[int], arena: Ptr,
+                 state: Ptr, acc: Ptr = None, stream=None) -> None:
+    first, count, k_off, v_off = _kvq_chunks(kvq, first, count, k_off, v_off, "hc_kvq_store")
+    _check(lib().hc_kvq_store(ctx, kvq, _p(kv_prefill), _at(k_off), _at(v_off), _at(first), _at(count), *_cache(kvq, arena, state, acc, "hc_kvq_store"),
+                              _stream(stream)), "hc_kvq_store", ctx)
+
+
+def hc_kvq_load(ctx: int, kvq: int, arena: Ptr, state: Ptr, first: Sequence[int], count: Sequence[int], kv_out: Ptr, k_off: Sequence[int],
+                v_off: Sequence[int], stream=None) -> None:
+    first, count, k_off, v_off = _kvq_chunks(kvq, first, count, k_off, v_off, "hc_kvq_load")
+    arena, state, _ = _cache(kvq, arena, state, None, "hc_kvq_load")
+    _check(lib().hc_kvq_load(ctx, kvq, arena, state, _at(first), _at(count), _p(kv_out), _at(k_off), _at(v_off), _stream(stream)), "hc_kvq_load", ctx)
+
+
+def hc_kvq_append(ctx: int, kvq: int, rope: hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Ptr, arena: Ptr, state: Ptr,
+                  acc: Ptr = None, stream=None) -> None:
+    """q [B, Hq, 128], k and v [B, Hkv, 128]: tensors or views with any stride from sequence to sequence."""
+    made, tokens = _made.get(ctx), q.shape
+    if made is not None and tokens[0] != made[0]:
+        raise ValueError(f"hc_kvq_append: rows of {tokens[0]} sequences; the context (B, Hq, Hkv) has {made}")
+    rows = _qkv(q, k, v, made)
+    q_out = _typed(q_out, torch.bfloat16, tokens[0] * tokens[1] * 256, "hc_kvq_append: q_out")
+    _check(lib().hc_kvq_append(ctx, kvq, C.byref(rope), *rows, q_out, *_cache(kvq, arena, state, acc, "hc_kvq_append"), _stream(stream)), "hc_kvq_append", ctx)
+
+
+def hc_kvq_attn(ctx: int, kvq: int, arena: Ptr, state: Ptr, q: Ptr, out: Ptr, lse: Ptr, acc: Ptr, decay: float, work: Ptr, work_bytes: int,
+                stream=None) -> None:
+    """q [B, Hq, 128] bf16, out [B, Hq, 128] f32, lse [B, Hq] f32."""
+    made = _tables.get(kvq)
+    rows = 0 if made is None else made[0] * made[1]
+    _check(lib().hc_kvq_attn(ctx, kvq, *_cache(kvq, arena, state, None, "hc_kvq_attn")[:2], _typed(q, torch.bfloat16, rows * 256, "hc_kvq_attn: q"),
+                             _typed(out, torch.float32, rows * 512, "hc_kvq_attn: out"), _typed(lse, torch.float32, rows * 4, "hc_kvq_attn: lse"),
+                             _cache(kvq, None, None, acc, "hc_kvq_attn")[2], float(decay), _sized(work, work_bytes, "hc_kvq_attn: work"), work_bytes, _stream(stream)),
+           "hc_kvq_attn", ctx)
+
+
+def hc_kvq_evict(ctx: int, kvq: int, arena: Ptr, state: Ptr, acc: Ptr, to: int, to_arena: Ptr, to_state: Ptr, to_acc: Ptr, kept: Ptr, work: Ptr,
+                 work_bytes: int, stream=None) -> None:
+    made = _tables.get(to)
+    _check(lib().hc_kvq_evict(ctx, kvq, *_cache(kvq, arena, state, acc, "hc_kvq_evict"), to, *_cache(to, to_arena, to_state, to_acc, "hc_kvq_evict: target"),
+                              _typed(kept, torch.int32, 0 if made is None else 4 * made[4], "hc_kvq_evict: kept"), _sized(work, work_bytes, "hc_kvq_evict: work"),
+                              work_bytes, _stream(stream)), "hc_kvq_evict", ctx)
 
 
 def hc_layer_window_slot(layer: int) -> int:

@@ -60,7 +60,7 @@ extern "C" const char* hc_last_error(const hc_ctx* ctx)
     return (ctx && ctx->magic == HC_CTX_MAGIC) ? ctx->err : "invalid context";
 }
 
-static bool ctx_ok(const hc_ctx* c) { return c && c->magic == HC_CTX_MAGIC; }
+static bool ctx_ok(const hc_ctx* c) { return hc_ctx_ok(c); }
 static bool layer_ok(const hc_layer* l) { return l && l->magic == HC_LAYER_MAGIC && ctx_ok(l->ctx); }
 
 static hc_status check_config(const hc_config* cfg)
@@ -1058,7 +1058,7 @@ extern "C" hc_status hc_append_kv(hc_ctx* ctx, hc_layer* layer, const void* k_ne
 }
 
 // ---- in front of the cache: rotation, prompt attention, append with rotation ----
-static hc_status rope_check(hc_ctx* ctx, const char* who, const hc_rope* r, const hc_rows_in& in, int32_t in_type, const void* q_out)
+hc_status hc_check_rope(hc_ctx* ctx, const char* who, const hc_rope* r, const hc_rows_in& in, int32_t in_type, const void* q_out)
 {
     if (!r || !in.q || !in.k || !in.v || !q_out) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
     if (in_type != HC_BF16 && in_type != HC_F32) return hc_fail(ctx, HC_EINVAL, "%s: in_type %d", who, (int)in_type);
@@ -1077,7 +1077,7 @@ static hc_status rope_check(hc_ctx* ctx, const char* who, const hc_rope* r, cons
 }
 
 // Packed tokens and the blocks of kv_prefill that they go to or come from; total: how many tokens.
-static hc_status chunk_check(hc_ctx* ctx, const char* who, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+hc_status hc_check_chunk(hc_ctx* ctx, const char* who, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
                              const int32_t* count, long long* total)
 {
     const hc_config& c = ctx->cfg;
@@ -1106,9 +1106,9 @@ extern "C" hc_status hc_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const voi
     if (!ctx_ok(ctx)) return HC_ESTATE;
     const hc_rows_in in{q, k, v, q_stride, k_stride, v_stride, in_type == HC_F32};
     long long tokens = 0;
-    hc_status s = chunk_check(ctx, "hc_prefill_rope", kv_prefill, k_off, v_off, first, count, &tokens);
+    hc_status s = hc_check_chunk(ctx, "hc_prefill_rope", kv_prefill, k_off, v_off, first, count, &tokens);
     if (s != HC_OK || tokens == 0) return s;                 // (q and the like may be NULL where there are no tokens)
-    s = rope_check(ctx, "hc_prefill_rope", rope, in, in_type, q_out);
+    s = hc_check_rope(ctx, "hc_prefill_rope", rope, in, in_type, q_out);
     if (s != HC_OK) return s;
     return hc_launch_prefill_rope(ctx, rope, in, first, count, q_out, kv_prefill, k_off, v_off, (hipStream_t)stream);
 }
@@ -1120,7 +1120,7 @@ extern "C" hc_status hc_prefill_attn(hc_ctx* ctx, const void* q, const void* kv_
 {
     if (!ctx_ok(ctx)) return HC_ESTATE;
     long long tokens = 0;
-    const hc_status s = chunk_check(ctx, "hc_prefill_attn", kv_prefill, k_off, v_off, first, count, &tokens);
+    const hc_status s = hc_check_chunk(ctx, "hc_prefill_attn", kv_prefill, k_off, v_off, first, count, &tokens);
     if (s != HC_OK || tokens == 0) return s;
     if (!q || !out || !work) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: null pointer");
     if (((uintptr_t)q | (uintptr_t)out) & 15) return hc_fail(ctx, HC_EINVAL, "hc_prefill_attn: q and out must be 16-byte aligned");
@@ -1137,7 +1137,7 @@ extern "C" hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope*
     if (!ctx_ok(ctx)) return HC_ESTATE;
     const hc_rows_in in{q, k, v, q_stride, k_stride, v_stride, in_type == HC_F32};
     hc_status s = append_check(ctx, layer, k, v, kv_arena, host_tier, "hc_append_rope");
-    if (s == HC_OK) s = rope_check(ctx, "hc_append_rope", rope, in, in_type, q_out);
+    if (s == HC_OK) s = hc_check_rope(ctx, "hc_append_rope", rope, in, in_type, q_out);
     if (s != HC_OK) return s;
     if (((uintptr_t)kv_arena | (uintptr_t)host_tier) & 15) return hc_fail(ctx, HC_EINVAL, "hc_append_rope: buffers must be 16-byte aligned");
     hipStream_t st = (hipStream_t)stream;

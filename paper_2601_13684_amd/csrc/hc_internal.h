@@ -248,6 +248,7 @@ __device__ __forceinline__ void hc_advance_head(HeadDev* __restrict__ heads, Seg
 constexpr uint32_t HC_CTX_MAGIC = 0x48435458u;    // "HCTX"
 constexpr uint32_t HC_LAYER_MAGIC = 0x48434c59u;  // "HCLY"
 
+inline bool hc_ctx_ok(const hc_ctx* c) { return c && c->magic == HC_CTX_MAGIC; }
 hc_status hc_fail(hc_ctx* ctx, hc_status st, const char* fmt, ...);
 // Does this layer's split pass filter the pivot logits (and its monitor read them that way)?
 inline bool hc_layer_filtered(const hc_ctx* ctx, const hc_layer* L)
@@ -406,6 +407,10 @@ struct hc_rows_in {
     int64_t q_stride, k_stride, v_stride;
     bool f32;
 };
+hc_status hc_check_rope(hc_ctx* ctx, const char* who, const hc_rope* r, const hc_rows_in& in, int32_t in_type, const void* q_out);
+// Packed tokens and the blocks of kv_prefill that they go to or come from; total: how many tokens.
+hc_status hc_check_chunk(hc_ctx* ctx, const char* who, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                         const int32_t* count, long long* total);
 hc_status hc_launch_prefill_rope(hc_ctx* ctx, const hc_rope* rope, const hc_rows_in& in, const int32_t* first, const int32_t* count, void* q_out,
                                  void* kv, const int64_t* k_off, const int64_t* v_off, hipStream_t st);
 hc_status hc_launch_append_rope(hc_ctx* ctx, const hc_layer* L, const hc_rope* rope, const hc_rows_in& in, void* q_out, void* arena, void* tier, hipStream_t st);

@@ -1,0 +1,689 @@
+// hc_kvq.hip -- the cache held in 4 bits (its format: hc_kvq.h): rows into it (a prompt's, the decode token's), back to bf16, and eviction by
+// accumulated weight.  Attention over it: hc_kvq_attn.hip.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+
+#include "hc_kvq.h"
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+
+// Eight elements of a row (bf16) as a dword of codes; scale: the byte of the 32 values that this lane and the three beside it hold.
+__device__ __forceinline__ uint32_t encode(const u32x4 x, uint32_t& scale)
+{
+    uint32_t top = 0;                                            // largest magnitude, as the bits of a float: they order as the numbers do, with
+#pragma unroll                                                   // infinities and NaNs behind them
+    for (int i = 0; i < 4; ++i) top = max(top, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
+    top = max(top, dpp<0xB1>(top));                              // quad_perm [1,0,3,2]
+    top = max(top, dpp<0x4E>(top));                              // quad_perm [2,3,0,1]
+    if (top >= 0x7f800000u) {
+        scale = 255u;
+        return 0u;
+    }
+    // 2^x (1 + m) <= 7 2^e = 2^(e + 2) 1.75:  e = x - 2, and one more where m > 0.75
+    scale = (uint32_t)max(((int)((top + 0x1fffffu) >> 23)) - 2, 2);
+    const float unit = kq_scale(scale);
+    const uint32_t a = x[0], b = x[1], c = x[2], d = x[3];
+    uint32_t codes = 0;                                          // (the conversion rounds to the nearest, ties to the even code, and 7 down to 6)
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(kq_bf16x2, a), unit, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(kq_bf16x2, b), unit, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(kq_bf16x2, c), unit, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(kq_bf16x2, d), unit, 3);
+    return codes;
+}
+
+// Codes and scale bytes to row `row` of K (v: of V) of a head; 16 lanes a row.  The four scale bytes of a row are stored by one lane.
+__device__ __forceinline__ void put_row(uint8_t* __restrict__ block, int cap, int v, int row, int lane16, uint32_t codes, uint32_t scale)
+{
+    uint8_t* const at = block + (v ? (int64_t)68 * cap : 0);
+    *reinterpret_cast<uint32_t*>(at + (int64_t)row * 64 + lane16 * 4) = codes;
+    uint32_t s = scale << (lane16 & 12) * 2;                     // bytes of the groups of four lanes
+    s |= dpp<0x128>(s);                                          // rotate by 8
+    s |= dpp<0x124>(s);                                          // rotate by 4
+    if (lane16 == 0) *reinterpret_cast<uint32_t*>(at + (int64_t)64 * cap + (int64_t)row * 4) = s;
+}
+
+// ---- rows in and out --------------------------------------------------------------------------------------------------------------------
+
+constexpr int RW_BLK = 256;
+constexpr int RW_TOKENS = 64;                 // of a workgroup
+constexpr int RW_SEQS = HC_PROMPT_SEQS, RW_HEADS = HC_PROMPT_HEADS;
+
+// Packed tokens of a launch, sequence by sequence, as hc_prefill_rope has them.
+struct RowsArgs {
+    uint8_t* arena;
+    uint16_t* kv;
+    const hc_kvq_head* heads;                 // of the launch's first sequence
+    int2* state;
+    float* acc;
+    int Hkv, n_seq, tokens, whole;
+    int end[RW_SEQS], first[RW_SEQS];
+    int64_t k_off[RW_HEADS], v_off[RW_HEADS];
+};
+
+// Which tokens of which sequences a workgroup takes: RW_TOKENS packed ones from blockIdx.x * RW_TOKENS on, or (whole) all of sequence blockIdx.x, which
+// are no more.  sm_seq, sm_tok: of each its sequence, and its number there.
+__device__ __forceinline__ int rows_share(const RowsArgs& a, int* sm_seq, int* sm_tok)
+{
+    const int tid = threadIdx.x;
+    const int t0 = a.whole ? (blockIdx.x > 0 ? a.end[blockIdx.x - 1] : 0) : blockIdx.x * RW_TOKENS;
+    const int n = a.whole ? a.end[blockIdx.x] - t0 : min(RW_TOKENS, a.tokens - t0);
+    if (tid < n) {
+        int lo = 0, hi = a.n_seq - 1;                            // the first sequence that ends behind this token
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.end[mid] > t0 + tid) hi = mid;
+            else lo = mid + 1;
+        }
+        sm_seq[tid] = lo;
+        sm_tok[tid] = t0 + tid - (lo > 0 ? a.end[lo - 1] : 0);
+    }
+    __syncthreads();
+    return n;
+}
+
+__global__ __launch_bounds__(RW_BLK) void kvq_store_kernel(RowsArgs a)
+{
+    __shared__ int sm_seq[RW_TOKENS], sm_tok[RW_TOKENS];
+    const int n = rows_share(a, sm_seq, sm_tok), h = blockIdx.y, tid = threadIdx.x, lane16 = tid & 15;
+    for (int i = tid >> 4; i < 2 * n; i += RW_BLK / 16) {
+        const int t = i >> 1, v = i & 1, b = sm_seq[t], bh = b * a.Hkv + h;
+        const hc_kvq_head hd = a.heads[bh];
+        const int64_t row = (int64_t)min(max(a.state[bh].x, 0), hd.cap) + sm_tok[t];
+        const int64_t from = (v ? a.v_off[bh] : a.k_off[bh]) + ((int64_t)a.first[b] + sm_tok[t]) * HC_D;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a.kv + from + lane16 * 8);
+        uint32_t scale;
+        const uint32_t codes = encode(x, scale);
+        if (row < hd.cap) {
+            put_row(a.arena + hd.off, hd.cap, v, (int)row, lane16, codes, scale);
+            if (a.acc && v == 0 && lane16 == 1) a.acc[hd.row_off + row] = 0.f;
+        }
+    }
+    if (!a.whole || n == 0) return;
+    __syncthreads();                                             // (everyone has read the state)
+    if (tid == 0) {
+        const int bh = blockIdx.x * a.Hkv + h, cap = a.heads[bh].cap;
+        const int rows = min(max(a.state[bh].x, 0), cap);
+        a.state[bh] = make_int2(min(n, cap - rows) + rows, a.first[blockIdx.x] + n);
+    }
+}
+
+// Rows and positions of the heads after a store of several workgroups to a sequence.
+__global__ __launch_bounds__(RW_BLK) void kvq_count_kernel(RowsArgs a)
+{
+    for (int bh = threadIdx.x; bh < a.n_seq * a.Hkv; bh += RW_BLK) {
+        const int b = bh / a.Hkv, n = a.end[b] - (b > 0 ? a.end[b - 1] : 0), cap = a.heads[bh].cap;
+        if (n == 0) continue;
+        const int rows = min(max(a.state[bh].x, 0), cap);
+        a.state[bh] = make_int2(min(n, cap - rows) + rows, a.first[b] + n);
+    }
+}
+
+__global__ __launch_bounds__(RW_BLK) void kvq_load_kernel(RowsArgs a)
+{
+    __shared__ int sm_seq[RW_TOKENS], sm_tok[RW_TOKENS];
+    const int n = rows_share(a, sm_seq, sm_tok), h = blockIdx.y, tid = threadIdx.x, lane16 = tid & 15;
+    for (int i = tid >> 4; i < 2 * n; i += RW_BLK / 16) {
+        const int t = i >> 1, v = i & 1, b = sm_seq[t], bh = b * a.Hkv + h;
+        const hc_kvq_head hd = a.heads[bh];
+        const int64_t row = (int64_t)a.first[b] + sm_tok[t];
+        if (row >= min(a.state[bh].x, hd.cap)) continue;
+        const uint8_t* const at = a.arena + hd.off + (v ? (int64_t)68 * hd.cap : 0);
+        const uint32_t codes = *reinterpret_cast<const uint32_t*>(at + row * 64 + lane16 * 4);
+        const float scale = kq_scale(at[(int64_t)64 * hd.cap + row * 4 + (lane16 >> 2)]);
+        const u32x4 x{kq_pair<0>(codes, scale), kq_pair<1>(codes, scale), kq_pair<2>(codes, scale), kq_pair<3>(codes, scale)};
+        *reinterpret_cast<u32x4*>(a.kv + (v ? a.v_off[bh] : a.k_off[bh]) + (int64_t)sm_tok[t] * HC_D + lane16 * 8) = x;
+    }
+}
+
+// ---- the decode token ---------------------------------------------------------------------------------------------------------------------
+
+struct TokenArgs {
+    double turns[HC_D / 2];                   // frequencies in full turns a position
+    const float *q_norm, *k_norm;
+    float eps, gain;
+    int rot, half;
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;
+    uint16_t* q_out;
+    uint8_t* arena;
+    const hc_kvq_head* heads;
+    int2* state;
+    float* acc;
+    int Hkv, G;
+};
+
+__host__ __device__ constexpr int token_threads(int G) { return (16 * (G + 2) + 63) / 64 * 64; }
+
+__device__ __forceinline__ double sum16(double x)
+{
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) x += __shfl_xor(x, d, 16);
+    return x;
+}
+
+// One workgroup per KV head and sequence: the token's K row, its V row and the G query rows of the group, 16 lanes a row, eight elements in a row to
+// each.  Norm and rotation in 64 bits: next to the border between two codes the step from one to the other is a third of the value, and whoever
+// computes in more bits than the row's own has the same row; a row a head is too little work to show.
+template <bool F32>
+__global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(TokenArgs a)
+{
+    __shared__ double2 sm_turn[HC_D / 2];
+    __shared__ double sm_x[HC_MAX_G + 1][HC_D];
+    const int bh = blockIdx.x, b = bh / a.Hkv, h = bh - b * a.Hkv, tid = threadIdx.x;
+    const hc_kvq_head hd = a.heads[bh];
+    const int2 st = a.state[bh];
+    const int lane16 = tid & 15, row = tid >> 4;                 // 0: V, 1: K, 2 + g: query head g of the group
+    const int e0 = lane16 * 8;
+    double x[8];
+    u32x4 raw{};
+    const bool mine = row < a.G + 2;
+    if (mine) {
+        const void* src = row == 0 ? a.v : row == 1 ? a.k : a.q;
+        const size_t from = (row == 0   ? (size_t)b * a.v_stride + (size_t)h * HC_D
+                             : row == 1 ? (size_t)b * a.k_stride + (size_t)h * HC_D
+                                        : (size_t)b * a.q_stride + (size_t)(h * a.G + row - 2) * HC_D) + e0;
+        if (F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = ((const float*)src)[from + e];
+        } else {
+            raw = *reinterpret_cast<const u32x4*>((const uint16_t*)src + from);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0;
+    }
+    if (2 * tid < a.rot) {
+        const double t = (double)st.y * a.turns[tid];
+        double s, c;
+        sincospi(2.0 * (t - rint(t)), &s, &c);
+        sm_turn[tid] = make_double2(c * a.gain, s * a.gain);
+    }
+    const float* const weight = row == 0 ? nullptr : row == 1 ? a.k_norm : a.q_norm;
+    double q = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q = fma(x[e], x[e], q);
+    q = sum16(q);
+    if (weight && mine) {
+        const double f = 1.0 / sqrt(q * (1.0 / HC_D) + (double)a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= f * (double)weight[e0 + e];
+    }
+    if (mine && row > 0)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sm_x[row - 1][e0 + e] = x[e];
+    __syncthreads();                                             // (and everyone has read the state)
+    if (mine && row > 0) {
+        const int half = a.rot / 2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = e0 + e;
+            if (i >= a.rot) continue;
+            const bool second = a.half ? i >= half : (i & 1);
+            const int pair = a.half ? (second ? i - half : i) : i >> 1;
+            const double other = sm_x[row - 1][a.half ? (second ? i - half : i + half) : i ^ 1];
+            const double2 t = sm_turn[pair];
+            x[e] = second ? fma(x[e], t.x, other * t.y) : fma(x[e], t.x, -other * t.y);
+        }
+    }
+    // one rounding to bf16 (through 32 bits rounded to odd, so that the two steps round as one)
+    u32x4 w{};
+    if (row == 0 && !F32) w = raw;
+    else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float f = (float)x[e];
+            uint32_t u = __float_as_uint(f);
+            if ((double)f != x[e] && !(u & 1) && (u & 0x7fffffffu) < 0x7f800000u) u += fabs((double)f) > fabs(x[e]) ? -1 : 1;
+            u = (u & 0x7fffffffu) > 0x7f800000u ? u | 0x400000u : u + 0x7fffu + ((u >> 16) & 1);
+            w[e / 2] |= e & 1 ? u & 0xffff0000u : u >> 16;
+        }
+    uint32_t scale;
+    const uint32_t codes = encode(w, scale);
+    const int at = min(max(st.x, 0), hd.cap);
+    if (mine && row >= 2) *reinterpret_cast<u32x4*>(a.q_out + ((size_t)bh * a.G + row - 2) * HC_D + e0) = w;
+    else if (row < 2 && at < hd.cap) {
+        put_row(a.arena + hd.off, hd.cap, row == 0, at, lane16, codes, scale);
+        if (a.acc && row == 0 && lane16 == 1) a.acc[hd.row_off + at] = 0.f;
+    }
+    if (tid == 0) a.state[bh] = make_int2(min(at + 1, hd.cap), st.y + 1);
+}
+
+// ---- eviction -------------------------------------------------------------------------------------------------------------------------------
+
+constexpr int EV_BLK = 1024, EV_WAVES = EV_BLK / 64;
+constexpr int EV_LDS_ROWS = 36 * 1024;        // rows whose keys LDS has room for
+constexpr int EV_BINS = 2048;
+
+// Order-preserving key of a weight: hc_score_key, larger keys first.
+struct SelectArgs {
+    const hc_kvq_head *heads, *to;
+    const int2* state;
+    int2* to_state;
+    const float* acc;
+    int32_t* list;                            // row j that stays, at the head's place in the table it is in
+    int lds_rows, list_is_to;
+};
+
+// One workgroup per head: the rows that stay, in order.
+__global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(SelectArgs a)
+{
+    __shared__ uint32_t sm_hist[EV_BINS];
+    __shared__ uint32_t sm_wave[EV_WAVES][2];
+    __shared__ uint32_t sm_found[2];
+    extern __shared__ uint32_t sm_key[];
+    const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const hc_kvq_head from = a.heads[bh], to = a.to[bh];
+    const int2 st = a.state[bh];
+    const int n = min(max(st.x, 0), from.cap), m = min(n, to.budget);
+    int32_t* const list = a.list + (a.list_is_to ? to.row_off : from.row_off);
+    if (tid == 0) a.to_state[bh] = make_int2(m, st.y);
+    if (m == n) {
+        for (int i = tid; i < n; i += EV_BLK) list[i] = i;
+        return;
+    }
+    const int lo = to.sink, hi = n - to.recent, k = m - to.sink - to.recent;      // k of [lo, hi) stay
+    const float* const acc = a.acc + from.row_off;
+    const bool held = n <= a.lds_rows;
+    if (held)
+        for (int i = tid; i < n; i += EV_BLK) sm_key[i] = hc_score_key(acc[i]);
+    auto key = [&](int i) { return held ? sm_key[i] : hc_score_key(acc[i]); };
+    uint32_t found = 0, left = k;                                // the k-th largest key's digits so far; how many of the keys that have them stay
+    if (k > 0) {
+        int shift = 21, bits = 11;
+        for (int pass = 0; pass < 3; ++pass) {
+            const uint32_t known = pass == 0 ? 0u : ~0u << (shift + bits);
+            for (int i = tid; i < EV_BINS; i += EV_BLK) sm_hist[i] = 0;
+            __syncthreads();
+            for (int i = lo + tid; i < hi; i += EV_BLK) {
+                const uint32_t u = key(i);
+                if ((u & known) == found) atomicAdd(&sm_hist[(u >> shift) & ((1u << bits) - 1)], 1u);
+            }
+            __syncthreads();
+            // bins from the largest on: thread t has bins 2047 - 2t and 2046 - 2t
+            const uint32_t c0 = sm_hist[EV_BINS - 1 - 2 * tid], c1 = sm_hist[EV_BINS - 2 - 2 * tid];
+            uint32_t sum = c0 + c1;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t o = __shfl_up(sum, d);
+                if (lane >= d) sum += o;
+            }
+            if (lane == 63) sm_wave[w][0] = sum;
+            __syncthreads();
+            uint32_t before = sum - c0 - c1;
+            for (int i = 0; i < w; ++i) before += sm_wave[i][0];
+            if (before < left && left <= before + c0 + c1) {
+                const int first = left <= before + c0;
+                sm_found[0] = (uint32_t)(first ? EV_BINS - 1 - 2 * tid : EV_BINS - 2 - 2 * tid);
+                sm_found[1] = left - before - (first ? 0u : c0);
+            }
+            __syncthreads();
+            found |= sm_found[0] << shift;
+            left = sm_found[1];
+            bits = pass == 0 ? 11 : 10;
+            shift -= bits;
+            __syncthreads();
+        }
+    } else {
+        found = ~0u;                                             // (no key is larger)
+        __syncthreads();
+    }
+    // every wave a run of rows: how many of its keys are larger, and equal; then, knowing what is before it, which rows stay
+    const int run = ((n + EV_WAVES - 1) / EV_WAVES + 63) / 64 * 64, r0 = min(n, w * run), r1 = min(n, r0 + run);
+    uint32_t larger = 0, equal = 0;
+    for (int i = r0 + lane; i - lane < r1; i += 64) {
+        const bool in = i < r1 && i >= lo && i < hi;
+        const uint32_t u = in ? key(i) : 0u;
+        larger += __popcll(__builtin_amdgcn_ballot_w64((i < r1 && !in) || (in && u > found)));
+        equal += __popcll(__builtin_amdgcn_ballot_w64(in && u == found));
+    }
+    if (lane == 0) {
+        sm_wave[w][0] = larger;
+        sm_wave[w][1] = equal;
+    }
+    __syncthreads();
+    uint32_t ties = 0, at = 0;                                   // equal keys before; rows that stay before
+    for (int i = 0; i < w; ++i) {
+        at += sm_wave[i][0];
+        ties += sm_wave[i][1];
+    }
+    at += min(ties, left);
+    const uint64_t below = (1ull << lane) - 1;
+    for (int i = r0 + lane; i - lane < r1; i += 64) {
+        const bool in = i < r1 && i >= lo && i < hi;
+        const uint32_t u = in ? key(i) : 0u;
+        const uint64_t eq = __builtin_amdgcn_ballot_w64(in && u == found);
+        const bool stays = i < r1 && (!in || u > found || (u == found && ties + __popcll(eq & below) < left));
+        const uint64_t all = __builtin_amdgcn_ballot_w64(stays);
+        if (stays) list[at + __popcll(all & below)] = i;
+        at += __popcll(all);
+        ties += __popcll(eq);
+    }
+}
+
+constexpr int MV_BLK = 256, MV_ROWS = 64;
+
+struct MoveArgs {
+    const hc_kvq_head *heads, *to;
+    const int2* to_state;
+    const int32_t* list;
+    const uint8_t* arena;
+    uint8_t* to_arena;
+    const float* acc;
+    float* to_acc;
+    int list_is_to;
+};
+
+// The rows that stay, to their places: 4 lanes of 16 bytes to a row's codes.
+__global__ __launch_bounds__(MV_BLK) void kvq_move_kernel(MoveArgs a)
+{
+    const int bh = blockIdx.y, tid = threadIdx.x;
+    const int m = a.to_state[bh].x, j = blockIdx.x * MV_ROWS + (tid >> 2), part = tid & 3;
+    if (j >= m) return;
+    const hc_kvq_head from = a.heads[bh], to = a.to[bh];
+    const int64_t i = a.list[(a.list_is_to ? to.row_off : from.row_off) + j];
+    const uint8_t* const src = a.arena + from.off;
+    uint8_t* const dst = a.to_arena + to.off;
+    const u32x4 k = *reinterpret_cast<const u32x4*>(src + i * 64 + part * 16);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(src + (int64_t)68 * from.cap + i * 64 + part * 16);
+    uint32_t more = 0;
+    if (part == 0) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)64 * from.cap + i * 4);
+    if (part == 1) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)132 * from.cap + i * 4);
+    if (part == 2) more = __float_as_uint(a.acc[from.row_off + i]);
+    *reinterpret_cast<u32x4*>(dst + (int64_t)j * 64 + part * 16) = k;
+    *reinterpret_cast<u32x4*>(dst + (int64_t)68 * to.cap + (int64_t)j * 64 + part * 16) = v;
+    if (part == 0) *reinterpret_cast<uint32_t*>(dst + (int64_t)64 * to.cap + (int64_t)j * 4) = more;
+    if (part == 1) *reinterpret_cast<uint32_t*>(dst + (int64_t)132 * to.cap + (int64_t)j * 4) = more;
+    if (part == 2) a.to_acc[to.row_off + j] = __uint_as_float(more);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------------------------
+
+bool kvq_ok(const hc_kvq* k) { return k && k->magic == HC_KVQ_MAGIC; }
+
+// The cache, its state and its tables as a call is handed them.
+hc_status cache_check(hc_ctx* ctx, const char* who, const hc_kvq* kvq, const void* arena, const int32_t* state, const float* acc, bool need_acc)
+{
+    if (!kvq_ok(kvq) || kvq->ctx != ctx) return hc_fail(ctx, HC_ESTATE, "%s: not a cache of this context", who);
+    if (!arena || !state || (need_acc && !acc)) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
+    if ((uintptr_t)arena & 63) return hc_fail(ctx, HC_EINVAL, "%s: the cache must be 64-byte aligned", who);
+    if (((uintptr_t)state & 7) || ((uintptr_t)acc & 3)) return hc_fail(ctx, HC_EINVAL, "%s: misaligned state or weights", who);
+    return HC_OK;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb)
+{
+    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+// Calls `launch` with the tokens of as many sequences at a time as a launch's arguments have room for.
+template <typename F>
+hc_status rows_launches(const hc_kvq* kvq, RowsArgs& a, const int32_t* first, const int32_t* count, const int64_t* k_off, const int64_t* v_off, void* state, F launch)
+{
+    const hc_config& c = kvq->ctx->cfg;
+    a.Hkv = c.Hkv;
+    const int most = std::min(RW_SEQS, RW_HEADS / c.Hkv);
+    for (int b0 = 0; b0 < c.B; b0 += most) {
+        a.n_seq = std::min(most, c.B - b0);
+        long long tokens = 0;
+        int longest = 0;
+        for (int i = 0; i < a.n_seq; ++i) {
+            tokens += count[b0 + i];
+            longest = std::max(longest, count[b0 + i]);
+            a.end[i] = (int)tokens;
+            a.first[i] = first[b0 + i];
+        }
+        if (tokens == 0) continue;
+        for (int i = 0; i < a.n_seq * c.Hkv; ++i) {
+            a.k_off[i] = k_off[b0 * c.Hkv + i];
+            a.v_off[i] = v_off[b0 * c.Hkv + i];
+        }
+        a.heads = kvq->heads + (size_t)b0 * c.Hkv;
+        a.state = (int2*)state + (size_t)b0 * c.Hkv;
+        a.tokens = (int)tokens;
+        a.whole = longest <= RW_TOKENS;
+        const hc_status s = launch(dim3((unsigned)(a.whole ? a.n_seq : (tokens + RW_TOKENS - 1) / RW_TOKENS), (unsigned)c.Hkv));
+        if (s != HC_OK) return s;
+    }
+    return HC_OK;
+}
+
+}   // namespace
+
+extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq** out)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    if (!heads || !out) return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: null argument");
+    *out = nullptr;
+    const int n = ctx->cfg.B * ctx->cfg.Hkv;
+    int64_t bytes = 0, rows = 0, units = 0;
+    int32_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const hc_kvq_head& h = heads[i];
+        if (h.cap < 16 || h.cap % 16 != 0 || h.cap > ctx->cfg.max_ctx)
+            return hc_fail(ctx, HC_ESHAPE, "hc_kvq_create: head %d: cap %d must be a multiple of 16, 16 .. max_ctx", i, (int)h.cap);
+        if (h.off < 0 || (h.off & 63) || h.off > ((int64_t)1 << 50) || h.row_off < 0 || h.row_off > ((int64_t)1 << 45))
+            return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: head %d: off must be a multiple of 64 bytes, and neither it nor row_off negative", i);
+        if (h.sink < 0 || h.recent < 0 || h.budget < 1 || h.budget > h.cap)
+            return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: head %d: budget %d of %d rows, sink %d, recent %d", i, (int)h.budget, (int)h.cap, (int)h.sink, (int)h.recent);
+        bytes = std::max(bytes, h.off + (int64_t)136 * h.cap);
+        rows = std::max(rows, h.row_off + h.cap);
+        units += (h.cap + KQ_TILE - 1) / KQ_TILE;
+        most = std::max(most, h.cap);
+    }
+    if (units > INT_MAX) return hc_fail(ctx, HC_ESHAPE, "hc_kvq_create: more rows than one call takes");
+    hc_kvq* k = new (std::nothrow) hc_kvq();
+    if (!k) return hc_fail(ctx, HC_ENOMEM, "host allocation failed");
+    std::vector<int> order;
+    std::vector<int2> chunks;
+    std::vector<int32_t> caps;
+    int bad = -1;
+    try {
+        k->host.assign(heads, heads + n);
+        for (int i = 0; i < n; ++i) {
+            order.push_back(i);
+            caps.push_back(heads[i].cap);
+            for (int r = 0; r < heads[i].cap; r += KQ_CHUNK) chunks.push_back(make_int2(i, r));
+        }
+    } catch (const std::bad_alloc&) {
+        delete k;
+        return hc_fail(ctx, HC_ENOMEM, "host allocation failed");
+    }
+    std::sort(order.begin(), order.end(), [&](int a, int b) { return heads[a].off < heads[b].off; });
+    for (int i = 1; i < n; ++i)
+        if (heads[order[i - 1]].off + (int64_t)136 * heads[order[i - 1]].cap > heads[order[i]].off) bad = order[i];
+    std::sort(order.begin(), order.end(), [&](int a, int b) { return heads[a].row_off < heads[b].row_off; });
+    for (int i = 1; i < n; ++i)
+        if (heads[order[i - 1]].row_off + heads[order[i - 1]].cap > heads[order[i]].row_off) bad = order[i];
+    if (bad >= 0) {
+        delete k;
+        return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: head %d: its block or its rows overlap another head's", bad);
+    }
+    k->magic = HC_KVQ_MAGIC;
+    k->ctx = ctx;
+    k->n = n;
+    k->max_cap = most;
+    k->bytes = bytes;
+    k->rows = rows;
+    k->units = units;
+    k->n_chunks = (int)chunks.size();
+    auto upload = [&](const void* from, size_t size, void** to) {
+        hipError_t e = hipMalloc(to, size);
+        return e == hipSuccess ? hipMemcpy(*to, from, size, hipMemcpyHostToDevice) : e;
+    };
+    hipError_t e = upload(heads, (size_t)n * sizeof(hc_kvq_head), (void**)&k->heads);
+    if (e == hipSuccess) e = upload(caps.data(), (size_t)n * sizeof(int32_t), (void**)&k->caps);
+    if (e == hipSuccess) e = upload(chunks.data(), chunks.size() * sizeof(int2), (void**)&k->chunks);
+    if (e == hipSuccess) e = hc_allow_lds((const void*)kvq_select_kernel);
+    if (e != hipSuccess) {
+        (void)hc_kvq_destroy(k);
+        return hc_hip_fail(ctx, e, "hc_kvq_create");
+    }
+    *out = k;
+    return HC_OK;
+}
+
+extern "C" hc_status hc_kvq_destroy(hc_kvq* k)
+{
+    if (!kvq_ok(k)) return HC_ESTATE;
+    (void)hipFree(k->heads);
+    (void)hipFree(k->caps);
+    (void)hipFree(k->chunks);
+    k->magic = 0;
+    delete k;
+    return HC_OK;
+}
+
+extern "C" size_t hc_kvq_work_bytes(const hc_ctx* ctx, const hc_kvq* kvq)
+{
+    return hc_ctx_ok(ctx) && kvq_ok(kvq) && kvq->ctx == ctx ? hc_kvq_plan(kvq).bytes : 0;
+}
+
+extern "C" hc_status hc_kvq_store(hc_ctx* ctx, const hc_kvq* kvq, const void* kv_prefill, const int64_t* k_off, const int64_t* v_off, const int32_t* first,
+                                  const int32_t* count, void* arena, int32_t* state, float* acc, void* stream)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    hc_status s = cache_check(ctx, "hc_kvq_store", kvq, arena, state, acc, false);
+    long long tokens = 0;
+    if (s == HC_OK) s = hc_check_chunk(ctx, "hc_kvq_store", kv_prefill, k_off, v_off, first, count, &tokens);
+    if (s != HC_OK || tokens == 0) return s;
+    RowsArgs a{};
+    a.arena = (uint8_t*)arena;
+    a.kv = (uint16_t*)kv_prefill;
+    hipStream_t st = (hipStream_t)stream;
+    a.acc = acc;
+    return rows_launches(kvq, a, first, count, k_off, v_off, state, [&](dim3 grid) -> hc_status {
+        kvq_store_kernel<<<grid, dim3(RW_BLK), 0, st>>>(a);
+        HC_HIP(ctx, hipGetLastError());
+        if (!a.whole) {
+            kvq_count_kernel<<<dim3(1), dim3(RW_BLK), 0, st>>>(a);
+            HC_HIP(ctx, hipGetLastError());
+        }
+        return HC_OK;
+    });
+}
+
+extern "C" hc_status hc_kvq_load(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const int32_t* first, const int32_t* count,
+                                 void* kv_out, const int64_t* k_off, const int64_t* v_off, void* stream)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    hc_status s = cache_check(ctx, "hc_kvq_load", kvq, arena, state, nullptr, false);
+    long long tokens = 0;
+    if (s == HC_OK) s = hc_check_chunk(ctx, "hc_kvq_load", kv_out, k_off, v_off, first, count, &tokens);
+    if (s != HC_OK || tokens == 0) return s;
+    RowsArgs a{};
+    a.arena = (uint8_t*)const_cast<void*>(arena);
+    a.kv = (uint16_t*)kv_out;
+    hipStream_t st = (hipStream_t)stream;
+    return rows_launches(kvq, a, first, count, k_off, v_off, const_cast<int32_t*>(state), [&](dim3 grid) -> hc_status {
+        kvq_load_kernel<<<grid, dim3(RW_BLK), 0, st>>>(a);
+        HC_HIP(ctx, hipGetLastError());
+        return HC_OK;
+    });
+}
+
+extern "C" hc_status hc_kvq_append(hc_ctx* ctx, const hc_kvq* kvq, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
+                                   int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* arena, int32_t* state, float* acc, void* stream)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    const hc_rows_in in{q, k, v, q_stride, k_stride, v_stride, in_type == HC_F32};
+    hc_status s = cache_check(ctx, "hc_kvq_append", kvq, arena, state, acc, false);
+    if (s == HC_OK) s = hc_check_rope(ctx, "hc_kvq_append", rope, in, in_type, q_out);
+    if (s != HC_OK) return s;
+    TokenArgs a{};
+    for (int i = 0; i < rope->rot_dim / 2; ++i) a.turns[i] = rope->freq[i] * (0.5 / M_PI);
+    a.q_norm = rope->q_norm;
+    a.k_norm = rope->k_norm;
+    a.eps = rope->eps;
+    a.gain = rope->gain;
+    a.rot = rope->rot_dim;
+    a.half = rope->layout == HC_ROPE_HALF;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_out = (uint16_t*)q_out;
+    a.arena = (uint8_t*)arena;
+    a.heads = kvq->heads;
+    a.state = (int2*)state;
+    a.acc = acc;
+    a.Hkv = ctx->cfg.Hkv;
+    a.G = ctx->G;
+    const dim3 grid((unsigned)kvq->n), block((unsigned)token_threads(ctx->G));
+    if (in.f32) kvq_append_kernel<true><<<grid, block, 0, (hipStream_t)stream>>>(a);
+    else kvq_append_kernel<false><<<grid, block, 0, (hipStream_t)stream>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    return HC_OK;
+}
+
+extern "C" hc_status hc_kvq_attn(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const void* q, float* out, float* lse, float* acc,
+                                 float decay, void* work, size_t work_bytes, void* stream)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    const hc_status s = cache_check(ctx, "hc_kvq_attn", kvq, arena, state, acc, false);
+    if (s != HC_OK) return s;
+    if (!q || !out || !lse || !work) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: null pointer");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: q and out must be 16-byte aligned");
+    if ((uintptr_t)lse & 3) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: misaligned float pointer");
+    if (acc && !(decay >= 0.f && decay <= 1.f)) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: decay must be 0 .. 1");
+    if ((uintptr_t)work & 255) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: work must be 256-byte aligned");
+    if (work_bytes < hc_kvq_plan(kvq).bytes)
+        return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: work buffer of %zu bytes, %zu needed", work_bytes, hc_kvq_plan(kvq).bytes);
+    return hc_launch_kvq_attn(ctx, kvq, arena, state, q, out, lse, acc, decay, work, (hipStream_t)stream);
+}
+
+extern "C" hc_status hc_kvq_evict(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const float* acc, const hc_kvq* to, void* to_arena,
+                                  int32_t* to_state, float* to_acc, int32_t* kept, void* work, size_t work_bytes, void* stream)
+{
+    if (!hc_ctx_ok(ctx)) return HC_ESTATE;
+    hc_status s = cache_check(ctx, "hc_kvq_evict", kvq, arena, state, acc, true);
+    if (s == HC_OK) s = cache_check(ctx, "hc_kvq_evict", to, to_arena, to_state, to_acc, true);
+    if (s != HC_OK) return s;
+    if ((uintptr_t)kept & 3) return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: misaligned list");
+    const size_t nh = (size_t)kvq->n * 8;
+    if (overlap(arena, (size_t)kvq->bytes, to_arena, (size_t)to->bytes) || overlap(state, nh, to_state, nh) ||
+        overlap(acc, (size_t)kvq->rows * 4, to_acc, (size_t)to->rows * 4))
+        return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: the two caches, their states or their weights overlap");
+    if (!work) return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: null pointer");
+    if ((uintptr_t)work & 255) return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: work must be 256-byte aligned");
+    if (work_bytes < hc_kvq_plan(kvq).bytes)
+        return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: work buffer of %zu bytes, %zu needed", work_bytes, hc_kvq_plan(kvq).bytes);
+    int32_t most = 1;
+    for (int i = 0; i < kvq->n; ++i) {
+        const hc_kvq_head& h = to->host[i];
+        if (h.budget < std::min((int64_t)kvq->host[i].cap, (int64_t)h.sink + h.recent))
+            return hc_fail(ctx, HC_EINVAL, "hc_kvq_evict: head %d: a budget of %d rows has no room for sink %d and recent %d", i, (int)h.budget, (int)h.sink, (int)h.recent);
+        most = std::max(most, std::min(h.budget, kvq->host[i].cap));
+    }
+    hipStream_t st = (hipStream_t)stream;
+    int32_t* const list = kept ? kept : (int32_t*)((char*)work + hc_kvq_plan(kvq).list);
+    const int lds_rows = std::min(kvq->max_cap, EV_LDS_ROWS);
+    const SelectArgs sel{kvq->heads, to->heads, (const int2*)state, (int2*)to_state, acc, list, lds_rows, kept != nullptr};
+    kvq_select_kernel<<<dim3((unsigned)kvq->n), dim3(EV_BLK), (size_t)lds_rows * sizeof(uint32_t), st>>>(sel);
+    HC_HIP(ctx, hipGetLastError());
+    const MoveArgs mv{kvq->heads, to->heads, (const int2*)to_state, list, (const uint8_t*)arena, (uint8_t*)to_arena, acc, to_acc, kept != nullptr};
+    for (int h0 = 0; h0 < kvq->n; h0 += 65535) {
+        MoveArgs m = mv;
+        m.heads += h0;
+        m.to += h0;
+        m.to_state += h0;
+        kvq_move_kernel<<<dim3((unsigned)((most + MV_ROWS - 1) / MV_ROWS), (unsigned)std::min(65535, kvq->n - h0)), dim3(MV_BLK), 0, st>>>(m);
+        HC_HIP(ctx, hipGetLastError());
+    }
+    return HC_OK;
+}

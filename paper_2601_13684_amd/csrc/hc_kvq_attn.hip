@@ -1,0 +1,450 @@
+// hc_kvq_attn.hip -- attention of the decode token over the cache held in 4 bits (its format: hc_kvq.h), and every row's share of the weights.
+//
+//   t_j = q . K[j] log2(e) / sqrt(128),   p_j = 2^(t_j - m),   out = sum_j p_j V[j] / sum_j p_j,   lse = (m + log2 sum_j p_j) ln 2
+//   acc_j <- decay acc_j + (1/G) sum_g p_gj / sum_i p_gi
+//
+// A workgroup takes an equal share of the tiles of 32 rows of all heads one after the other; lengths are on the device, and each
+// wave finds its share by itself.  A wave takes whole tiles, the next one's loads in flight under the present one's arithmetic, and nothing goes
+// through LDS until a head's end.  S^T = K Q^T and O^T = V^T P^T on the matrix cores (16x16x32), keys along S^T's rows, so that the lane that has a
+// weight is the lane that hands it to the second product, and the products' order of the keys is chosen (row 4 x + y of the first is key
+// 4 y + x) so that a load of V takes four rows side by side.
+//   K   a lane's 16 bytes are 32 values of one scale: what the first product's four steps take; q is laid out alike
+//   V   a lane's dword is 8 values of one row; of 8 rows they become, two by two, operands of 8 tiles of 16 values
+// Codes become bf16 exactly.  The matrix cores have 16 columns for a group of at most 8 query heads: the others take what the rounding of the weights to
+// bf16 leaves, in two steps, so that the weights lose nothing (8 + 8 + 8 bits): columns g, G + g, 2 G + g for the parts of query head g, added at the end.
+// Groups of eight take a second product for the last part.
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "hc_kvq.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+constexpr int KA_BLK = 256, KA_WAVES = KA_BLK / 64;
+constexpr float KA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
+constexpr float KA_LN2 = 0.6931471805599453f;
+constexpr float KA_SLACK = 8.0f;             // a weight is at most 2^8 before the reference moves
+constexpr int KA_LEAST = KA_WAVES;           // tiles of a workgroup, where there are so few
+
+struct AttnArgs {
+    const uint8_t* arena;
+    const int2* state;
+    const hc_kvq_head* heads;
+    const int32_t* caps;
+    const uint16_t* q;
+    float *part_ml, *part_o;                 // [slots][G][2], [slots][G][128]
+    float* logits;                           // q . K, [rows][G], or nullptr
+    int n;
+};
+
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + KQ_TILE - 1) / KQ_TILE; }
+
+// Tiles of a workgroup, of all.
+__device__ __forceinline__ int share(int tiles, int workgroups) { return max(KA_LEAST, (tiles + workgroups - 1) / workgroups); }
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x)
+{
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+// Sum over the columns of a row of 16 that hold the parts of one query head.
+template <int G>
+__device__ __forceinline__ float sum_parts(float x)
+{
+    x = dpp_add<0x128>(x);                   // rotate by 8
+    if (G <= 4) x = dpp_add<0x124>(x);       // by 4
+    if (G <= 2) x = dpp_add<0x122>(x);
+    if (G <= 1) x = dpp_add<0x121>(x);
+    return x;
+}
+
+struct Tile {
+    u32x4 k[2];                              // of two rows
+    uint32_t ks[2];
+    uint32_t v[8], vs[8];                    // of eight rows
+};
+
+template <int G, bool LOGITS>
+__global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
+{
+    __shared__ float sm_ml[KA_WAVES][G][2];
+    __shared__ __attribute__((aligned(16))) float sm_o[KA_WAVES][G][HC_D];
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
+
+    // this workgroup's share, and the head that it begins in
+    const int each = (a.n + 63) / 64, mine0 = min(a.n, lane * each), mine1 = min(a.n, mine0 + each);
+    int sum = 0;
+    for (int i = mine0; i < mine1; ++i) sum += tiles_of(kq_rows(a.state, a.caps, i));
+    int upto = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63), per = share(total, (int)gridDim.x);
+    const int u0 = (int)min((long long)total, (long long)blockIdx.x * per), u1 = min(total, u0 + per);
+    if (u0 >= u1) return;
+    const int owner = __popcll(__builtin_amdgcn_ballot_w64(upto <= u0));
+    int bh = __builtin_amdgcn_readfirstlane(owner * each);
+    int before = __builtin_amdgcn_readlane(upto - sum, owner);
+
+    const int part = G <= 4 ? col / G : col / 8;                 // of the weights that this column takes
+    const bool dead = part > 2;
+    const uint32_t m1 = part >= 1 ? 0xffff0000u : 0u, m2 = part >= 2 ? 0xffff0000u : 0u;
+    const float cs = dead ? 0.f : KA_SCALE;
+
+    for (int u = u0; u < u1; ++bh) {
+        const int n = kq_rows(a.state, a.caps, bh), tiles = tiles_of(n);
+        if (before + tiles <= u) {
+            before += tiles;
+            continue;
+        }
+        const int t0 = u - before, t1 = min(tiles, u1 - before);
+        const hc_kvq_head hd = a.heads[bh];
+        const uint8_t* const K = a.arena + hd.off;
+        const uint8_t* const V = K + (int64_t)68 * hd.cap;
+        const uint32_t s_off = 64u * (uint32_t)hd.cap;
+        bf16x8 Q[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
+        float ref = dead ? FLT_MAX : -FLT_MAX, l = 0.f;
+        f32x4 O[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        auto load = [&](int t, Tile& x) {
+            const uint32_t r0 = (uint32_t)t * KQ_TILE;
+            if ((int)r0 + KQ_TILE <= n) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t row = r0 + 16 * s + 4 * (col & 3) + (col >> 2);
+                    x.k[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(K + row * 64u + grp * 16u));
+                    x.ks[s] = K[s_off + row * 4u + grp];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t row = r0 + 4 * i + grp;
+                    x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(V + row * 64u + col * 4u));
+                    x.vs[i] = V[s_off + row * 4u + (col >> 2)];
+                }
+            } else {                                             // rows behind the last: zeros of K and V (their weights are zeros, too)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t row = r0 + 16 * s + 4 * (col & 3) + (col >> 2);
+                    x.k[s] = u32x4{0, 0, 0, 0};
+                    x.ks[s] = 127;
+                    if ((int)row < n) {
+                        x.k[s] = *reinterpret_cast<const u32x4*>(K + row * 64u + grp * 16u);
+                        x.ks[s] = K[s_off + row * 4u + grp];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t row = r0 + 4 * i + grp;
+                    x.v[i] = 0;
+                    x.vs[i] = 127;
+                    if ((int)row < n) {
+                        x.v[i] = *reinterpret_cast<const uint32_t*>(V + row * 64u + col * 4u);
+                        x.vs[i] = V[s_off + row * 4u + (col >> 2)];
+                    }
+                }
+            }
+        };
+        auto compute = [&](int t, const Tile& x) {
+            f32x4 S[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                S[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float f = kq_scale(x.ks[s]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const u32x4 k{kq_pair<0>(x.k[s][c], f), kq_pair<1>(x.k[s][c], f), kq_pair<2>(x.k[s][c], f), kq_pair<3>(x.k[s][c], f)};
+                    S[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), Q[c], S[s], 0, 0, 0);
+                }
+            }
+            const int r0 = t * KQ_TILE;
+            if (LOGITS) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int row = r0 + 4 * i + grp;
+                    if (col < G && row < n) a.logits[((size_t)hd.row_off + row) * G + col] = S[i >> 2][i & 3];
+                }
+            }
+            if (r0 + KQ_TILE > n) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r0 + 4 * i + grp >= n) S[i >> 2][i & 3] = -INFINITY;
+            }
+            float p[8], top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+                top = fmaxf(top, p[i]);
+            }
+            if (__builtin_amdgcn_ballot_w64(top > KA_SLACK && !dead)) {
+                float y = S[0][0] * cs;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * cs);
+                y = fmaxf(y, __shfl_xor(y, 16));
+                y = fmaxf(y, __shfl_xor(y, 32));
+                y = fmaxf(y, ref);
+                const float f = exp2f(ref - y);
+                ref = y;
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) O[j] *= f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+            }
+            uint32_t P1[8], P2[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = dead ? 0.f : __builtin_amdgcn_exp2f(p[i]);
+                l += e;
+                const float r1 = e - __uint_as_float(__float_as_uint(e) & (G == 8 ? 0xffff0000u : m1));
+                if (G == 8) {
+                    P1[i] = __float_as_uint(part ? r1 : e);
+                    P2[i] = part ? 0u : __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u));
+                } else {
+                    P1[i] = __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & m2));
+                }
+            }
+            u32x4 B1, B2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                B1[i] = __builtin_amdgcn_perm(P1[2 * i + 1], P1[2 * i], 0x07060302u);
+                if (G == 8) B2[i] = __builtin_amdgcn_perm(P2[2 * i + 1], P2[2 * i], 0x07060302u);
+            }
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i]);
+            auto values = [&](auto byte) {
+                constexpr int B = decltype(byte)::value;
+                uint32_t c[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) c[i] = kq_pair<B>(x.v[i], f[i]);
+                u32x4 lo, hi;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lo[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+                    hi[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
+                }
+                O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B1), O[2 * B], 0, 0, 0);
+                O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B1), O[2 * B + 1], 0, 0, 0);
+                if (G == 8) {
+                    O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B2), O[2 * B], 0, 0, 0);
+                    O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B2), O[2 * B + 1], 0, 0, 0);
+                }
+            };
+            values(std::integral_constant<int, 0>{});
+            values(std::integral_constant<int, 1>{});
+            values(std::integral_constant<int, 2>{});
+            values(std::integral_constant<int, 3>{});
+        };
+
+        Tile x, y;
+        int t = t0 + w;
+        if (t < t1) load(t, x);
+        for (; t < t1; t += 2 * KA_WAVES) {
+            if (t + KA_WAVES < t1) load(t + KA_WAVES, y);
+            compute(t, x);
+            if (t + KA_WAVES >= t1) break;
+            if (t + 2 * KA_WAVES < t1) load(t + 2 * KA_WAVES, x);
+            compute(t + KA_WAVES, y);
+        }
+
+        // the parts of a weight, and the waves, together
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (lane < G) {
+            sm_ml[w][lane][0] = ref;
+            sm_ml[w][lane][1] = l;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            f32x4 lo, hi;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = sum_parts<G>(O[j][r]);
+                hi[j] = sum_parts<G>(O[4 + j][r]);
+            }
+            if (col < G) {
+                float* const to = &sm_o[w][col][8 * (4 * grp + r)];
+                *reinterpret_cast<f32x4*>(to) = lo;
+                *reinterpret_cast<f32x4*>(to + 4) = hi;
+            }
+        }
+        __syncthreads();
+        const size_t slot = (size_t)blockIdx.x + bh;
+        for (int i = tid; i < G * HC_D; i += KA_BLK) {
+            const int g = i / HC_D, d = i % HC_D;
+            float m = sm_ml[0][g][0], o = 0.f, s = 0.f;
+#pragma unroll
+            for (int k = 1; k < KA_WAVES; ++k) m = fmaxf(m, sm_ml[k][g][0]);
+#pragma unroll
+            for (int k = 0; k < KA_WAVES; ++k) {
+                const float f = exp2f(sm_ml[k][g][0] - m);
+                o = fmaf(f, sm_o[k][g][d], o);
+                s = fmaf(f, sm_ml[k][g][1], s);
+            }
+            a.part_o[(slot * G + g) * HC_D + d] = o;
+            if (d == 0) {
+                a.part_ml[(slot * G + g) * 2] = m;
+                a.part_ml[(slot * G + g) * 2 + 1] = s;
+            }
+        }
+        __syncthreads();
+        u = before + t1;
+        before += tiles;
+    }
+}
+
+struct CombineArgs {
+    const int2* state;
+    const int32_t* caps;
+    const hc_kvq_head* heads;
+    const int2* chunks;
+    const float *part_ml, *part_o;
+    const float* logits;
+    float *out, *lse, *acc;
+    float decay;
+    int n, workgroups;                       // of the pass over the rows
+};
+
+// Slots of head bh: [first, first + count).
+__device__ __forceinline__ void slots_of(const CombineArgs& a, int bh, int lane, size_t& first, int& count)
+{
+    int all = 0, before = 0;
+    for (int i = lane; i < a.n; i += 64) {
+        const int t = tiles_of(kq_rows(a.state, a.caps, i));
+        all += t;
+        if (i < bh) before += t;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        all += __shfl_xor(all, d);
+        before += __shfl_xor(before, d);
+    }
+    const int per = share(all, a.workgroups), mine = tiles_of(kq_rows(a.state, a.caps, bh));
+    const int w0 = before / per;
+    first = (size_t)w0 + bh;
+    count = mine ? (before + mine - 1) / per - w0 + 1 : 0;
+}
+
+// The first n G workgroups: output and lse of a query head each.  Those behind them: KQ_CHUNK rows' weights each.
+template <int G>
+__global__ __launch_bounds__(KA_BLK) void kvq_combine_kernel(CombineArgs a)
+{
+    __shared__ float sm_o[KA_BLK / 32][HC_D];
+    __shared__ float sm_m[KA_BLK / 64], sm_l[KA_BLK / 64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int lead = a.n * G;
+    if ((int)blockIdx.x < lead) {
+        const int bh = blockIdx.x / G, g = blockIdx.x % G;
+        size_t first;
+        int count;
+        slots_of(a, bh, lane, first, count);
+        const float* const ml = a.part_ml + (first * G + g) * 2;
+        const float* const po = a.part_o + (first * G + g) * HC_D;
+        float m = -FLT_MAX;
+        for (int i = tid; i < count; i += KA_BLK) m = fmaxf(m, ml[(size_t)i * G * 2]);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        if (lane == 0) sm_m[w] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KA_BLK / 64; ++i) m = fmaxf(m, sm_m[i]);
+        // 32 lanes of four values to a partial result
+        const int lane32 = tid & 31, row = tid >> 5;
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        for (int i = row; i < count; i += KA_BLK / 32) {
+            const float f = exp2f(ml[(size_t)i * G * 2] - m);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(po + (size_t)i * G * HC_D + 4 * lane32);
+            l = fmaf(f, ml[(size_t)i * G * 2 + 1], l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+        }
+        *reinterpret_cast<f32x4*>(&sm_o[row][4 * lane32]) = o;
+        l += __shfl_xor(l, 32);                                  // (two partial results to a wave)
+        if (lane == 0) sm_l[w] = l;
+        __syncthreads();
+        if (tid < HC_D) {
+            float x = 0.f, s = 0.f;
+#pragma unroll
+            for (int i = 0; i < KA_BLK / 32; ++i) x += sm_o[i][tid];
+#pragma unroll
+            for (int i = 0; i < KA_BLK / 64; ++i) s += sm_l[i];
+            a.out[(size_t)blockIdx.x * HC_D + tid] = s == 0.f ? 0.f : x / s;       // (no rows: nothing)
+            if (tid == 0) a.lse[blockIdx.x] = s == 0.f ? -INFINITY : (m + log2f(s)) * KA_LN2;
+        }
+        return;
+    }
+    const int2 chunk = a.chunks[blockIdx.x - lead];
+    const int bh = chunk.x, n = min(kq_rows(a.state, a.caps, bh), chunk.y + KQ_CHUNK);
+    if (chunk.y >= n) return;
+    size_t first;
+    int count;
+    slots_of(a, bh, lane, first, count);
+    float ref[G], share_of[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const float* const ml = a.part_ml + (first * G + g) * 2;
+        float m = -FLT_MAX, l = 0.f;
+        for (int i = lane; i < count; i += 64) m = fmaxf(m, ml[(size_t)i * G * 2]);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        for (int i = lane; i < count; i += 64) l = fmaf(exp2f(ml[(size_t)i * G * 2] - m), ml[(size_t)i * G * 2 + 1], l);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d);
+        ref[g] = m;
+        share_of[g] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
+    }
+    const int64_t row_off = a.heads[bh].row_off;
+    for (int r = chunk.y + tid; r < n; r += KA_BLK) {
+        const float* const s = a.logits + (row_off + r) * G;
+        float x = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[g], KA_SCALE, -ref[g])), share_of[g], x);
+        a.acc[row_off + r] = fmaf(a.acc[row_off + r], a.decay, x);
+    }
+}
+
+template <int G>
+hc_status launch(hc_ctx* ctx, const AttnArgs& a, CombineArgs c, int n_chunks, hipStream_t st)
+{
+    const dim3 grid((unsigned)c.workgroups), block(KA_BLK);
+    if (a.logits) kvq_attn_kernel<G, true><<<grid, block, 0, st>>>(a);
+    else kvq_attn_kernel<G, false><<<grid, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_combine_kernel<G><<<dim3((unsigned)(a.n * G + (a.logits ? n_chunks : 0))), block, 0, st>>>(c);
+    HC_HIP(ctx, hipGetLastError());
+    return HC_OK;
+}
+
+}   // namespace
+
+hc_status hc_launch_kvq_attn(hc_ctx* ctx, const hc_kvq* k, const void* arena, const int32_t* state, const void* q, float* out, float* lse, float* acc,
+                             float decay, void* work, hipStream_t st)
+{
+    const hc_kvq_layout l = hc_kvq_plan(k);
+    float* const ml = (float*)((char*)work + l.part_ml);
+    float* const po = (float*)((char*)work + l.part_o);
+    float* const logits = acc ? (float*)((char*)work + l.logits) : nullptr;
+    const int workgroups = (int)std::min((int64_t)KQ_WG_PER_CU * ctx->n_cu, std::max((int64_t)1, (k->units + KA_LEAST - 1) / KA_LEAST));
+    const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->caps, (const uint16_t*)q, ml, po, logits, k->n};
+    const CombineArgs c{(const int2*)state, k->caps, k->heads, k->chunks, ml, po, logits, out, lse, acc, decay, k->n, workgroups};
+    switch (ctx->G) {
+    case 1: return launch<1>(ctx, a, c, k->n_chunks, st);
+    case 2: return launch<2>(ctx, a, c, k->n_chunks, st);
+    case 4: return launch<4>(ctx, a, c, k->n_chunks, st);
+    default: return launch<8>(ctx, a, c, k->n_chunks, st);
+    }
+}
