@@ -17,7 +17,7 @@ struct hc_kvq {
     int64_t units;                 // tiles of KQ_TILE rows of all heads at their caps
     std::vector<hc_kvq_head> host;
     hc_kvq_head* heads = nullptr;  // the same on the device
-    int32_t* caps = nullptr;       // [n]
+    int2* room = nullptr;          // [n]: cap, and tiles of the heads before it
     int2* chunks = nullptr;        // (head, first row) of every KQ_CHUNK rows of a head's cap
     int n_chunks = 0;
 };
@@ -40,7 +40,7 @@ inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
     l.part_ml = 0;
     l.part_o = up((size_t)l.slots * G * 2 * sizeof(float));
     l.logits = l.part_o + up((size_t)l.slots * G * HC_D * sizeof(float));
-    const size_t attn = l.logits + up((size_t)k->rows * G * sizeof(float));
+    const size_t attn = l.logits + up((size_t)k->units * KQ_TILE * G * sizeof(float));
     l.list = 0;
     const size_t evict = up((size_t)k->rows * sizeof(int32_t));
     l.bytes = attn > evict ? attn : evict;
@@ -60,8 +60,8 @@ __device__ __forceinline__ uint32_t kq_pair(uint32_t codes, float scale)
 }
 // The scale byte as the factor that the conversions take (they make no number of an infinite one, as s = 255 stands for).
 __device__ __forceinline__ float kq_scale(uint32_t s) { return __uint_as_float(s << 23); }
-__device__ __forceinline__ int kq_rows(const int2* __restrict__ state, const int32_t* __restrict__ caps, int i)
+__device__ __forceinline__ int kq_rows(const int2* __restrict__ state, const int2* __restrict__ room, int i)
 {
-    return min(max(state[i].x, 0), caps[i]);
+    return min(max(state[i].x, 0), room[i].x);
 }
 #endif

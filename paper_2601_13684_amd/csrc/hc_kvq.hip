@@ -484,18 +484,18 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
         units += (h.cap + KQ_TILE - 1) / KQ_TILE;
         most = std::max(most, h.cap);
     }
-    if (units > INT_MAX) return hc_fail(ctx, HC_ESHAPE, "hc_kvq_create: more rows than one call takes");
+    if (units + (int64_t)n * 64 > INT_MAX) return hc_fail(ctx, HC_ESHAPE, "hc_kvq_create: more rows than one call takes");
     hc_kvq* k = new (std::nothrow) hc_kvq();
     if (!k) return hc_fail(ctx, HC_ENOMEM, "host allocation failed");
     std::vector<int> order;
     std::vector<int2> chunks;
-    std::vector<int32_t> caps;
+    std::vector<int2> room;
     int bad = -1;
     try {
         k->host.assign(heads, heads + n);
         for (int i = 0; i < n; ++i) {
             order.push_back(i);
-            caps.push_back(heads[i].cap);
+            room.push_back(make_int2(heads[i].cap, i == 0 ? 0 : room[i - 1].y + (heads[i - 1].cap + KQ_TILE - 1) / KQ_TILE));
             for (int r = 0; r < heads[i].cap; r += KQ_CHUNK) chunks.push_back(make_int2(i, r));
         }
     } catch (const std::bad_alloc&) {
@@ -525,7 +525,7 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
         return e == hipSuccess ? hipMemcpy(*to, from, size, hipMemcpyHostToDevice) : e;
     };
     hipError_t e = upload(heads, (size_t)n * sizeof(hc_kvq_head), (void**)&k->heads);
-    if (e == hipSuccess) e = upload(caps.data(), (size_t)n * sizeof(int32_t), (void**)&k->caps);
+    if (e == hipSuccess) e = upload(room.data(), (size_t)n * sizeof(int2), (void**)&k->room);
     if (e == hipSuccess) e = upload(chunks.data(), chunks.size() * sizeof(int2), (void**)&k->chunks);
     if (e == hipSuccess) e = hc_allow_lds((const void*)kvq_select_kernel);
     if (e != hipSuccess) {
@@ -540,7 +540,7 @@ extern "C" hc_status hc_kvq_destroy(hc_kvq* k)
 {
     if (!kvq_ok(k)) return HC_ESTATE;
     (void)hipFree(k->heads);
-    (void)hipFree(k->caps);
+    (void)hipFree(k->room);
     (void)hipFree(k->chunks);
     k->magic = 0;
     delete k;

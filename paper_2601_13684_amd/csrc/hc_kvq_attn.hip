@@ -26,28 +26,31 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int KA_BLK = 256, KA_WAVES = KA_BLK / 64;
 constexpr float KA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
 constexpr float KA_LN2 = 0.6931471805599453f;
 constexpr float KA_SLACK = 8.0f;             // a weight is at most 2^8 before the reference moves
 constexpr int KA_LEAST = KA_WAVES;           // tiles of a workgroup, where there are so few
+constexpr int KA_START = 12;                 // what beginning a head costs a workgroup, in tiles
 
 struct AttnArgs {
     const uint8_t* arena;
     const int2* state;
     const hc_kvq_head* heads;
-    const int32_t* caps;
+    const int2* room;
     const uint16_t* q;
     float *part_ml, *part_o;                 // [slots][G][2], [slots][G][128]
-    float* logits;                           // q . K, [rows][G], or nullptr
+    float* logits;                           // q . K, [tiles of the caps][4 groups of lanes][G][8], or nullptr: see kvq_attn_kernel
     int n;
 };
 
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + KQ_TILE - 1) / KQ_TILE; }
 
-// Tiles of a workgroup, of all.
-__device__ __forceinline__ int share(int tiles, int workgroups) { return max(KA_LEAST, (tiles + workgroups - 1) / workgroups); }
+// The work is a line on which every head with rows has KA_START places and then one for each of its tiles; workgroup i has the share [i per, (i + 1) per) of it.
+__device__ __forceinline__ int places_of(int rows) { return rows > 0 ? KA_START + tiles_of(rows) : 0; }
+__device__ __forceinline__ int share(int places, int workgroups) { return max(KA_LEAST, (places + workgroups - 1) / workgroups); }
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x)
@@ -65,23 +68,61 @@ __device__ __forceinline__ float sum_parts(float x)
     return x;
 }
 
+// A tile in LDS: K's codes, V's, K's scales, V's.  K's 16-byte chunk c of row r is at place c ^ (r / 4 % 4) of the row's 64 bytes, so that the 16 lanes
+// of a phase of the reads (one chunk of 16 rows) go over all banks; the scales of row 4 x + y are at place 8 y + x, so that the eight that a lane takes for V
+// lie side by side.
+constexpr int T_V = 2048, T_KS = 4096, T_VS = T_KS + 128, T_BYTES = T_VS + 128;
+constexpr int KA_BUFS = 4, T_STEP = KA_WAVES * T_BYTES;
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// What a lane reads of a tile.
 struct Tile {
-    u32x4 k[2];                              // of two rows
+    u32x4 k[2];                              // codes and scale of K's rows 16 s + 4 (col % 4) + col / 4
     uint32_t ks[2];
-    uint32_t v[8], vs[8];                    // of eight rows
+    u32x2 v[4];                              // codes and four scales of V's rows 4 i + grp, i = 0 .. 7
+    u32x4 vs[2];
 };
+// Reads it from buffer BUF once all but `later` of the wave's loads have arrived.  One block with its wait at the end: the compiler does not tell a read of one
+// buffer from the loads into the next ones, and would wait for all of them.
+template <int BUF, int later>
+__device__ __forceinline__ void read_tile(Tile& x, uint32_t k_at, uint32_t s_at, uint32_t v_at, uint32_t f_at)
+{
+    asm volatile(
+        "s_waitcnt vmcnt(%14)\n\t"
+        "ds_read_b128 %0, %10 offset:%15\n\t"
+        "ds_read_u8 %2, %11 offset:%17\n\t"
+        "ds_read_b128 %1, %10 offset:%16\n\t"
+        "ds_read_u8 %3, %11 offset:%18\n\t"
+        "ds_read2st64_b32 %4, %12 offset0:%19 offset1:%20\n\t"
+        "ds_read2st64_b32 %5, %12 offset0:%21 offset1:%22\n\t"
+        "ds_read2st64_b32 %6, %12 offset0:%23 offset1:%24\n\t"
+        "ds_read2st64_b32 %7, %12 offset0:%25 offset1:%26\n\t"
+        "ds_read_b128 %8, %13 offset:%27\n\t"
+        "ds_read_b128 %9, %13 offset:%28\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x.k[0]), "=&v"(x.k[1]), "=&v"(x.ks[0]), "=&v"(x.ks[1]), "=&v"(x.v[0]), "=&v"(x.v[1]), "=&v"(x.v[2]), "=&v"(x.v[3]), "=&v"(x.vs[0]), "=&v"(x.vs[1])
+        : "v"(k_at), "v"(s_at), "v"(v_at), "v"(f_at), "n"(later), "n"(BUF * T_STEP), "n"(BUF * T_STEP + 1024), "n"(BUF * T_STEP + T_KS),
+          "n"(BUF * T_STEP + T_KS + 16), "n"((BUF * T_STEP + T_V) / 256), "n"((BUF * T_STEP + T_V) / 256 + 1), "n"((BUF * T_STEP + T_V) / 256 + 2),
+          "n"((BUF * T_STEP + T_V) / 256 + 3), "n"((BUF * T_STEP + T_V) / 256 + 4), "n"((BUF * T_STEP + T_V) / 256 + 5), "n"((BUF * T_STEP + T_V) / 256 + 6),
+          "n"((BUF * T_STEP + T_V) / 256 + 7), "n"(BUF * T_STEP + T_VS), "n"(BUF * T_STEP + T_VS + 16)
+        : "memory");
+}
+static_assert(T_STEP % 256 == 0 && T_V % 256 == 0 && (KA_BUFS * T_STEP) / 256 <= 272, "offsets of the reads");
 
 template <int G, bool LOGITS>
 __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
 {
     __shared__ float sm_ml[KA_WAVES][G][2];
-    __shared__ __attribute__((aligned(16))) float sm_o[KA_WAVES][G][HC_D];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KA_BUFS][KA_WAVES][T_BYTES];
+    static_assert(G * HC_D * sizeof(float) <= T_BYTES, "a wave's sums go through its first buffer");
+    auto sm_o = [&](int wave, int g) { return reinterpret_cast<float*>(&sm_tile[0][wave][0]) + g * HC_D; };
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
     // this workgroup's share, and the head that it begins in
     const int each = (a.n + 63) / 64, mine0 = min(a.n, lane * each), mine1 = min(a.n, mine0 + each);
     int sum = 0;
-    for (int i = mine0; i < mine1; ++i) sum += tiles_of(kq_rows(a.state, a.caps, i));
+    for (int i = mine0; i < mine1; ++i) sum += places_of(kq_rows(a.state, a.room, i));
     int upto = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -92,25 +133,39 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
     const int u0 = (int)min((long long)total, (long long)blockIdx.x * per), u1 = min(total, u0 + per);
     if (u0 >= u1) return;
     const int owner = __popcll(__builtin_amdgcn_ballot_w64(upto <= u0));
-    int bh = __builtin_amdgcn_readfirstlane(owner * each);
+    int bh = __builtin_amdgcn_readfirstlane(owner * each), window = bh - 64;
     int before = __builtin_amdgcn_readlane(upto - sum, owner);
+    int h_rows = 0, h_cap = 0, h_first = 0;                      // a lane's of the 64 heads from `window` on
+    int64_t h_off = 0;
 
     const int part = G <= 4 ? col / G : col / 8;                 // of the weights that this column takes
     const bool dead = part > 2;
     const uint32_t m1 = part >= 1 ? 0xffff0000u : 0u, m2 = part >= 2 ? 0xffff0000u : 0u;
     const float cs = dead ? 0.f : KA_SCALE;
 
-    for (int u = u0; u < u1; ++bh) {
-        const int n = kq_rows(a.state, a.caps, bh), tiles = tiles_of(n);
-        if (before + tiles <= u) {
-            before += tiles;
-            continue;
+    // what the lane reads of a tile: K's rows 16 s + 4 (col % 4) + col / 4 and V's 4 i + grp
+    const uint32_t tile0 = (uint32_t)(uintptr_t)(lds_char*)&sm_tile[0][w][0];
+    uint32_t k_read = tile0 + (4 * (col & 3) + (col >> 2)) * 64 + (grp ^ (col & 3)) * 16, s_read = tile0 + (8 * (col >> 2) + (col & 3)) * 4 + grp;
+    uint32_t v_read = tile0 + lane * 4, f_read = tile0 + grp * 32;
+    asm("" : "+v"(k_read), "+v"(s_read), "+v"(v_read), "+v"(f_read));      // (opaque, so that a buffer goes into an instruction's offset)
+    for (; before < u1 && bh < a.n; ++bh) {
+        if (bh >= window + 64) {
+            window = bh;
+            const int i = min(bh + lane, a.n - 1);
+            const int2 room = a.room[i];
+            h_rows = min(max(a.state[i].x, 0), room.x);
+            h_cap = room.x;
+            h_first = room.y;
+            h_off = a.heads[i].off;
         }
-        const int t0 = u - before, t1 = min(tiles, u1 - before);
-        const hc_kvq_head hd = a.heads[bh];
-        const uint8_t* const K = a.arena + hd.off;
-        const uint8_t* const V = K + (int64_t)68 * hd.cap;
-        const uint32_t s_off = 64u * (uint32_t)hd.cap;
+        const int n = __builtin_amdgcn_readlane(h_rows, bh - window), tiles = tiles_of(n), begin = before + KA_START;
+        before += places_of(n);
+        const int t0 = max(u0 - begin, 0), t1 = min(tiles, u1 - begin);
+        if (t0 >= t1) continue;
+        const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h_off >> 32), bh - window) << 32 |
+                             (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window);
+        const uint32_t cap = __builtin_amdgcn_readlane(h_cap, bh - window);
+        const int first_tile = LOGITS ? __builtin_amdgcn_readlane(h_first, bh - window) : 0;
         bf16x8 Q[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
@@ -119,45 +174,36 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        auto load = [&](int t, Tile& x) {
-            const uint32_t r0 = (uint32_t)t * KQ_TILE;
-            if ((int)r0 + KQ_TILE <= n) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint32_t row = r0 + 16 * s + 4 * (col & 3) + (col >> 2);
-                    x.k[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(K + row * 64u + grp * 16u));
-                    x.ks[s] = K[s_off + row * 4u + grp];
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t row = r0 + 4 * i + grp;
-                    x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(V + row * 64u + col * 4u));
-                    x.vs[i] = V[s_off + row * 4u + (col >> 2)];
-                }
-            } else {                                             // rows behind the last: zeros of K and V (their weights are zeros, too)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint32_t row = r0 + 16 * s + 4 * (col & 3) + (col >> 2);
-                    x.k[s] = u32x4{0, 0, 0, 0};
-                    x.ks[s] = 127;
-                    if ((int)row < n) {
-                        x.k[s] = *reinterpret_cast<const u32x4*>(K + row * 64u + grp * 16u);
-                        x.ks[s] = K[s_off + row * 4u + grp];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t row = r0 + 4 * i + grp;
-                    x.v[i] = 0;
-                    x.vs[i] = 127;
-                    if ((int)row < n) {
-                        x.v[i] = *reinterpret_cast<const uint32_t*>(V + row * 64u + col * 4u);
-                        x.vs[i] = V[s_off + row * 4u + (col >> 2)];
-                    }
-                }
+        // a lane's places: 16 bytes of codes of row lane / 4, and the scales of row 4 (lane % 8) + lane / 8 % 4, K's or V's
+        const int c_row = lane >> 2, s_row = 4 * (lane & 7) + (lane >> 3 & 3);
+        const uint32_t k_chunk = ((lane & 3) ^ (lane >> 4)) * 16, v_chunk = (lane & 3) * 16, s_base = (lane < 32 ? 64u : 132u) * cap;
+        const uint32_t k_at = c_row * 64 + k_chunk, v_at = 68 * cap + c_row * 64 + v_chunk, s_at = s_base + s_row * 4;
+        auto load = [&](int t, auto buf) {
+            lds_char* const to = (lds_char*)&sm_tile[decltype(buf)::value][w][0];
+            // (a tile behind the last is loaded from a buffer of no bytes, which costs no memory: the number of loads on their way is then always the same)
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.arena + off), 0, t < t1 ? 136u * cap : 0u, 0x00027000);
+            const int r0 = t * KQ_TILE;
+            uint32_t k0 = k_at, k1 = k_at + 1024, v0 = v_at, v1 = v_at + 1024, s0 = s_at;
+            if (r0 + KQ_TILE > n) {                              // rows behind the last repeat it; their weights and values become zeros
+                const int last = max(n - 1 - r0, 0);
+                k0 = min(c_row, last) * 64 + k_chunk;
+                k1 = min(c_row + 16, last) * 64 + k_chunk;
+                v0 = 68 * cap + min(c_row, last) * 64 + v_chunk;
+                v1 = 68 * cap + min(c_row + 16, last) * 64 + v_chunk;
+                s0 = s_base + min(s_row, last) * 4;
             }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, k0, r0 * 64, 0, 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 1024), 16, k1, r0 * 64, 0, 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_KS), 4, s0, r0 * 4, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V), 16, v0, r0 * 64, 0, 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V + 1024), 16, v1, r0 * 64, 0, 2);
         };
-        auto compute = [&](int t, const Tile& x) {
+        auto compute = [&](int t, auto buf) {
+            Tile x;
+            read_tile<decltype(buf)::value, 15>(x, k_read, s_read, v_read, f_read);
+            uint32_t xv[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xv[i] = x.v[i >> 1][i & 1];
             f32x4 S[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -169,18 +215,23 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                     S[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), Q[c], S[s], 0, 0, 0);
                 }
             }
-            const int r0 = t * KQ_TILE;
-            if (LOGITS) {
+            float f[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = r0 + 4 * i + grp;
-                    if (col < G && row < n) a.logits[((size_t)hd.row_off + row) * G + col] = S[i >> 2][i & 3];
-                }
+            for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i >> 2][i & 3] >> (col >> 2) * 8 & 255u);
+            const int r0 = t * KQ_TILE;
+            if (LOGITS && col < G) {                             // (rows 4 i + grp, i = 0 .. 7, side by side)
+                f32x4* const to = reinterpret_cast<f32x4*>(a.logits + ((size_t)(first_tile + t) * 4 + grp) * G * 8 + col * 8);
+                to[0] = S[0];
+                to[1] = S[1];
             }
             if (r0 + KQ_TILE > n) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (r0 + 4 * i + grp >= n) S[i >> 2][i & 3] = -INFINITY;
+                    if (r0 + 4 * i + grp >= n) {
+                        S[i >> 2][i & 3] = -INFINITY;
+                        xv[i] = 0;
+                        f[i] = 1.f;
+                    }
             }
             float p[8], top = -INFINITY;
 #pragma unroll
@@ -195,11 +246,11 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                 y = fmaxf(y, __shfl_xor(y, 16));
                 y = fmaxf(y, __shfl_xor(y, 32));
                 y = fmaxf(y, ref);
-                const float f = exp2f(ref - y);
+                const float less = exp2f(ref - y);
                 ref = y;
-                l *= f;
+                l *= less;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) O[j] *= f;
+                for (int j = 0; j < 8; ++j) O[j] *= less;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
             }
@@ -222,14 +273,11 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                 B1[i] = __builtin_amdgcn_perm(P1[2 * i + 1], P1[2 * i], 0x07060302u);
                 if (G == 8) B2[i] = __builtin_amdgcn_perm(P2[2 * i + 1], P2[2 * i], 0x07060302u);
             }
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i]);
             auto values = [&](auto byte) {
                 constexpr int B = decltype(byte)::value;
                 uint32_t c[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = kq_pair<B>(x.v[i], f[i]);
+                for (int i = 0; i < 8; ++i) c[i] = kq_pair<B>(xv[i], f[i]);
                 u32x4 lo, hi;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -249,16 +297,33 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
             values(std::integral_constant<int, 3>{});
         };
 
-        Tile x, y;
+        // a wave's tiles, KA_WAVES apart; while one is worked on, three are on their way
+        using B0 = std::integral_constant<int, 0>;
+        using B1 = std::integral_constant<int, 1>;
+        using B2 = std::integral_constant<int, 2>;
+        using B3 = std::integral_constant<int, 3>;
         int t = t0 + w;
-        if (t < t1) load(t, x);
-        for (; t < t1; t += 2 * KA_WAVES) {
-            if (t + KA_WAVES < t1) load(t + KA_WAVES, y);
-            compute(t, x);
-            if (t + KA_WAVES >= t1) break;
-            if (t + 2 * KA_WAVES < t1) load(t + 2 * KA_WAVES, x);
-            compute(t + KA_WAVES, y);
+        auto step = [&](auto buf) {
+            compute(t, buf);
+            load(t + 4 * KA_WAVES, buf);
+            t += KA_WAVES;
+        };
+#pragma unroll
+        for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(Q[c]));      // (they are there: the waits below count the tiles' loads alone)
+        load(t, B0{});
+        load(t + KA_WAVES, B1{});
+        load(t + 2 * KA_WAVES, B2{});
+        load(t + 3 * KA_WAVES, B3{});
+        while (t < t1) {
+            step(B0{});
+            if (t >= t1) break;
+            step(B1{});
+            if (t >= t1) break;
+            step(B2{});
+            if (t >= t1) break;
+            step(B3{});
         }
+        __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): sums go through a buffer
 
         // the parts of a weight, and the waves, together
         l += __shfl_xor(l, 16);
@@ -276,7 +341,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                 hi[j] = sum_parts<G>(O[4 + j][r]);
             }
             if (col < G) {
-                float* const to = &sm_o[w][col][8 * (4 * grp + r)];
+                float* const to = sm_o(w, col) + 8 * (4 * grp + r);
                 *reinterpret_cast<f32x4*>(to) = lo;
                 *reinterpret_cast<f32x4*>(to + 4) = hi;
             }
@@ -291,7 +356,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
 #pragma unroll
             for (int k = 0; k < KA_WAVES; ++k) {
                 const float f = exp2f(sm_ml[k][g][0] - m);
-                o = fmaf(f, sm_o[k][g][d], o);
+                o = fmaf(f, sm_o(k, g)[d], o);
                 s = fmaf(f, sm_ml[k][g][1], s);
             }
             a.part_o[(slot * G + g) * HC_D + d] = o;
@@ -301,14 +366,12 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
             }
         }
         __syncthreads();
-        u = before + t1;
-        before += tiles;
     }
 }
 
 struct CombineArgs {
     const int2* state;
-    const int32_t* caps;
+    const int2* room;
     const hc_kvq_head* heads;
     const int2* chunks;
     const float *part_ml, *part_o;
@@ -323,19 +386,19 @@ __device__ __forceinline__ void slots_of(const CombineArgs& a, int bh, int lane,
 {
     int all = 0, before = 0;
     for (int i = lane; i < a.n; i += 64) {
-        const int t = tiles_of(kq_rows(a.state, a.caps, i));
-        all += t;
-        if (i < bh) before += t;
+        const int places = places_of(kq_rows(a.state, a.room, i));
+        all += places;
+        if (i < bh) before += places;
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         all += __shfl_xor(all, d);
         before += __shfl_xor(before, d);
     }
-    const int per = share(all, a.workgroups), mine = tiles_of(kq_rows(a.state, a.caps, bh));
-    const int w0 = before / per;
+    const int per = share(all, a.workgroups), mine = tiles_of(kq_rows(a.state, a.room, bh));
+    const int begin = before + KA_START, w0 = begin / per;
     first = (size_t)w0 + bh;
-    count = mine ? (before + mine - 1) / per - w0 + 1 : 0;
+    count = mine ? (begin + mine - 1) / per - w0 + 1 : 0;
 }
 
 // The first n G workgroups: output and lse of a query head each.  Those behind them: KQ_CHUNK rows' weights each.
@@ -388,7 +451,7 @@ __global__ __launch_bounds__(KA_BLK) void kvq_combine_kernel(CombineArgs a)
         return;
     }
     const int2 chunk = a.chunks[blockIdx.x - lead];
-    const int bh = chunk.x, n = min(kq_rows(a.state, a.caps, bh), chunk.y + KQ_CHUNK);
+    const int bh = chunk.x, n = min(kq_rows(a.state, a.room, bh), chunk.y + KQ_CHUNK);
     if (chunk.y >= n) return;
     size_t first;
     int count;
@@ -408,11 +471,12 @@ __global__ __launch_bounds__(KA_BLK) void kvq_combine_kernel(CombineArgs a)
         share_of[g] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
     }
     const int64_t row_off = a.heads[bh].row_off;
+    const float* const logits = a.logits + (size_t)a.room[bh].y * KQ_TILE * G;
     for (int r = chunk.y + tid; r < n; r += KA_BLK) {
-        const float* const s = a.logits + (row_off + r) * G;
+        const float* const s = logits + ((size_t)(r / KQ_TILE) * 4 + r % 4) * G * 8 + r / 4 % 8;
         float x = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[g], KA_SCALE, -ref[g])), share_of[g], x);
+        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[g * 8], KA_SCALE, -ref[g])), share_of[g], x);
         a.acc[row_off + r] = fmaf(a.acc[row_off + r], a.decay, x);
     }
 }
@@ -438,9 +502,9 @@ hc_status hc_launch_kvq_attn(hc_ctx* ctx, const hc_kvq* k, const void* arena, co
     float* const ml = (float*)((char*)work + l.part_ml);
     float* const po = (float*)((char*)work + l.part_o);
     float* const logits = acc ? (float*)((char*)work + l.logits) : nullptr;
-    const int workgroups = (int)std::min((int64_t)KQ_WG_PER_CU * ctx->n_cu, std::max((int64_t)1, (k->units + KA_LEAST - 1) / KA_LEAST));
-    const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->caps, (const uint16_t*)q, ml, po, logits, k->n};
-    const CombineArgs c{(const int2*)state, k->caps, k->heads, k->chunks, ml, po, logits, out, lse, acc, decay, k->n, workgroups};
+    const int workgroups = (int)std::min((int64_t)KQ_WG_PER_CU * ctx->n_cu, std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
+    const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->room, (const uint16_t*)q, ml, po, logits, k->n};
+    const CombineArgs c{(const int2*)state, k->room, k->heads, k->chunks, ml, po, logits, out, lse, acc, decay, k->n, workgroups};
     switch (ctx->G) {
     case 1: return launch<1>(ctx, a, c, k->n_chunks, st);
     case 2: return launch<2>(ctx, a, c, k->n_chunks, st);
