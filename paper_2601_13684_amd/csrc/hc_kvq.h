@@ -23,12 +23,14 @@ struct hc_kvq {
 };
 constexpr uint32_t HC_KVQ_MAGIC = 0x4843344bu;
 constexpr int KQ_TILE = 32;                  // rows that a wave of the attention pass takes at a time
-constexpr int KQ_CHUNK = 2048;               // rows of accumulated weights that a workgroup takes
+constexpr int KQ_CHUNK = 1024;               // rows of accumulated weights that a workgroup takes
 constexpr int KQ_WG_PER_CU = 2;              // workgroups of the attention pass to a compute unit
+constexpr int KQ_MOST_WG = 1024;             // of them, on any device
+inline int hc_kvq_workgroups(const hc_ctx* ctx) { return ctx->n_cu * KQ_WG_PER_CU < KQ_MOST_WG ? ctx->n_cu * KQ_WG_PER_CU : KQ_MOST_WG; }
 
 // Work buffer (byte offsets): what hc_kvq_attn and hc_kvq_evict leave there, one after the other.
 struct hc_kvq_layout {
-    size_t part_ml, part_o, logits, list, bytes;
+    size_t plan, part_ml, part_o, logits, list, bytes;
     int slots;
 };
 inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
@@ -36,9 +38,10 @@ inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     const int G = k->ctx->G;
     hc_kvq_layout l;
-    l.slots = KQ_WG_PER_CU * k->ctx->n_cu + k->n;
-    l.part_ml = 0;
-    l.part_o = up((size_t)l.slots * G * 2 * sizeof(float));
+    l.slots = hc_kvq_workgroups(k->ctx) + k->n;
+    l.plan = 0;
+    l.part_ml = up((size_t)k->n * sizeof(int2));
+    l.part_o = l.part_ml + up((size_t)l.slots * G * 2 * sizeof(float));
     l.logits = l.part_o + up((size_t)l.slots * G * HC_D * sizeof(float));
     const size_t attn = l.logits + up((size_t)k->units * KQ_TILE * G * sizeof(float));
     l.list = 0;

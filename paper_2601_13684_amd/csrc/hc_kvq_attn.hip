@@ -42,7 +42,8 @@ struct AttnArgs {
     const int2* room;
     const uint16_t* q;
     float *part_ml, *part_o;                 // [slots][G][2], [slots][G][128]
-    float* logits;                           // q . K, [tiles of the caps][4 groups of lanes][G][8], or nullptr: see kvq_attn_kernel
+    int2* plan;                              // [n]: first slot of the head's partial results, and how many; of heads with rows
+    float* logits;                           // q . K, [tiles of the caps][8][G][4], or nullptr: place 2 x + y, z of a tile is row 16 y + 4 z + x
     int n;
 };
 
@@ -166,6 +167,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                              (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window);
         const uint32_t cap = __builtin_amdgcn_readlane(h_cap, bh - window);
         const int first_tile = LOGITS ? __builtin_amdgcn_readlane(h_first, bh - window) : 0;
+        if (t0 == 0 && tid == 0) a.plan[bh] = make_int2((int)blockIdx.x + bh, (begin + tiles - 1) / per - (int)blockIdx.x + 1);
         bf16x8 Q[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
@@ -200,7 +202,9 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
         };
         auto compute = [&](int t, auto buf) {
             Tile x;
-            read_tile<decltype(buf)::value, 15>(x, k_read, s_read, v_read, f_read);
+            // three tiles' loads, and where logits are stored those of the three tiles before this one: not yet behind the first tiles
+            if (LOGITS && t < t0 + 3 * KA_WAVES) __builtin_amdgcn_s_waitcnt(0x0f7f);       // vmcnt(15)
+            read_tile<decltype(buf)::value, LOGITS ? 18 : 15>(x, k_read, s_read, v_read, f_read);
             uint32_t xv[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) xv[i] = x.v[i >> 1][i & 1];
@@ -219,11 +223,8 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i >> 2][i & 3] >> (col >> 2) * 8 & 255u);
             const int r0 = t * KQ_TILE;
-            if (LOGITS && col < G) {                             // (rows 4 i + grp, i = 0 .. 7, side by side)
-                f32x4* const to = reinterpret_cast<f32x4*>(a.logits + ((size_t)(first_tile + t) * 4 + grp) * G * 8 + col * 8);
-                to[0] = S[0];
-                to[1] = S[1];
-            }
+            if (LOGITS && col < 2 * G)                           // (columns g and G + g have the same: 2 G lanes store half of the eight each)
+                *reinterpret_cast<f32x4*>(a.logits + ((size_t)(first_tile + t) * 8 + 2 * grp) * G * 4 + col * 4) = col < G ? S[0] : S[1];
             if (r0 + KQ_TILE > n) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -374,121 +375,130 @@ struct CombineArgs {
     const int2* room;
     const hc_kvq_head* heads;
     const int2* chunks;
+    const int2* plan;
     const float *part_ml, *part_o;
     const float* logits;
     float *out, *lse, *acc;
     float decay;
-    int n, workgroups;                       // of the pass over the rows
+    int n;
 };
 
-// Slots of head bh: [first, first + count).
-__device__ __forceinline__ void slots_of(const CombineArgs& a, int bh, int lane, size_t& first, int& count)
+// (m, l) and (n, k): sums l 2^m and k 2^n
+__device__ __forceinline__ void join(float& m, float& l, float n, float k)
 {
-    int all = 0, before = 0;
-    for (int i = lane; i < a.n; i += 64) {
-        const int places = places_of(kq_rows(a.state, a.room, i));
-        all += places;
-        if (i < bh) before += places;
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        all += __shfl_xor(all, d);
-        before += __shfl_xor(before, d);
-    }
-    const int per = share(all, a.workgroups), mine = tiles_of(kq_rows(a.state, a.room, bh));
-    const int begin = before + KA_START, w0 = begin / per;
-    first = (size_t)w0 + bh;
-    count = mine ? (begin + mine - 1) / per - w0 + 1 : 0;
+    const float top = fmaxf(m, n);
+    l = l * exp2f(m - top) + k * exp2f(n - top);
+    m = top;
 }
 
-// The first n G workgroups: output and lse of a query head each.  Those behind them: KQ_CHUNK rows' weights each.
+constexpr int KC_BLK = 512, KC_WAVES = KC_BLK / 64, KC_ROWS = KC_BLK / 32;
+
+// The first n G workgroups: output and lse of a query head each, KC_ROWS partial results at a time, 32 lanes of four values to each.  Those behind them:
+// KQ_CHUNK rows' weights each.
 template <int G>
-__global__ __launch_bounds__(KA_BLK) void kvq_combine_kernel(CombineArgs a)
+__global__ __launch_bounds__(KC_BLK) void kvq_combine_kernel(CombineArgs a)
 {
-    __shared__ float sm_o[KA_BLK / 32][HC_D];
-    __shared__ float sm_m[KA_BLK / 64], sm_l[KA_BLK / 64];
+    __shared__ float sm_o[KC_ROWS][HC_D];
+    __shared__ float sm_w[KQ_MOST_WG];
+    __shared__ float sm_m[KC_WAVES], sm_l[KC_WAVES];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int lead = a.n * G;
     if ((int)blockIdx.x < lead) {
         const int bh = blockIdx.x / G, g = blockIdx.x % G;
-        size_t first;
-        int count;
-        slots_of(a, bh, lane, first, count);
-        const float* const ml = a.part_ml + (first * G + g) * 2;
-        const float* const po = a.part_o + (first * G + g) * HC_D;
-        float m = -FLT_MAX;
-        for (int i = tid; i < count; i += KA_BLK) m = fmaxf(m, ml[(size_t)i * G * 2]);
+        const int2 plan = a.plan[bh];
+        const size_t first = (size_t)plan.x;
+        const int count = kq_rows(a.state, a.room, bh) ? plan.y : 0;
+        const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + first * G + g;
+        float m = -FLT_MAX, l = 0.f;
+        for (int i = tid; i < count; i += KC_BLK) {
+            const float2 x = ml[(size_t)i * G];
+            sm_w[i] = x.x;
+            join(m, l, x.x, x.y);
+        }
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        if (lane == 0) sm_m[w] = m;
+        for (int d = 32; d > 0; d >>= 1) join(m, l, __shfl_xor(m, d), __shfl_xor(l, d));
+        if (lane == 0) {
+            sm_m[w] = m;
+            sm_l[w] = l;
+        }
         __syncthreads();
+        m = sm_m[0];
+        l = sm_l[0];
 #pragma unroll
-        for (int i = 0; i < KA_BLK / 64; ++i) m = fmaxf(m, sm_m[i]);
-        // 32 lanes of four values to a partial result
+        for (int i = 1; i < KC_WAVES; ++i) join(m, l, sm_m[i], sm_l[i]);
         const int lane32 = tid & 31, row = tid >> 5;
+        const float* const po = a.part_o + (first * G + g) * HC_D + 4 * lane32;
         f32x4 o{0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
-        for (int i = row; i < count; i += KA_BLK / 32) {
-            const float f = exp2f(ml[(size_t)i * G * 2] - m);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(po + (size_t)i * G * HC_D + 4 * lane32);
-            l = fmaf(f, ml[(size_t)i * G * 2 + 1], l);
+#pragma unroll 4
+        for (int i = row; i < count; i += KC_ROWS) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(po + (size_t)i * G * HC_D);
+            const float f = exp2f(sm_w[i] - m);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
         }
         *reinterpret_cast<f32x4*>(&sm_o[row][4 * lane32]) = o;
-        l += __shfl_xor(l, 32);                                  // (two partial results to a wave)
-        if (lane == 0) sm_l[w] = l;
         __syncthreads();
         if (tid < HC_D) {
-            float x = 0.f, s = 0.f;
+            float x = 0.f;
 #pragma unroll
-            for (int i = 0; i < KA_BLK / 32; ++i) x += sm_o[i][tid];
-#pragma unroll
-            for (int i = 0; i < KA_BLK / 64; ++i) s += sm_l[i];
-            a.out[(size_t)blockIdx.x * HC_D + tid] = s == 0.f ? 0.f : x / s;       // (no rows: nothing)
-            if (tid == 0) a.lse[blockIdx.x] = s == 0.f ? -INFINITY : (m + log2f(s)) * KA_LN2;
+            for (int i = 0; i < KC_ROWS; ++i) x += sm_o[i][tid];
+            a.out[(size_t)blockIdx.x * HC_D + tid] = l == 0.f ? 0.f : x / l;       // (no rows: nothing)
+            if (tid == 0) a.lse[blockIdx.x] = l == 0.f ? -INFINITY : (m + log2f(l)) * KA_LN2;
         }
         return;
     }
     const int2 chunk = a.chunks[blockIdx.x - lead];
     const int bh = chunk.x, n = min(kq_rows(a.state, a.room, bh), chunk.y + KQ_CHUNK);
     if (chunk.y >= n) return;
-    size_t first;
-    int count;
-    slots_of(a, bh, lane, first, count);
-    float ref[G], share_of[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const float* const ml = a.part_ml + (first * G + g) * 2;
-        float m = -FLT_MAX, l = 0.f;
-        for (int i = lane; i < count; i += 64) m = fmaxf(m, ml[(size_t)i * G * 2]);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        for (int i = lane; i < count; i += 64) l = fmaf(exp2f(ml[(size_t)i * G * 2] - m), ml[(size_t)i * G * 2 + 1], l);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d);
-        ref[g] = m;
-        share_of[g] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
-    }
+    constexpr int EACH = KQ_CHUNK / KC_BLK;
     const int64_t row_off = a.heads[bh].row_off;
     const float* const logits = a.logits + (size_t)a.room[bh].y * KQ_TILE * G;
-    for (int r = chunk.y + tid; r < n; r += KA_BLK) {
-        const float* const s = logits + ((size_t)(r / KQ_TILE) * 4 + r % 4) * G * 8 + r / 4 % 8;
+    const int2 plan = a.plan[bh];
+    const size_t first = (size_t)plan.x;
+    const int count = plan.y;
+    float s[EACH][G], old[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int r = min(chunk.y + k * KC_BLK + tid, n - 1);
+        const float* const from = logits + ((size_t)(r / KQ_TILE) * 8 + r % 4 * 2 + r / 16 % 2) * G * 4 + r / 4 % 4;
+#pragma unroll
+        for (int g = 0; g < G; ++g) s[k][g] = from[g * 4];
+        old[k] = a.acc[row_off + r];
+    }
+    for (int g = w; g < G; g += KC_WAVES) {                      // a wave to a query head
+        const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + first * G + g;
+        float m = -FLT_MAX, l = 0.f;
+#pragma unroll 4
+        for (int i = lane; i < count; i += 64) {
+            const float2 x = ml[(size_t)i * G];
+            join(m, l, x.x, x.y);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) join(m, l, __shfl_xor(m, d), __shfl_xor(l, d));
+        if (lane == 0) {
+            sm_m[g] = m;
+            sm_l[g] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int r = chunk.y + k * KC_BLK + tid;
         float x = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[g * 8], KA_SCALE, -ref[g])), share_of[g], x);
-        a.acc[row_off + r] = fmaf(a.acc[row_off + r], a.decay, x);
+        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[k][g], KA_SCALE, -sm_m[g])), sm_l[g], x);
+        if (r < n) a.acc[row_off + r] = fmaf(old[k], a.decay, x);
     }
 }
 
 template <int G>
-hc_status launch(hc_ctx* ctx, const AttnArgs& a, CombineArgs c, int n_chunks, hipStream_t st)
+hc_status launch(hc_ctx* ctx, const AttnArgs& a, const CombineArgs& c, int workgroups, int n_chunks, hipStream_t st)
 {
-    const dim3 grid((unsigned)c.workgroups), block(KA_BLK);
+    const dim3 grid((unsigned)workgroups), block(KA_BLK);
     if (a.logits) kvq_attn_kernel<G, true><<<grid, block, 0, st>>>(a);
     else kvq_attn_kernel<G, false><<<grid, block, 0, st>>>(a);
     HC_HIP(ctx, hipGetLastError());
-    kvq_combine_kernel<G><<<dim3((unsigned)(a.n * G + (a.logits ? n_chunks : 0))), block, 0, st>>>(c);
+    kvq_combine_kernel<G><<<dim3((unsigned)(a.n * G + (a.logits ? n_chunks : 0))), dim3(KC_BLK), 0, st>>>(c);
     HC_HIP(ctx, hipGetLastError());
     return HC_OK;
 }
@@ -501,14 +511,15 @@ hc_status hc_launch_kvq_attn(hc_ctx* ctx, const hc_kvq* k, const void* arena, co
     const hc_kvq_layout l = hc_kvq_plan(k);
     float* const ml = (float*)((char*)work + l.part_ml);
     float* const po = (float*)((char*)work + l.part_o);
+    int2* const plan = (int2*)((char*)work + l.plan);
     float* const logits = acc ? (float*)((char*)work + l.logits) : nullptr;
-    const int workgroups = (int)std::min((int64_t)KQ_WG_PER_CU * ctx->n_cu, std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
-    const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->room, (const uint16_t*)q, ml, po, logits, k->n};
-    const CombineArgs c{(const int2*)state, k->room, k->heads, k->chunks, ml, po, logits, out, lse, acc, decay, k->n, workgroups};
+    const int workgroups = (int)std::min((int64_t)hc_kvq_workgroups(ctx), std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
+    const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->room, (const uint16_t*)q, ml, po, plan, logits, k->n};
+    const CombineArgs c{(const int2*)state, k->room, k->heads, k->chunks, plan, ml, po, logits, out, lse, acc, decay, k->n};
     switch (ctx->G) {
-    case 1: return launch<1>(ctx, a, c, k->n_chunks, st);
-    case 2: return launch<2>(ctx, a, c, k->n_chunks, st);
-    case 4: return launch<4>(ctx, a, c, k->n_chunks, st);
-    default: return launch<8>(ctx, a, c, k->n_chunks, st);
+    case 1: return launch<1>(ctx, a, c, workgroups, k->n_chunks, st);
+    case 2: return launch<2>(ctx, a, c, workgroups, k->n_chunks, st);
+    case 4: return launch<4>(ctx, a, c, workgroups, k->n_chunks, st);
+    default: return launch<8>(ctx, a, c, workgroups, k->n_chunks, st);
     }
 }
