@@ -182,7 +182,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
         const uint32_t k_at = c_row * 64 + k_chunk, v_at = 68 * cap + c_row * 64 + v_chunk, s_at = s_base + s_row * 4;
         // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
         // 224K rows of eight heads, no logits 42.4 / 43.1, logits 53.3 / 47.6; two such heads and six short ones 16.6 / 18.2, 20.1 / 19.1.
-        constexpr int NT = LOGITS ? 0 : 2;
+        static constexpr int NT = LOGITS ? 0 : 2;
         auto load = [&](int t, auto buf) {
             lds_char* const to = (lds_char*)&sm_tile[decltype(buf)::value][w][0];
             // (a tile behind the last is loaded from a buffer of no bytes, which costs no memory: the number of loads on their way is then always the same)
