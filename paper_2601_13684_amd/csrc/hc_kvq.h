@@ -20,17 +20,21 @@ struct hc_kvq {
     int2* room = nullptr;          // [n]: cap, and tiles of the heads before it
     int2* chunks = nullptr;        // (head, first row) of every KQ_CHUNK rows of a head's cap
     int n_chunks = 0;
+    int2* spans = nullptr;         // the same of every KQ_SPAN rows
+    int n_spans = 0;
 };
 constexpr uint32_t HC_KVQ_MAGIC = 0x4843344bu;
 constexpr int KQ_TILE = 32;                  // rows that a wave of the attention pass takes at a time
 constexpr int KQ_CHUNK = 1024;               // rows of accumulated weights that a workgroup takes
+constexpr int KQ_SPAN = 4096;                // rows that a workgroup of an eviction takes
+constexpr int KQ_BINS = 2048;                // of an eviction's histograms: 11 bits of a key
 constexpr int KQ_WG_PER_CU = 2;              // workgroups of the attention pass to a compute unit
 constexpr int KQ_MOST_WG = 1024;             // of them, on any device
 inline int hc_kvq_workgroups(const hc_ctx* ctx) { return ctx->n_cu * KQ_WG_PER_CU < KQ_MOST_WG ? ctx->n_cu * KQ_WG_PER_CU : KQ_MOST_WG; }
 
 // Work buffer (byte offsets): what hc_kvq_attn and hc_kvq_evict leave there, one after the other.
 struct hc_kvq_layout {
-    size_t plan, part_ml, part_o, logits, list, bytes;
+    size_t plan, part_ml, part_o, logits, list, hist, found, counts, bytes;
     int slots;
 };
 inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
@@ -45,7 +49,10 @@ inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
     l.logits = l.part_o + up((size_t)l.slots * G * HC_D * sizeof(float));
     const size_t attn = l.logits + up((size_t)k->units * KQ_TILE * G * sizeof(float));
     l.list = 0;
-    const size_t evict = up((size_t)k->rows * sizeof(int32_t));
+    l.hist = up((size_t)k->rows * sizeof(int32_t));
+    l.found = l.hist + up((size_t)k->n * 3 * KQ_BINS * sizeof(uint32_t));
+    l.counts = l.found + up((size_t)k->n * 3 * sizeof(uint2));
+    const size_t evict = l.counts + up((size_t)k->n_spans * sizeof(uint2));
     l.bytes = attn > evict ? attn : evict;
     return l;
 }

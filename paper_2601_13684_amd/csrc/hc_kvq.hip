@@ -264,107 +264,158 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------------------
 
-constexpr int EV_BLK = 1024, EV_WAVES = EV_BLK / 64;
-constexpr int EV_LDS_ROWS = 36 * 1024;        // rows whose keys LDS has room for
-constexpr int EV_BINS = 2048;
+// Keys order as the weights do (hc_score_key), larger ones first; the k-th largest is found digit by digit, 11, 11 and 10 bits from the top, with a histogram of
+// the keys that have the digits found so far.
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit(uint32_t key, int pass) { return (key >> digit_shift(pass)) & (pass == 2 ? 1023u : 2047u); }
+__device__ __forceinline__ uint32_t known_bits(int pass) { return pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u; }
 
-// Order-preserving key of a weight: hc_score_key, larger keys first.
-struct SelectArgs {
+// The bin, from the largest on, in which the k-th key is (k >= 1), and its number there.  BLK threads, KQ_BINS / BLK bins of `mine` each, largest first.
+template <int BLK>
+__device__ __forceinline__ uint2 find_bin(const uint32_t (&mine)[KQ_BINS / BLK], uint32_t k, uint32_t* sm_wave, uint32_t* sm_found)
+{
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < KQ_BINS / BLK; ++i) all += mine[i];
+    uint32_t upto = all;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) sm_wave[w] = upto;
+    __syncthreads();
+    uint32_t before = upto - all;
+    for (int i = 0; i < w; ++i) before += sm_wave[i];
+    if (before < k && k <= before + all) {
+        uint32_t at = 0, n = before;
+#pragma unroll
+        for (int i = 0; i < KQ_BINS / BLK; ++i)
+            if (n < k) {                                         // (the last bin that begins before the k-th key)
+                at = i;
+                before = n;
+                n += mine[i];
+            }
+        sm_found[0] = KQ_BINS - 1 - tid * (KQ_BINS / BLK) - at;
+        sm_found[1] = k - before;
+    }
+    __syncthreads();
+    const uint2 r = make_uint2(sm_found[0], sm_found[1]);
+    __syncthreads();
+    return r;
+}
+
+struct EvictArgs {
     const hc_kvq_head *heads, *to;
     const int2* state;
     int2* to_state;
     const float* acc;
-    int32_t* list;                            // row j that stays, at the head's place in the table it is in
-    int lds_rows, list_is_to;
+    float* to_acc;
+    const uint8_t* arena;
+    uint8_t* to_arena;
+    int32_t* list;                            // rows that stay
+    int list_is_to;                           // it is indexed as the target's tables, not the source's
+    const int2* spans;
+    uint32_t* hist;                           // [n][3][KQ_BINS]
+    uint2* found;                             // [n][3]: after a digit, the key's digits so far, and its number among the keys that have them
+    uint2* counts;                            // [spans]: rows that stay for certain, and keys equal to the k-th
 };
 
-// One workgroup per head: the rows that stay, in order.
-__global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(SelectArgs a)
+// What a head is to keep: the first `lo` of n rows, those from `hi` on, and k of those between them; all, where m == n.
+struct Keep {
+    int n, m, lo, hi, k;
+};
+__device__ __forceinline__ Keep keep_of(const hc_kvq_head& from, const hc_kvq_head& to, int2 state)
 {
-    __shared__ uint32_t sm_hist[EV_BINS];
-    __shared__ uint32_t sm_wave[EV_WAVES][2];
+    Keep x;
+    x.n = min(max(state.x, 0), from.cap);
+    x.m = min(x.n, to.budget);
+    x.lo = to.sink;
+    x.hi = x.n - to.recent;
+    x.k = x.m - to.sink - to.recent;
+    return x;
+}
+
+// Row i of a head's block to row j of another, with its weight: 4 lanes of 16 bytes to a row's codes.
+__device__ __forceinline__ void move_row(const uint8_t* __restrict__ src, const hc_kvq_head& from, int64_t i, uint8_t* __restrict__ dst, const hc_kvq_head& to, int64_t j,
+                                         int part, const float* __restrict__ acc, float* __restrict__ to_acc)
+{
+    const u32x4 k = *reinterpret_cast<const u32x4*>(src + i * 64 + part * 16);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(src + (int64_t)68 * from.cap + i * 64 + part * 16);
+    uint32_t more = 0;
+    if (part < 2) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)(part == 0 ? 64 : 132) * from.cap + i * 4);
+    if (part == 2) more = __float_as_uint(acc[from.row_off + i]);
+    *reinterpret_cast<u32x4*>(dst + j * 64 + part * 16) = k;
+    *reinterpret_cast<u32x4*>(dst + (int64_t)68 * to.cap + j * 64 + part * 16) = v;
+    if (part < 2) *reinterpret_cast<uint32_t*>(dst + (int64_t)(part == 0 ? 64 : 132) * to.cap + j * 4) = more;
+    if (part == 2) to_acc[to.row_off + j] = __uint_as_float(more);
+}
+
+constexpr int EV_BLK = 1024, EV_WAVES = EV_BLK / 64;
+constexpr int EV_LDS_ROWS = 8 * 1024;         // longest head of a table that is done a workgroup to a head
+
+// One workgroup per head: the rows that stay, in order.  Keys in LDS.
+__global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(EvictArgs a)
+{
+    __shared__ uint32_t sm_hist[KQ_BINS];
+    __shared__ uint32_t sm_wave[EV_WAVES], sm_more[EV_WAVES];
     __shared__ uint32_t sm_found[2];
-    extern __shared__ uint32_t sm_key[];
+    __shared__ uint32_t sm_key[EV_LDS_ROWS];
     const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const hc_kvq_head from = a.heads[bh], to = a.to[bh];
     const int2 st = a.state[bh];
-    const int n = min(max(st.x, 0), from.cap), m = min(n, to.budget);
+    const Keep x = keep_of(from, to, st);
     int32_t* const list = a.list + (a.list_is_to ? to.row_off : from.row_off);
-    if (tid == 0) a.to_state[bh] = make_int2(m, st.y);
-    if (m == n) {
-        for (int i = tid; i < n; i += EV_BLK) list[i] = i;
+    if (tid == 0) a.to_state[bh] = make_int2(x.m, st.y);
+    if (x.m == x.n) {
+        for (int i = tid; i < x.n; i += EV_BLK) list[i] = i;
         return;
     }
-    const int lo = to.sink, hi = n - to.recent, k = m - to.sink - to.recent;      // k of [lo, hi) stay
     const float* const acc = a.acc + from.row_off;
-    const bool held = n <= a.lds_rows;
-    if (held)
-        for (int i = tid; i < n; i += EV_BLK) sm_key[i] = hc_score_key(acc[i]);
-    auto key = [&](int i) { return held ? sm_key[i] : hc_score_key(acc[i]); };
-    uint32_t found = 0, left = k;                                // the k-th largest key's digits so far; how many of the keys that have them stay
-    if (k > 0) {
-        int shift = 21, bits = 11;
+    for (int i = tid; i < x.n; i += EV_BLK) sm_key[i] = hc_score_key(acc[i]);
+    uint32_t found = ~0u, left = x.k;                            // (no key is larger, where none stays by its weight)
+    if (x.k > 0) {
+        found = 0;
         for (int pass = 0; pass < 3; ++pass) {
-            const uint32_t known = pass == 0 ? 0u : ~0u << (shift + bits);
-            for (int i = tid; i < EV_BINS; i += EV_BLK) sm_hist[i] = 0;
+            for (int i = tid; i < KQ_BINS; i += EV_BLK) sm_hist[i] = 0;
             __syncthreads();
-            for (int i = lo + tid; i < hi; i += EV_BLK) {
-                const uint32_t u = key(i);
-                if ((u & known) == found) atomicAdd(&sm_hist[(u >> shift) & ((1u << bits) - 1)], 1u);
+            for (int i = x.lo + tid; i < x.hi; i += EV_BLK) {
+                const uint32_t u = sm_key[i];
+                if ((u & known_bits(pass)) == found) atomicAdd(&sm_hist[digit(u, pass)], 1u);
             }
             __syncthreads();
-            // bins from the largest on: thread t has bins 2047 - 2t and 2046 - 2t
-            const uint32_t c0 = sm_hist[EV_BINS - 1 - 2 * tid], c1 = sm_hist[EV_BINS - 2 - 2 * tid];
-            uint32_t sum = c0 + c1;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_up(sum, d);
-                if (lane >= d) sum += o;
-            }
-            if (lane == 63) sm_wave[w][0] = sum;
-            __syncthreads();
-            uint32_t before = sum - c0 - c1;
-            for (int i = 0; i < w; ++i) before += sm_wave[i][0];
-            if (before < left && left <= before + c0 + c1) {
-                const int first = left <= before + c0;
-                sm_found[0] = (uint32_t)(first ? EV_BINS - 1 - 2 * tid : EV_BINS - 2 - 2 * tid);
-                sm_found[1] = left - before - (first ? 0u : c0);
-            }
-            __syncthreads();
-            found |= sm_found[0] << shift;
-            left = sm_found[1];
-            bits = pass == 0 ? 11 : 10;
-            shift -= bits;
-            __syncthreads();
+            const uint32_t mine[2] = {sm_hist[KQ_BINS - 1 - 2 * tid], sm_hist[KQ_BINS - 2 - 2 * tid]};
+            const uint2 r = find_bin<EV_BLK>(mine, left, sm_wave, sm_found);
+            found |= r.x << digit_shift(pass);
+            left = r.y;
         }
-    } else {
-        found = ~0u;                                             // (no key is larger)
-        __syncthreads();
     }
+    __syncthreads();
     // every wave a run of rows: how many of its keys are larger, and equal; then, knowing what is before it, which rows stay
-    const int run = ((n + EV_WAVES - 1) / EV_WAVES + 63) / 64 * 64, r0 = min(n, w * run), r1 = min(n, r0 + run);
+    const int run = ((x.n + EV_WAVES - 1) / EV_WAVES + 63) / 64 * 64, r0 = min(x.n, w * run), r1 = min(x.n, r0 + run);
     uint32_t larger = 0, equal = 0;
     for (int i = r0 + lane; i - lane < r1; i += 64) {
-        const bool in = i < r1 && i >= lo && i < hi;
-        const uint32_t u = in ? key(i) : 0u;
+        const bool in = i < r1 && i >= x.lo && i < x.hi;
+        const uint32_t u = in ? sm_key[i] : 0u;
         larger += __popcll(__builtin_amdgcn_ballot_w64((i < r1 && !in) || (in && u > found)));
         equal += __popcll(__builtin_amdgcn_ballot_w64(in && u == found));
     }
     if (lane == 0) {
-        sm_wave[w][0] = larger;
-        sm_wave[w][1] = equal;
+        sm_wave[w] = larger;
+        sm_more[w] = equal;
     }
     __syncthreads();
     uint32_t ties = 0, at = 0;                                   // equal keys before; rows that stay before
     for (int i = 0; i < w; ++i) {
-        at += sm_wave[i][0];
-        ties += sm_wave[i][1];
+        at += sm_wave[i];
+        ties += sm_more[i];
     }
     at += min(ties, left);
     const uint64_t below = (1ull << lane) - 1;
     for (int i = r0 + lane; i - lane < r1; i += 64) {
-        const bool in = i < r1 && i >= lo && i < hi;
-        const uint32_t u = in ? key(i) : 0u;
+        const bool in = i < r1 && i >= x.lo && i < x.hi;
+        const uint32_t u = in ? sm_key[i] : 0u;
         const uint64_t eq = __builtin_amdgcn_ballot_w64(in && u == found);
         const bool stays = i < r1 && (!in || u > found || (u == found && ties + __popcll(eq & below) < left));
         const uint64_t all = __builtin_amdgcn_ballot_w64(stays);
@@ -374,40 +425,222 @@ __global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(SelectArgs a)
     }
 }
 
-constexpr int MV_BLK = 256, MV_ROWS = 64;
+// ---- the same of longer heads: a workgroup to KQ_SPAN rows, a launch to a digit ----
 
-struct MoveArgs {
-    const hc_kvq_head *heads, *to;
-    const int2* to_state;
-    const int32_t* list;
-    const uint8_t* arena;
-    uint8_t* to_arena;
-    const float* acc;
-    float* to_acc;
-    int list_is_to;
-};
+constexpr int SP_BLK = 512, SP_WAVES = SP_BLK / 64, SP_EACH = KQ_SPAN / SP_BLK;
 
-// The rows that stay, to their places: 4 lanes of 16 bytes to a row's codes.
-__global__ __launch_bounds__(MV_BLK) void kvq_move_kernel(MoveArgs a)
+__global__ __launch_bounds__(SP_BLK) void kvq_evict_clear_kernel(EvictArgs a)
 {
-    const int bh = blockIdx.y, tid = threadIdx.x;
-    const int m = a.to_state[bh].x, j = blockIdx.x * MV_ROWS + (tid >> 2), part = tid & 3;
-    if (j >= m) return;
+    const int bh = blockIdx.x;
+    const Keep x = keep_of(a.heads[bh], a.to[bh], a.state[bh]);
+    if (x.m == x.n || x.k == 0) return;
+    uint32_t* const hist = a.hist + (size_t)bh * 3 * KQ_BINS;
+    for (int i = threadIdx.x; i < 3 * KQ_BINS; i += SP_BLK) hist[i] = 0;
+}
+
+// The keys of a span that are to be told apart, wave by wave in runs of 64 SP_EACH rows; others: 0 with `in` false.
+struct SpanKeys {
+    uint32_t u[SP_EACH];
+    bool in[SP_EACH];
+};
+__device__ __forceinline__ void span_keys(const EvictArgs& a, const hc_kvq_head& from, const Keep& x, int first, SpanKeys& s)
+{
+    const int r0 = first + (threadIdx.x >> 6) * 64 * SP_EACH + (threadIdx.x & 63);
+    const float* const acc = a.acc + from.row_off;
+#pragma unroll
+    for (int k = 0; k < SP_EACH; ++k) {
+        const int r = r0 + 64 * k;
+        s.in[k] = r >= x.lo && r < x.hi;
+        s.u[k] = s.in[k] ? __float_as_uint(acc[r]) : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < SP_EACH; ++k) s.u[k] = s.in[k] ? hc_score_key(__uint_as_float(s.u[k])) : 0u;
+}
+__device__ __forceinline__ uint2 span_find(const EvictArgs& a, int bh, int pass, uint32_t k, uint32_t* sm_wave, uint32_t* sm_found)
+{
+    const u32x4 h = *reinterpret_cast<const u32x4*>(a.hist + ((size_t)bh * 3 + pass) * KQ_BINS + KQ_BINS - 4 - 4 * threadIdx.x);
+    const uint32_t mine[4] = {h[3], h[2], h[1], h[0]};
+    return find_bin<SP_BLK>(mine, k, sm_wave, sm_found);
+}
+static_assert(KQ_BINS / SP_BLK == 4, "bins of a thread");
+
+// Digit PASS of the keys that have the digits before it; the digit before it is found first.
+template <int PASS>
+__global__ __launch_bounds__(SP_BLK) void kvq_evict_digit_kernel(EvictArgs a)
+{
+    __shared__ uint32_t sm_hist[KQ_BINS], sm_wave[SP_WAVES], sm_found[2];
+    const int2 span = a.spans[blockIdx.x];
+    const int bh = span.x, tid = threadIdx.x;
+    const hc_kvq_head from = a.heads[bh];
+    const Keep x = keep_of(from, a.to[bh], a.state[bh]);
+    if (x.m == x.n || x.k == 0 || span.y >= x.hi || span.y + KQ_SPAN <= x.lo) return;
+    SpanKeys s;
+    span_keys(a, from, x, span.y, s);
+    for (int i = tid; i < KQ_BINS; i += SP_BLK) sm_hist[i] = 0;
+    uint32_t found = 0;
+    if (PASS > 0) {
+        const uint2 last = PASS == 1 ? make_uint2(0u, (uint32_t)x.k) : a.found[(size_t)bh * 3 + PASS - 2];
+        const uint2 r = span_find(a, bh, PASS - 1, last.y, sm_wave, sm_found);
+        found = last.x | r.x << digit_shift(PASS - 1);
+        if (tid == 0) a.found[(size_t)bh * 3 + PASS - 1] = make_uint2(found, r.y);       // (every span of the head writes the same)
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SP_EACH; ++k)
+        if (s.in[k] && (s.u[k] & known_bits(PASS)) == found) atomicAdd(&sm_hist[digit(s.u[k], PASS)], 1u);
+    __syncthreads();
+    uint32_t* const hist = a.hist + ((size_t)bh * 3 + PASS) * KQ_BINS;
+    for (int i = tid; i < KQ_BINS; i += SP_BLK)
+        if (sm_hist[i]) atomicAdd(&hist[i], sm_hist[i]);
+}
+
+// How many rows of a span stay for certain, and how many keys are the k-th's equals.
+__global__ __launch_bounds__(SP_BLK) void kvq_evict_count_kernel(EvictArgs a)
+{
+    __shared__ uint32_t sm_wave[SP_WAVES], sm_found[2], sm_more[SP_WAVES];
+    const int2 span = a.spans[blockIdx.x];
+    const int bh = span.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const hc_kvq_head from = a.heads[bh];
+    const Keep x = keep_of(from, a.to[bh], a.state[bh]);
+    if (x.m == x.n || span.y >= x.n) return;
+    SpanKeys s;
+    span_keys(a, from, x, span.y, s);
+    uint32_t key = ~0u;
+    if (x.k > 0) {
+        const uint2 last = a.found[(size_t)bh * 3 + 1];
+        const uint2 r = span_find(a, bh, 2, last.y, sm_wave, sm_found);
+        key = last.x | r.x;
+        if (tid == 0) a.found[(size_t)bh * 3 + 2] = make_uint2(key, r.y);
+    }
+    uint32_t larger = 0, equal = 0;
+#pragma unroll
+    for (int k = 0; k < SP_EACH; ++k) {
+        const int r = span.y + w * 64 * SP_EACH + 64 * k + lane;
+        larger += __popcll(__builtin_amdgcn_ballot_w64(r < x.n && (!s.in[k] || s.u[k] > key)));
+        equal += __popcll(__builtin_amdgcn_ballot_w64(s.in[k] && s.u[k] == key));
+    }
+    __syncthreads();
+    if (lane == 0) {
+        sm_wave[w] = larger;
+        sm_more[w] = equal;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        for (int i = 1; i < SP_WAVES; ++i) {
+            larger += sm_wave[i];
+            equal += sm_more[i];
+        }
+        a.counts[blockIdx.x] = make_uint2(larger, equal);
+    }
+}
+
+// The rows of a span that stay, to their places.
+__global__ __launch_bounds__(SP_BLK) void kvq_evict_place_kernel(EvictArgs a)
+{
+    __shared__ uint32_t sm_wave[SP_WAVES], sm_more[SP_WAVES];
+    __shared__ uint16_t sm_list[KQ_SPAN];
+    const int2 span = a.spans[blockIdx.x];
+    const int bh = span.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const hc_kvq_head from = a.heads[bh], to = a.to[bh];
-    const int64_t i = a.list[(a.list_is_to ? to.row_off : from.row_off) + j];
+    const int2 st = a.state[bh];
+    const Keep x = keep_of(from, to, st);
+    if (span.y == 0 && tid == 0) a.to_state[bh] = make_int2(x.m, st.y);
+    if (span.y >= x.n) return;
+    int count, at;                                               // rows of this span that stay; the first one's place
+    if (x.m == x.n) {
+        count = min(KQ_SPAN, x.n - span.y);
+        at = span.y;
+        for (int i = tid; i < count; i += SP_BLK) sm_list[i] = (uint16_t)i;
+    } else {
+        SpanKeys s;
+        span_keys(a, from, x, span.y, s);
+        const uint2 last = x.k > 0 ? a.found[(size_t)bh * 3 + 2] : make_uint2(~0u, 0u);
+        // what the head's spans before this one keep
+        const int index = span.y / KQ_SPAN;
+        uint32_t larger = 0, equal = 0;
+        for (int i = tid; i < index; i += SP_BLK) {
+            const uint2 c = a.counts[blockIdx.x - index + i];
+            larger += c.x;
+            equal += c.y;
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            larger += __shfl_xor(larger, d);
+            equal += __shfl_xor(equal, d);
+        }
+        if (lane == 0) {
+            sm_wave[w] = larger;
+            sm_more[w] = equal;
+        }
+        __syncthreads();
+        uint32_t ties = 0, before = 0;
+        for (int i = 0; i < SP_WAVES; ++i) {
+            before += sm_wave[i];
+            ties += sm_more[i];
+        }
+        before += min(ties, last.y);
+        __syncthreads();
+        larger = equal = 0;
+#pragma unroll
+        for (int k = 0; k < SP_EACH; ++k) {
+            const int r = span.y + w * 64 * SP_EACH + 64 * k + lane;
+            larger += __popcll(__builtin_amdgcn_ballot_w64(r < x.n && (!s.in[k] || s.u[k] > last.x)));
+            equal += __popcll(__builtin_amdgcn_ballot_w64(s.in[k] && s.u[k] == last.x));
+        }
+        if (lane == 0) {
+            sm_wave[w] = larger;
+            sm_more[w] = equal;
+        }
+        __syncthreads();
+        const uint32_t ties0 = ties;
+        uint32_t here = 0, all = 0, all_ties = ties;
+        for (int i = 0; i < SP_WAVES; ++i) {
+            if (i < w) {
+                here += sm_wave[i];
+                ties += sm_more[i];
+            }
+            all += sm_wave[i];
+            all_ties += sm_more[i];
+        }
+        const uint32_t kept0 = min(ties0, last.y);
+        here += min(ties, last.y) - kept0;
+        count = (int)(all + min(all_ties, last.y) - kept0);
+        at = (int)before;
+        const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+        for (int k = 0; k < SP_EACH; ++k) {
+            const int i = w * 64 * SP_EACH + 64 * k + lane, r = span.y + i;
+            const uint64_t eq = __builtin_amdgcn_ballot_w64(s.in[k] && s.u[k] == last.x);
+            const bool stays = r < x.n && (!s.in[k] || s.u[k] > last.x || (s.u[k] == last.x && ties + __popcll(eq & below) < last.y));
+            const uint64_t some = __builtin_amdgcn_ballot_w64(stays);
+            if (stays) sm_list[here + __popcll(some & below)] = (uint16_t)i;
+            here += __popcll(some);
+            ties += __popcll(eq);
+        }
+    }
+    __syncthreads();
+    if (a.list)
+        for (int i = tid; i < count; i += SP_BLK) a.list[to.row_off + at + i] = span.y + sm_list[i];
     const uint8_t* const src = a.arena + from.off;
     uint8_t* const dst = a.to_arena + to.off;
-    const u32x4 k = *reinterpret_cast<const u32x4*>(src + i * 64 + part * 16);
-    const u32x4 v = *reinterpret_cast<const u32x4*>(src + (int64_t)68 * from.cap + i * 64 + part * 16);
-    uint32_t more = 0;
-    if (part == 0) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)64 * from.cap + i * 4);
-    if (part == 1) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)132 * from.cap + i * 4);
-    if (part == 2) more = __float_as_uint(a.acc[from.row_off + i]);
-    *reinterpret_cast<u32x4*>(dst + (int64_t)j * 64 + part * 16) = k;
-    *reinterpret_cast<u32x4*>(dst + (int64_t)68 * to.cap + (int64_t)j * 64 + part * 16) = v;
-    if (part == 0) *reinterpret_cast<uint32_t*>(dst + (int64_t)64 * to.cap + (int64_t)j * 4) = more;
-    if (part == 1) *reinterpret_cast<uint32_t*>(dst + (int64_t)132 * to.cap + (int64_t)j * 4) = more;
-    if (part == 2) a.to_acc[to.row_off + j] = __uint_as_float(more);
+    const int part = tid & 3;
+#pragma unroll 2
+    for (int q = tid >> 2; q < count; q += SP_BLK / 4) {
+        const int64_t i = span.y + sm_list[q], j = at + q;
+        move_row(src, from, i, dst, to, j, part, a.acc, a.to_acc);
+    }
+}
+
+constexpr int MV_BLK = 256, MV_ROWS = 64;
+
+// The rows that stay, to their places.
+__global__ __launch_bounds__(MV_BLK) void kvq_move_kernel(EvictArgs a)
+{
+    const int bh = blockIdx.y, tid = threadIdx.x;
+    const int m = a.to_state[bh].x, j = blockIdx.x * MV_ROWS + (tid >> 2);
+    if (j >= m) return;
+    const hc_kvq_head from = a.heads[bh], to = a.to[bh];
+    move_row(a.arena + from.off, from, a.list[(a.list_is_to ? to.row_off : from.row_off) + j], a.to_arena + to.off, to, j, tid & 3, a.acc, a.to_acc);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------------
@@ -488,7 +721,7 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
     hc_kvq* k = new (std::nothrow) hc_kvq();
     if (!k) return hc_fail(ctx, HC_ENOMEM, "host allocation failed");
     std::vector<int> order;
-    std::vector<int2> chunks;
+    std::vector<int2> chunks, spans;
     std::vector<int2> room;
     int bad = -1;
     try {
@@ -497,6 +730,7 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
             order.push_back(i);
             room.push_back(make_int2(heads[i].cap, i == 0 ? 0 : room[i - 1].y + (heads[i - 1].cap + KQ_TILE - 1) / KQ_TILE));
             for (int r = 0; r < heads[i].cap; r += KQ_CHUNK) chunks.push_back(make_int2(i, r));
+            for (int r = 0; r < heads[i].cap; r += KQ_SPAN) spans.push_back(make_int2(i, r));
         }
     } catch (const std::bad_alloc&) {
         delete k;
@@ -520,6 +754,7 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
     k->rows = rows;
     k->units = units;
     k->n_chunks = (int)chunks.size();
+    k->n_spans = (int)spans.size();
     auto upload = [&](const void* from, size_t size, void** to) {
         hipError_t e = hipMalloc(to, size);
         return e == hipSuccess ? hipMemcpy(*to, from, size, hipMemcpyHostToDevice) : e;
@@ -527,7 +762,7 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
     hipError_t e = upload(heads, (size_t)n * sizeof(hc_kvq_head), (void**)&k->heads);
     if (e == hipSuccess) e = upload(room.data(), (size_t)n * sizeof(int2), (void**)&k->room);
     if (e == hipSuccess) e = upload(chunks.data(), chunks.size() * sizeof(int2), (void**)&k->chunks);
-    if (e == hipSuccess) e = hc_allow_lds((const void*)kvq_select_kernel);
+    if (e == hipSuccess) e = upload(spans.data(), spans.size() * sizeof(int2), (void**)&k->spans);
     if (e != hipSuccess) {
         (void)hc_kvq_destroy(k);
         return hc_hip_fail(ctx, e, "hc_kvq_create");
@@ -542,6 +777,7 @@ extern "C" hc_status hc_kvq_destroy(hc_kvq* k)
     (void)hipFree(k->heads);
     (void)hipFree(k->room);
     (void)hipFree(k->chunks);
+    (void)hipFree(k->spans);
     k->magic = 0;
     delete k;
     return HC_OK;
@@ -671,19 +907,40 @@ extern "C" hc_status hc_kvq_evict(hc_ctx* ctx, const hc_kvq* kvq, const void* ar
         most = std::max(most, std::min(h.budget, kvq->host[i].cap));
     }
     hipStream_t st = (hipStream_t)stream;
-    int32_t* const list = kept ? kept : (int32_t*)((char*)work + hc_kvq_plan(kvq).list);
-    const int lds_rows = std::min(kvq->max_cap, EV_LDS_ROWS);
-    const SelectArgs sel{kvq->heads, to->heads, (const int2*)state, (int2*)to_state, acc, list, lds_rows, kept != nullptr};
-    kvq_select_kernel<<<dim3((unsigned)kvq->n), dim3(EV_BLK), (size_t)lds_rows * sizeof(uint32_t), st>>>(sel);
-    HC_HIP(ctx, hipGetLastError());
-    const MoveArgs mv{kvq->heads, to->heads, (const int2*)to_state, list, (const uint8_t*)arena, (uint8_t*)to_arena, acc, to_acc, kept != nullptr};
-    for (int h0 = 0; h0 < kvq->n; h0 += 65535) {
-        MoveArgs m = mv;
-        m.heads += h0;
-        m.to += h0;
-        m.to_state += h0;
-        kvq_move_kernel<<<dim3((unsigned)((most + MV_ROWS - 1) / MV_ROWS), (unsigned)std::min(65535, kvq->n - h0)), dim3(MV_BLK), 0, st>>>(m);
+    const hc_kvq_layout l = hc_kvq_plan(kvq);
+    char* const w = (char*)work;
+    EvictArgs a{kvq->heads, to->heads, (const int2*)state, (int2*)to_state, acc, to_acc, (const uint8_t*)arena, (uint8_t*)to_arena, kept, 1, kvq->spans,
+                (uint32_t*)(w + l.hist), (uint2*)(w + l.found), (uint2*)(w + l.counts)};
+    const dim3 heads((unsigned)kvq->n);
+    if (kvq->max_cap <= EV_LDS_ROWS) {
+        if (!kept) {
+            a.list = (int32_t*)(w + l.list);
+            a.list_is_to = 0;
+        }
+        kvq_select_kernel<<<heads, dim3(EV_BLK), 0, st>>>(a);
         HC_HIP(ctx, hipGetLastError());
+        for (int h0 = 0; h0 < kvq->n; h0 += 65535) {
+            EvictArgs m = a;
+            m.heads += h0;
+            m.to += h0;
+            m.to_state += h0;
+            kvq_move_kernel<<<dim3((unsigned)((most + MV_ROWS - 1) / MV_ROWS), (unsigned)std::min(65535, kvq->n - h0)), dim3(MV_BLK), 0, st>>>(m);
+            HC_HIP(ctx, hipGetLastError());
+        }
+        return HC_OK;
     }
+    const dim3 spans((unsigned)kvq->n_spans), block(SP_BLK);
+    kvq_evict_clear_kernel<<<heads, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_evict_digit_kernel<0><<<spans, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_evict_digit_kernel<1><<<spans, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_evict_digit_kernel<2><<<spans, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_evict_count_kernel<<<spans, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
+    kvq_evict_place_kernel<<<spans, block, 0, st>>>(a);
+    HC_HIP(ctx, hipGetLastError());
     return HC_OK;
 }
