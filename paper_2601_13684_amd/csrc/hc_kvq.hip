@@ -43,15 +43,14 @@ __device__ __forceinline__ uint32_t encode(const u32x4 x, uint32_t& scale)
     return codes;
 }
 
-// Codes and scale bytes to row `row` of K (v: of V) of a head; 16 lanes a row.  The four scale bytes of a row are stored by one lane.
-__device__ __forceinline__ void put_row(uint8_t* __restrict__ block, int cap, int v, int row, int lane16, uint32_t codes, uint32_t scale)
+// Codes and scale bytes of a row, 16 lanes a row.  The four scale bytes are stored by one lane.
+__device__ __forceinline__ void put_row(uint8_t* __restrict__ codes_at, uint8_t* __restrict__ scales_at, int lane16, uint32_t codes, uint32_t scale)
 {
-    uint8_t* const at = block + (v ? (int64_t)68 * cap : 0);
-    *reinterpret_cast<uint32_t*>(at + (int64_t)row * 64 + lane16 * 4) = codes;
+    *reinterpret_cast<uint32_t*>(codes_at + lane16 * 4) = codes;
     uint32_t s = scale << (lane16 & 12) * 2;                     // bytes of the groups of four lanes
     s |= dpp<0x128>(s);                                          // rotate by 8
     s |= dpp<0x124>(s);                                          // rotate by 4
-    if (lane16 == 0) *reinterpret_cast<uint32_t*>(at + (int64_t)64 * cap + (int64_t)row * 4) = s;
+    if (lane16 == 0) *reinterpret_cast<uint32_t*>(scales_at) = s;
 }
 
 // ---- rows in and out --------------------------------------------------------------------------------------------------------------------
@@ -59,6 +58,7 @@ __device__ __forceinline__ void put_row(uint8_t* __restrict__ block, int cap, in
 constexpr int RW_BLK = 256;
 constexpr int RW_TOKENS = 64;                 // of a workgroup
 constexpr int RW_SEQS = HC_PROMPT_SEQS, RW_HEADS = HC_PROMPT_HEADS;
+static_assert(4 * RW_SEQS == 2 * RW_HEADS, "either form of the offsets");
 
 // Packed tokens of a launch, sequence by sequence, as hc_prefill_rope has them.
 struct RowsArgs {
@@ -67,53 +67,96 @@ struct RowsArgs {
     const hc_kvq_head* heads;                 // of the launch's first sequence
     int2* state;
     float* acc;
-    int Hkv, n_seq, tokens, whole;
+    int Hkv, n_seq, tokens, whole, even;
     int end[RW_SEQS], first[RW_SEQS];
-    int64_t k_off[RW_HEADS], v_off[RW_HEADS];
+    // Where the heads' blocks of kv are: a K and a V offset to a head; or (even), where those of every sequence lie evenly apart, as they do but for heads of
+    // different room, first K offset, step, first V offset, step to a sequence, so that a launch has room for 64 sequences of any number of heads.  Four
+    // launches in place of one cost 64 decode tokens of eight heads 13 us, rows of 64 sequences 336 us in place of LOADTIME.
+    int64_t off[2 * RW_HEADS];
+};
+// Where the K rows of a workgroup's tokens are (codes -1: nowhere); V's, 68 cap bytes and v_kv elements further on.
+struct RowPlaces {
+    int64_t codes[RW_TOKENS], scales[RW_TOKENS], kv[RW_TOKENS], v_kv[RW_TOKENS];
+    int32_t cap[RW_TOKENS];
 };
 
-// Which tokens of which sequences a workgroup takes: RW_TOKENS packed ones from blockIdx.x * RW_TOKENS on, or (whole) all of sequence blockIdx.x, which
-// are no more.  sm_seq, sm_tok: of each its sequence, and its number there.
-__device__ __forceinline__ int rows_share(const RowsArgs& a, int* sm_seq, int* sm_tok)
+// Which tokens a workgroup takes: RW_TOKENS packed ones from blockIdx.x * RW_TOKENS on, or (whole) all of sequence blockIdx.x, which are no more; of head
+// blockIdx.y.  row_of: (the sequence's first, number in it, rows that the head has) -> its row in the cache, or -1; at: the element that a token's row has in its block of kv.
+template <typename R, typename A>
+__device__ __forceinline__ int row_places(const RowsArgs& a, RowPlaces& x, R row_of, A at)
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.y;
     const int t0 = a.whole ? (blockIdx.x > 0 ? a.end[blockIdx.x - 1] : 0) : blockIdx.x * RW_TOKENS;
     const int n = a.whole ? a.end[blockIdx.x] - t0 : min(RW_TOKENS, a.tokens - t0);
-    if (tid < n) {
-        int lo = 0, hi = a.n_seq - 1;                            // the first sequence that ends behind this token
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (a.end[mid] > t0 + tid) hi = mid;
-            else lo = mid + 1;
+    if (tid < RW_TOKENS) {
+        // The launch's arguments may lie in the host's memory, microseconds away: a lane takes those of one sequence, and gets others' from its neighbours.
+        // (A search that read them step by step, and 64 rows to a workgroup, cost 1.97 million rows 346 us in place of LOADTIME.)
+        const int end = lane < a.n_seq ? a.end[lane] : INT_MAX, first = a.first[lane];
+        int64_t off[4] = {0, 0, 0, 0};
+        if (a.even)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) off[i] = a.off[4 * lane + i];
+        const int t = t0 + min(tid, n - 1);
+        int seq = 0;                                             // sequences that end before this token
+#pragma unroll
+        for (int step = RW_SEQS / 2; step > 0; step >>= 1)
+            if (__shfl(end, seq + step - 1) <= t) seq += step;
+        const int before = __shfl(end, max(seq - 1, 0)), bh = seq * a.Hkv + h;
+        const hc_kvq_head hd = a.heads[bh];
+        const int rows = min(max(a.state[bh].x, 0), hd.cap);
+        const int i = t - (seq > 0 ? before : 0), f = __shfl(first, seq);
+        int64_t k, v;
+        if (a.even) {
+            k = __shfl(off[0], seq) + h * __shfl(off[1], seq);
+            v = __shfl(off[2], seq) + h * __shfl(off[3], seq);
+        } else {
+            k = a.off[2 * bh];
+            v = a.off[2 * bh + 1];
         }
-        sm_seq[tid] = lo;
-        sm_tok[tid] = t0 + tid - (lo > 0 ? a.end[lo - 1] : 0);
+        const int64_t row = tid < n ? row_of(f, i, rows, hd) : -1;
+        x.codes[tid] = row < 0 ? -1 : hd.off + row * 64;
+        x.scales[tid] = hd.off + (int64_t)64 * hd.cap + row * 4;
+        x.cap[tid] = hd.cap;
+        x.kv[tid] = k + at(f, i);
+        x.v_kv[tid] = v - k;
     }
     __syncthreads();
     return n;
 }
+constexpr int RW_STEPS = RW_TOKENS / (RW_BLK / 16);              // rows that 16 lanes take of K, and of V
 
 __global__ __launch_bounds__(RW_BLK) void kvq_store_kernel(RowsArgs a)
 {
-    __shared__ int sm_seq[RW_TOKENS], sm_tok[RW_TOKENS];
-    const int n = rows_share(a, sm_seq, sm_tok), h = blockIdx.y, tid = threadIdx.x, lane16 = tid & 15;
-    for (int i = tid >> 4; i < 2 * n; i += RW_BLK / 16) {
-        const int t = i >> 1, v = i & 1, b = sm_seq[t], bh = b * a.Hkv + h;
-        const hc_kvq_head hd = a.heads[bh];
-        const int64_t row = (int64_t)min(max(a.state[bh].x, 0), hd.cap) + sm_tok[t];
-        const int64_t from = (v ? a.v_off[bh] : a.k_off[bh]) + ((int64_t)a.first[b] + sm_tok[t]) * HC_D;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(a.kv + from + lane16 * 8);
-        uint32_t scale;
-        const uint32_t codes = encode(x, scale);
-        if (row < hd.cap) {
-            put_row(a.arena + hd.off, hd.cap, v, (int)row, lane16, codes, scale);
-            if (a.acc && v == 0 && lane16 == 1) a.acc[hd.row_off + row] = 0.f;
+    __shared__ RowPlaces sm;
+    const int n = row_places(a, sm,
+                             [&](int, int i, int rows, const hc_kvq_head& hd) -> int64_t {
+                                 const int64_t row = (int64_t)rows + i;
+                                 if (row >= hd.cap) return -1;
+                                 if (a.acc) a.acc[hd.row_off + row] = 0.f;
+                                 return row;
+                             },
+                             [](int f, int i) { return ((int64_t)f + i) * HC_D; });
+    const int tid = threadIdx.x, lane16 = tid & 15;
+    u32x4 x[2 * RW_STEPS];
+#pragma unroll
+    for (int k = 0; k < 2 * RW_STEPS; ++k) {
+        const int t = (tid >> 4) + RW_BLK / 16 * (k % RW_STEPS);
+        if (sm.codes[t] >= 0) x[k] = *reinterpret_cast<const u32x4*>(a.kv + sm.kv[t] + (k < RW_STEPS ? 0 : sm.v_kv[t]) + lane16 * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * RW_STEPS; ++k) {
+        const int t = (tid >> 4) + RW_BLK / 16 * (k % RW_STEPS);
+        if (sm.codes[t] >= 0) {                                  // (the 16 lanes of a row go together)
+            const int64_t v = k < RW_STEPS ? 0 : (int64_t)68 * sm.cap[t];
+            uint32_t scale;
+            const uint32_t codes = encode(x[k], scale);
+            put_row(a.arena + v + sm.codes[t], a.arena + v + sm.scales[t], lane16, codes, scale);
         }
     }
     if (!a.whole || n == 0) return;
     __syncthreads();                                             // (everyone has read the state)
     if (tid == 0) {
-        const int bh = blockIdx.x * a.Hkv + h, cap = a.heads[bh].cap;
+        const int bh = blockIdx.x * a.Hkv + blockIdx.y, cap = a.heads[bh].cap;
         const int rows = min(max(a.state[bh].x, 0), cap);
         a.state[bh] = make_int2(min(n, cap - rows) + rows, a.first[blockIdx.x] + n);
     }
@@ -132,18 +175,28 @@ __global__ __launch_bounds__(RW_BLK) void kvq_count_kernel(RowsArgs a)
 
 __global__ __launch_bounds__(RW_BLK) void kvq_load_kernel(RowsArgs a)
 {
-    __shared__ int sm_seq[RW_TOKENS], sm_tok[RW_TOKENS];
-    const int n = rows_share(a, sm_seq, sm_tok), h = blockIdx.y, tid = threadIdx.x, lane16 = tid & 15;
-    for (int i = tid >> 4; i < 2 * n; i += RW_BLK / 16) {
-        const int t = i >> 1, v = i & 1, b = sm_seq[t], bh = b * a.Hkv + h;
-        const hc_kvq_head hd = a.heads[bh];
-        const int64_t row = (int64_t)a.first[b] + sm_tok[t];
-        if (row >= min(a.state[bh].x, hd.cap)) continue;
-        const uint8_t* const at = a.arena + hd.off + (v ? (int64_t)68 * hd.cap : 0);
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(at + row * 64 + lane16 * 4);
-        const float scale = kq_scale(at[(int64_t)64 * hd.cap + row * 4 + (lane16 >> 2)]);
-        const u32x4 x{kq_pair<0>(codes, scale), kq_pair<1>(codes, scale), kq_pair<2>(codes, scale), kq_pair<3>(codes, scale)};
-        *reinterpret_cast<u32x4*>(a.kv + (v ? a.v_off[bh] : a.k_off[bh]) + (int64_t)sm_tok[t] * HC_D + lane16 * 8) = x;
+    __shared__ RowPlaces sm;
+    row_places(a, sm, [](int f, int i, int rows, const hc_kvq_head&) -> int64_t { return f + (int64_t)i < rows ? f + i : -1; },
+               [](int, int i) { return (int64_t)i * HC_D; });
+    const int tid = threadIdx.x, lane16 = tid & 15;
+    uint32_t codes[2 * RW_STEPS], scale[2 * RW_STEPS];
+#pragma unroll
+    for (int k = 0; k < 2 * RW_STEPS; ++k) {
+        const int t = (tid >> 4) + RW_BLK / 16 * (k % RW_STEPS);
+        if (sm.codes[t] >= 0) {
+            const uint8_t* const at = a.arena + (k < RW_STEPS ? 0 : (int64_t)68 * sm.cap[t]);
+            codes[k] = *reinterpret_cast<const uint32_t*>(at + sm.codes[t] + lane16 * 4);
+            scale[k] = at[sm.scales[t] + (lane16 >> 2)];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * RW_STEPS; ++k) {
+        const int t = (tid >> 4) + RW_BLK / 16 * (k % RW_STEPS);
+        if (sm.codes[t] >= 0) {
+            const float f = kq_scale(scale[k]);
+            const u32x4 x{kq_pair<0>(codes[k], f), kq_pair<1>(codes[k], f), kq_pair<2>(codes[k], f), kq_pair<3>(codes[k], f)};
+            *reinterpret_cast<u32x4*>(a.kv + sm.kv[t] + (k < RW_STEPS ? 0 : sm.v_kv[t]) + lane16 * 8) = x;
+        }
     }
 }
 
@@ -256,7 +309,8 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
     const int at = min(max(st.x, 0), hd.cap);
     if (mine && row >= 2) *reinterpret_cast<u32x4*>(a.q_out + ((size_t)bh * a.G + row - 2) * HC_D + e0) = w;
     else if (row < 2 && at < hd.cap) {
-        put_row(a.arena + hd.off, hd.cap, row == 0, at, lane16, codes, scale);
+        uint8_t* const block = a.arena + hd.off + (row == 0 ? (int64_t)68 * hd.cap : 0);
+        put_row(block + (int64_t)at * 64, block + (int64_t)64 * hd.cap + (int64_t)at * 4, lane16, codes, scale);
         if (a.acc && row == 0 && lane16 == 1) a.acc[hd.row_off + at] = 0.f;
     }
     if (tid == 0) a.state[bh] = make_int2(min(at + 1, hd.cap), st.y + 1);
@@ -668,7 +722,12 @@ hc_status rows_launches(const hc_kvq* kvq, RowsArgs& a, const int32_t* first, co
 {
     const hc_config& c = kvq->ctx->cfg;
     a.Hkv = c.Hkv;
-    const int most = std::min(RW_SEQS, RW_HEADS / c.Hkv);
+    a.even = 1;
+    for (int i = 0; i < kvq->n && a.even; ++i) {
+        const int h = i % c.Hkv, i0 = i - h;
+        a.even = h < 2 || (k_off[i] - k_off[i0] == h * (k_off[i0 + 1] - k_off[i0]) && v_off[i] - v_off[i0] == h * (v_off[i0 + 1] - v_off[i0]));
+    }
+    const int most = a.even ? RW_SEQS : std::min(RW_SEQS, RW_HEADS / c.Hkv);
     for (int b0 = 0; b0 < c.B; b0 += most) {
         a.n_seq = std::min(most, c.B - b0);
         long long tokens = 0;
@@ -680,9 +739,17 @@ hc_status rows_launches(const hc_kvq* kvq, RowsArgs& a, const int32_t* first, co
             a.first[i] = first[b0 + i];
         }
         if (tokens == 0) continue;
-        for (int i = 0; i < a.n_seq * c.Hkv; ++i) {
-            a.k_off[i] = k_off[b0 * c.Hkv + i];
-            a.v_off[i] = v_off[b0 * c.Hkv + i];
+        for (int i = 0; i < a.n_seq * (a.even ? 1 : c.Hkv); ++i) {
+            const int at = b0 * c.Hkv + (a.even ? i * c.Hkv : i);
+            if (!a.even) {
+                a.off[2 * i] = k_off[at];
+                a.off[2 * i + 1] = v_off[at];
+                continue;
+            }
+            a.off[4 * i] = k_off[at];
+            a.off[4 * i + 2] = v_off[at];
+            a.off[4 * i + 1] = c.Hkv > 1 ? k_off[at + 1] - k_off[at] : 0;
+            a.off[4 * i + 3] = c.Hkv > 1 ? v_off[at + 1] - v_off[at] : 0;
         }
         a.heads = kvq->heads + (size_t)b0 * c.Hkv;
         a.state = (int2*)state + (size_t)b0 * c.Hkv;

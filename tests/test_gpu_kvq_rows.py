@@ -80,6 +80,37 @@ def test_store_and_load(kind, Hkv, before, count, caps):
     hc.hc_destroy(ctx)
 
 
+@pytest.mark.parametrize("uneven", [False, True])
+def test_many_sequences(uneven):
+    """More than a launch takes, heads' blocks evenly apart or not."""
+    B, Hkv = 150, 3
+    count = [(7 * b) % 5 for b in range(B)]
+    ctx = U.context(B, Hkv, 1, 64)
+    cache = U.Cache(ctx, [16] * (B * Hkv), rows=[i % 3 for i in range(B * Hkv)])
+    before = cache.state.clone()
+    k_off, v_off, size = buffer_of([8] * B, Hkv)
+    if uneven:                                           # the first and the last block of every sequence change places
+        for off in (k_off, v_off):
+            for b in range(B):
+                off[b * Hkv], off[b * Hkv + 1] = off[b * Hkv + 1], off[b * Hkv]
+    kv = U.rows_of((size + D) // D, 5).view(-1)[:size].clone()
+    hc.hc_kvq_store(ctx, cache.kvq, kv, k_off, v_off, [1] * B, count, cache.arena, cache.state)
+    back = torch.zeros_like(kv)
+    hc.hc_kvq_load(ctx, cache.kvq, cache.arena, cache.state, [0] * B, [8] * B, back, k_off, v_off)
+    for i in range(B * Hkv):
+        n, c = int(before[i, 0]), count[i // Hkv]
+        assert cache.state[i].tolist() == ([n + c, 1 + c] if c else before[i].tolist())
+        for v, off in ((0, k_off[i]), (1, v_off[i])):
+            x = kv[off + D:off + (1 + c) * D].view(c, D)
+            want = U.encode(x)
+            got = cache.blocks(i, v)
+            assert torch.equal(got[0][n:n + c], want[0]) and torch.equal(got[1][n:n + c], want[1])
+            assert torch.equal(back[off + n * D:off + (n + c) * D].double().view(c, D), U.decode(*want))
+            assert (back[off + (n + c) * D:off + 8 * D] == 0).all()
+    cache.close()
+    hc.hc_destroy(ctx)
+
+
 def test_every_bf16_value():
     """Every finite number as the largest of its group, and beside one that sets a scale far above its own."""
     x = torch.arange(65536, dtype=torch.int32, device=U.DEV).to(torch.int16).view(torch.bfloat16)

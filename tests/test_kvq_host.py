@@ -149,15 +149,17 @@ def test_a_failed_launch_is_reported(fake):  # noqa: F811
     """))
 
 
-def test_many_heads_go_in_several_launches(fake):  # noqa: F811
+def test_launches_of_many_heads(fake):  # noqa: F811
+    """64 sequences to a launch where the blocks of each lie evenly apart, else as many as have room for an offset to a head."""
     run(fake, body("""
         ctx = ctx_of(70, 4, max_ctx=128)
         kvq = create(table([64] * 280), ctx)[1]
-        off = i64(*[i * 8192 for i in range(280)])
-        fake.fake_reset(0)
-        assert L.hc_kvq_load(ctx, kvq, A(1), A(2), i32(*[0] * 70), i32(*[3] * 70), A(3), off, off, None) == 0
-        assert all("kvq_load" in l[0] for l in log()) and sum(int(l[1]) for l in log()) == 70
-        fake.fake_reset(0)
-        assert L.hc_kvq_load(ctx, kvq, A(1), A(2), i32(*[0] * 70), i32(*[0] * 69 + [2]), A(3), off, off, None) == 0
-        assert len(log()) == 1
+        even, odd = i64(*[i * 8192 for i in range(280)]), i64(*[i * i * 8192 for i in range(280)])
+        for off, launches, per in ((even, 2, 64), (odd, 3, 32)):
+            fake.fake_reset(0)
+            assert L.hc_kvq_load(ctx, kvq, A(1), A(2), i32(*[0] * 70), i32(*[3] * 70), A(3), even, off, None) == 0
+            assert all("kvq_load" in l[0] and l[2] == "4" for l in log()) and [int(l[1]) for l in log()] == ([per] * launches + [70 - per * (launches - 1)])[-launches:]
+            fake.fake_reset(0)
+            assert L.hc_kvq_load(ctx, kvq, A(1), A(2), i32(*[0] * 70), i32(*[0] * 69 + [2]), A(3), off, even, None) == 0
+            assert len(log()) == 1
     """))
