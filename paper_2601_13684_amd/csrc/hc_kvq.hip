@@ -391,19 +391,27 @@ __device__ __forceinline__ Keep keep_of(const hc_kvq_head& from, const hc_kvq_he
     return x;
 }
 
-// Row i of a head's block to row j of another, with its weight: 4 lanes of 16 bytes to a row's codes.
-__device__ __forceinline__ void move_row(const uint8_t* __restrict__ src, const hc_kvq_head& from, int64_t i, uint8_t* __restrict__ dst, const hc_kvq_head& to, int64_t j,
-                                         int part, const float* __restrict__ acc, float* __restrict__ to_acc)
+// A row of a head's block, as the four lanes that move it hold it: 16 bytes of codes of K and V each, and of lane 0 K's scales, of lane 1 V's, of lane 2 the
+// weight.
+struct MovedRow {
+    u32x4 k, v;
+    uint32_t more;
+};
+__device__ __forceinline__ MovedRow take_row(const uint8_t* src, const hc_kvq_head& from, int64_t i, int part, const float* acc)
 {
-    const u32x4 k = *reinterpret_cast<const u32x4*>(src + i * 64 + part * 16);
-    const u32x4 v = *reinterpret_cast<const u32x4*>(src + (int64_t)68 * from.cap + i * 64 + part * 16);
-    uint32_t more = 0;
-    if (part < 2) more = *reinterpret_cast<const uint32_t*>(src + (int64_t)(part == 0 ? 64 : 132) * from.cap + i * 4);
-    if (part == 2) more = __float_as_uint(acc[from.row_off + i]);
-    *reinterpret_cast<u32x4*>(dst + j * 64 + part * 16) = k;
-    *reinterpret_cast<u32x4*>(dst + (int64_t)68 * to.cap + j * 64 + part * 16) = v;
-    if (part < 2) *reinterpret_cast<uint32_t*>(dst + (int64_t)(part == 0 ? 64 : 132) * to.cap + j * 4) = more;
-    if (part == 2) to_acc[to.row_off + j] = __uint_as_float(more);
+    MovedRow r;
+    r.k = *reinterpret_cast<const u32x4*>(src + i * 64 + part * 16);
+    r.v = *reinterpret_cast<const u32x4*>(src + (int64_t)68 * from.cap + i * 64 + part * 16);
+    r.more = 0;
+    if (part < 3)
+        r.more = *reinterpret_cast<const uint32_t*>(part < 2 ? src + (int64_t)(part == 0 ? 64 : 132) * from.cap + i * 4 : (const uint8_t*)(acc + from.row_off + i));
+    return r;
+}
+__device__ __forceinline__ void put_row(const MovedRow& r, uint8_t* dst, const hc_kvq_head& to, int64_t j, int part, float* to_acc)
+{
+    *reinterpret_cast<u32x4*>(dst + j * 64 + part * 16) = r.k;
+    *reinterpret_cast<u32x4*>(dst + (int64_t)68 * to.cap + j * 64 + part * 16) = r.v;
+    if (part < 3) *reinterpret_cast<uint32_t*>(part < 2 ? dst + (int64_t)(part == 0 ? 64 : 132) * to.cap + j * 4 : (uint8_t*)(to_acc + to.row_off + j)) = r.more;
 }
 
 constexpr int EV_BLK = 1024, EV_WAVES = EV_BLK / 64;
@@ -678,10 +686,19 @@ __global__ __launch_bounds__(SP_BLK) void kvq_evict_place_kernel(EvictArgs a)
     const uint8_t* const src = a.arena + from.off;
     uint8_t* const dst = a.to_arena + to.off;
     const int part = tid & 3;
-#pragma unroll 2
-    for (int q = tid >> 2; q < count; q += SP_BLK / 4) {
-        const int64_t i = span.y + sm_list[q], j = at + q;
-        move_row(src, from, i, dst, to, j, part, a.acc, a.to_acc);
+    constexpr int AT_ONCE = 4;
+    for (int q0 = 0; q0 < count; q0 += AT_ONCE * SP_BLK / 4) {
+        MovedRow r[AT_ONCE];
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const int q = q0 + e * SP_BLK / 4 + (tid >> 2);
+            if (q < count) r[e] = take_row(src, from, span.y + sm_list[q], part, a.acc);
+        }
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const int q = q0 + e * SP_BLK / 4 + (tid >> 2);
+            if (q < count) put_row(r[e], dst, to, at + q, part, a.to_acc);
+        }
     }
 }
 
@@ -694,7 +711,8 @@ __global__ __launch_bounds__(MV_BLK) void kvq_move_kernel(EvictArgs a)
     const int m = a.to_state[bh].x, j = blockIdx.x * MV_ROWS + (tid >> 2);
     if (j >= m) return;
     const hc_kvq_head from = a.heads[bh], to = a.to[bh];
-    move_row(a.arena + from.off, from, a.list[(a.list_is_to ? to.row_off : from.row_off) + j], a.to_arena + to.off, to, j, tid & 3, a.acc, a.to_acc);
+    const MovedRow r = take_row(a.arena + from.off, from, a.list[(a.list_is_to ? to.row_off : from.row_off) + j], tid & 3, a.acc);
+    put_row(r, a.to_arena + to.off, to, j, tid & 3, a.to_acc);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------------
