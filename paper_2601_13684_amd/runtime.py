@@ -410,6 +410,101 @@ class Prompt:
         return qr, out, lse
 
 
+class QuantTable:
+    """Where the heads of a cache held in 4 bits are: room[i] rows (rounded up to 16) for every (sequence, KV head), one after the other.  budget, sink, recent: what
+    ``QuantCache.evict`` leaves of a cache that it brings to this table.  One table serves the caches of all layers that are laid out alike; it has to outlive them."""
+
+    def __init__(self, ctx: Context, room: List[int], budget: Optional[List[int]] = None, sink: int = 0, recent: int = 0):
+        n = ctx.cfg.B * ctx.cfg.Hkv
+        if len(room) != n or (budget is not None and len(budget) != n):
+            raise ValueError(f"room and budget have a number a sequence and KV head, {n} of them")
+        self.ctx, self.room = ctx, [max(16, (int(r) + 15) // 16 * 16) for r in room]
+        self.heads, self.nbytes, self.rows = [], 0, 0
+        for i, cap in enumerate(self.room):
+            self.heads.append(hc.hc_kvq_head(off=self.nbytes, row_off=self.rows, cap=cap, budget=cap if budget is None else budget[i], sink=sink, recent=recent))
+            self.nbytes += (136 * cap + 63) // 64 * 64
+            self.rows += cap
+        with torch.cuda.device(ctx.device):
+            self.handle = hc.hc_kvq_create(ctx.handle, self.heads)
+
+    def work_bytes(self) -> int:
+        return hc.hc_kvq_work_bytes(self.ctx.handle, self.handle)
+
+    def close(self):
+        if self.handle:
+            hc.hc_kvq_destroy(self.handle)
+            self.handle = None
+
+
+class QuantCache:
+    """One layer's cache held in 4 bits: bytes, rows and positions of its heads on the device, with ``weights`` the attention that every row has drawn, and the
+    work buffer of attention and eviction (``work``: another's, of at least the table's work_bytes, where their calls do not overlap).  Its calls may be put on any
+    stream; on different streams they are put in order by the caller."""
+
+    def __init__(self, table: QuantTable, weights: bool = True, work: Optional[torch.Tensor] = None):
+        self.ctx, self.table = table.ctx, table
+        dev = self.ctx.device
+        self.arena = torch.zeros((table.nbytes,), dtype=torch.uint8, device=dev)
+        self.state = torch.zeros((len(table.heads), 2), dtype=torch.int32, device=dev)
+        self.acc = torch.zeros((table.rows,), dtype=torch.float32, device=dev) if weights else None
+        self.work = torch.empty((table.work_bytes(),), dtype=torch.uint8, device=dev) if work is None else work
+        self._own = [self.arena, self.state] + ([] if self.acc is None else [self.acc]) + ([self.work] if work is None else [])
+        self.made = _Made(dev)
+
+    def _used_on(self, stream) -> None:
+        self.made.used_on(stream, *self._own)
+
+    def store(self, prompt: Prompt, first: List[int], count: List[int], stream=None) -> None:
+        """Rows first[b] .. of every sequence of the prompt's buffer, count[b] of them, behind what the cache holds (hc_kvq_store)."""
+        if any(f < 0 or c < 0 or f + c > n for f, c, n in zip(first, count, prompt.length)):
+            raise ValueError("the prompt does not have these rows")
+        self._used_on(stream)
+        prompt.made.used_on(stream, prompt.kv)
+        hc.hc_kvq_store(self.ctx.handle, self.table.handle, prompt.kv, prompt.k_off, prompt.v_off, first, count, self.arena, self.state, self.acc, stream)
+
+    def load(self, first: List[int], count: List[int], kv_out: torch.Tensor, k_off, v_off, stream=None) -> None:
+        """Rows as bf16 (hc_kvq_load)."""
+        self._used_on(stream)
+        hc.hc_kvq_load(self.ctx.handle, self.table.handle, self.arena, self.state, first, count, kv_out, k_off, v_off, stream)
+
+    def append_rope(self, rope: hc.hc_rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+        """The decode token's projected heads, as LayerRuntime.append_rope takes them (hc_kvq_append).  Returns the queries for ``attn``."""
+        if q_out is None:
+            with _on(stream, self.ctx.device):
+                q_out = torch.empty((self.ctx.cfg.B, self.ctx.cfg.Hq, D), dtype=torch.bfloat16, device=self.ctx.device)
+        self._used_on(stream)
+        hc.hc_kvq_append(self.ctx.handle, self.table.handle, rope, q, k, v, q_out, self.arena, self.state, self.acc, stream)
+        return q_out
+
+    def attn(self, q: torch.Tensor, decay: float = 1.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
+        """Attention of the decode token (hc_kvq_attn); every row's weights are added to what it has drawn, times ``decay``.  Returns (out [B, Hq, D], lse
+        [B, Hq]), f32."""
+        cfg = self.ctx.cfg
+        with _on(stream, self.ctx.device):
+            if out is None:
+                out = torch.empty((cfg.B, cfg.Hq, D), dtype=torch.float32, device=self.ctx.device)
+            if lse is None:
+                lse = torch.empty((cfg.B, cfg.Hq), dtype=torch.float32, device=self.ctx.device)
+        self._used_on(stream)
+        hc.hc_kvq_attn(self.ctx.handle, self.table.handle, self.arena, self.state, q, out, lse, self.acc, decay, self.work, self.work.numel(), stream)
+        return out, lse
+
+    def evict(self, to: "QuantCache", kept: Optional[torch.Tensor] = None, stream=None) -> None:
+        """This cache's heads to the budgets of another's table, into it; what it held is given up (hc_kvq_evict).  kept (int32 [to.table.rows]): which rows
+        they were."""
+        if self.acc is None or to.acc is None:
+            raise ValueError("eviction goes by the rows' weights: both caches need them")
+        self._used_on(stream)
+        to._used_on(stream)
+        hc.hc_kvq_evict(self.ctx.handle, self.table.handle, self.arena, self.state, self.acc, to.table.handle, to.arena, to.state, to.acc, kept, self.work,
+                        self.work.numel(), stream)
+
+    def rows(self) -> List[int]:
+        """How many rows every head holds (waits for the device)."""
+        return self.state[:, 0].tolist()
+
+
 class _DeviceInts:
     """n int32 at a raw device address, in the form torch.as_tensor understands."""
 
