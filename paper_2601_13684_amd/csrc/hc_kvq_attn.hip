@@ -73,7 +73,7 @@ __device__ __forceinline__ float sum_parts(float x)
 // of a phase of the reads (one chunk of 16 rows) go over all banks; the scales of row 4 x + y are at place 8 y + x, so that the eight that a lane takes for V
 // lie side by side.
 constexpr int T_V = 2048, T_KS = 4096, T_VS = T_KS + 128, T_BYTES = T_VS + 128;
-constexpr int KA_BUFS = 4, T_STEP = KA_WAVES * T_BYTES;
+constexpr int KA_BUFS = 4;                   // of a wave, one after the other
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -103,238 +103,204 @@ __device__ __forceinline__ void read_tile(Tile& x, uint32_t k_at, uint32_t s_at,
         "ds_read_b128 %9, %13 offset:%28\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x.k[0]), "=&v"(x.k[1]), "=&v"(x.ks[0]), "=&v"(x.ks[1]), "=&v"(x.v[0]), "=&v"(x.v[1]), "=&v"(x.v[2]), "=&v"(x.v[3]), "=&v"(x.vs[0]), "=&v"(x.vs[1])
-        : "v"(k_at), "v"(s_at), "v"(v_at), "v"(f_at), "n"(later), "n"(BUF * T_STEP), "n"(BUF * T_STEP + 1024), "n"(BUF * T_STEP + T_KS),
-          "n"(BUF * T_STEP + T_KS + 16), "n"((BUF * T_STEP + T_V) / 256), "n"((BUF * T_STEP + T_V) / 256 + 1), "n"((BUF * T_STEP + T_V) / 256 + 2),
-          "n"((BUF * T_STEP + T_V) / 256 + 3), "n"((BUF * T_STEP + T_V) / 256 + 4), "n"((BUF * T_STEP + T_V) / 256 + 5), "n"((BUF * T_STEP + T_V) / 256 + 6),
-          "n"((BUF * T_STEP + T_V) / 256 + 7), "n"(BUF * T_STEP + T_VS), "n"(BUF * T_STEP + T_VS + 16)
+        : "v"(k_at), "v"(s_at), "v"(v_at), "v"(f_at), "n"(later), "n"(BUF * T_BYTES), "n"(BUF * T_BYTES + 1024), "n"(BUF * T_BYTES + T_KS),
+          "n"(BUF * T_BYTES + T_KS + 16), "n"((BUF * T_BYTES + T_V) / 256), "n"((BUF * T_BYTES + T_V) / 256 + 1), "n"((BUF * T_BYTES + T_V) / 256 + 2),
+          "n"((BUF * T_BYTES + T_V) / 256 + 3), "n"((BUF * T_BYTES + T_V) / 256 + 4), "n"((BUF * T_BYTES + T_V) / 256 + 5), "n"((BUF * T_BYTES + T_V) / 256 + 6),
+          "n"((BUF * T_BYTES + T_V) / 256 + 7), "n"(BUF * T_BYTES + T_VS), "n"(BUF * T_BYTES + T_VS + 16)
         : "memory");
 }
-static_assert(T_STEP % 256 == 0 && T_V % 256 == 0 && (KA_BUFS * T_STEP) / 256 <= 272, "offsets of the reads");
+static_assert(T_BYTES % 256 == 0 && T_V % 256 == 0 && KA_BUFS * T_BYTES / 256 < 256, "offsets of the reads");
 
-template <int G, bool LOGITS>
-__global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
-{
-    __shared__ float sm_ml[KA_WAVES][G][2];
-    __shared__ __attribute__((aligned(256))) char sm_tile[KA_BUFS][KA_WAVES][T_BYTES];
-    static_assert(G * HC_D * sizeof(float) <= T_BYTES, "a wave's sums go through its first buffer");
-    auto sm_o = [&](int wave, int g) { return reinterpret_cast<float*>(&sm_tile[0][wave][0]) + g * HC_D; };
-    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
+// One wave's part of a head: what it has of its queries and sums, and where its tiles go.
+template <int G>
+struct Wave {
+    int lane, col, grp;
+    int part;                                // of the weights that this column takes
+    bool dead;
+    uint32_t m1, m2;
+    float cs;
+    lds_char* lds;
+    uint32_t k_read, s_read, v_read, f_read; // what the lane reads of a tile: K's rows 16 s + 4 (col % 4) + col / 4 and V's 4 i + grp
+    const uint8_t* block;                    // the head's
+    uint32_t cap, k_at, v_at, s_at, k_chunk, v_chunk, s_base;
+    int n, c_row, s_row;
+    bf16x8 Q[4];
+    float ref, l;                            // weights are 2^(t - ref)
+    f32x4 O[8];
 
-    // this workgroup's share, and the head that it begins in
-    const int each = (a.n + 63) / 64, mine0 = min(a.n, lane * each), mine1 = min(a.n, mine0 + each);
-    int sum = 0;
-    for (int i = mine0; i < mine1; ++i) sum += places_of(kq_rows(a.state, a.room, i));
-    int upto = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
+    __device__ __forceinline__ explicit Wave(char* tiles)
+    {
+        lane = threadIdx.x & 63;
+        col = lane & 15;
+        grp = lane >> 4;
+        part = G <= 4 ? col / G : col / 8;
+        dead = part > 2;
+        m1 = part >= 1 ? 0xffff0000u : 0u;
+        m2 = part >= 2 ? 0xffff0000u : 0u;
+        cs = dead ? 0.f : KA_SCALE;
+        lds = (lds_char*)tiles;
+        const uint32_t tile0 = (uint32_t)(uintptr_t)lds;
+        k_read = tile0 + (4 * (col & 3) + (col >> 2)) * 64 + (grp ^ (col & 3)) * 16;
+        s_read = tile0 + (8 * (col >> 2) + (col & 3)) * 4 + grp;
+        v_read = tile0 + lane * 4;
+        f_read = tile0 + grp * 32;
+        asm("" : "+v"(k_read), "+v"(s_read), "+v"(v_read), "+v"(f_read));      // (opaque, so that a buffer goes into an instruction's offset)
+        // what it loads: 16 bytes of codes of row lane / 4, and the scales of row 4 (lane % 8) + lane / 8 % 4, K's or V's
+        c_row = lane >> 2;
+        s_row = 4 * (lane & 7) + (lane >> 3 & 3);
+        k_chunk = ((lane & 3) ^ (lane >> 4)) * 16;
+        v_chunk = (lane & 3) * 16;
     }
-    const int total = __builtin_amdgcn_readlane(upto, 63), per = share(total, (int)gridDim.x);
-    const int u0 = (int)min((long long)total, (long long)blockIdx.x * per), u1 = min(total, u0 + per);
-    if (u0 >= u1) return;
-    const int owner = __popcll(__builtin_amdgcn_ballot_w64(upto <= u0));
-    int bh = __builtin_amdgcn_readfirstlane(owner * each), window = bh - 64;
-    int before = __builtin_amdgcn_readlane(upto - sum, owner);
-    int h_rows = 0, h_cap = 0, h_first = 0;                      // a lane's of the 64 heads from `window` on
-    int64_t h_off = 0;
-
-    const int part = G <= 4 ? col / G : col / 8;                 // of the weights that this column takes
-    const bool dead = part > 2;
-    const uint32_t m1 = part >= 1 ? 0xffff0000u : 0u, m2 = part >= 2 ? 0xffff0000u : 0u;
-    const float cs = dead ? 0.f : KA_SCALE;
-
-    // what the lane reads of a tile: K's rows 16 s + 4 (col % 4) + col / 4 and V's 4 i + grp
-    const uint32_t tile0 = (uint32_t)(uintptr_t)(lds_char*)&sm_tile[0][w][0];
-    uint32_t k_read = tile0 + (4 * (col & 3) + (col >> 2)) * 64 + (grp ^ (col & 3)) * 16, s_read = tile0 + (8 * (col >> 2) + (col & 3)) * 4 + grp;
-    uint32_t v_read = tile0 + lane * 4, f_read = tile0 + grp * 32;
-    asm("" : "+v"(k_read), "+v"(s_read), "+v"(v_read), "+v"(f_read));      // (opaque, so that a buffer goes into an instruction's offset)
-    for (; before < u1 && bh < a.n; ++bh) {
-        if (bh >= window + 64) {
-            window = bh;
-            const int i = min(bh + lane, a.n - 1);
-            const int2 room = a.room[i];
-            h_rows = min(max(a.state[i].x, 0), room.x);
-            h_cap = room.x;
-            h_first = room.y;
-            h_off = a.heads[i].off;
-        }
-        const int n = __builtin_amdgcn_readlane(h_rows, bh - window), tiles = tiles_of(n), begin = before + KA_START;
-        before += places_of(n);
-        const int t0 = max(u0 - begin, 0), t1 = min(tiles, u1 - begin);
-        if (t0 >= t1) continue;
-        const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h_off >> 32), bh - window) << 32 |
-                             (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window);
-        const uint32_t cap = __builtin_amdgcn_readlane(h_cap, bh - window);
-        const int first_tile = LOGITS ? __builtin_amdgcn_readlane(h_first, bh - window) : 0;
-        if (t0 == 0 && tid == 0) a.plan[bh] = make_int2((int)blockIdx.x + bh, (begin + tiles - 1) / per - (int)blockIdx.x + 1);
-        bf16x8 Q[4];
+    __device__ __forceinline__ void begin(const AttnArgs& a, int bh, int64_t off, uint32_t room, int rows)
+    {
+        block = a.arena + off;
+        cap = room;
+        n = rows;
+        s_base = (lane < 32 ? 64u : 132u) * cap;
+        k_at = c_row * 64 + k_chunk;
+        v_at = 68 * cap + c_row * 64 + v_chunk;
+        s_at = s_base + s_row * 4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
-        float ref = dead ? FLT_MAX : -FLT_MAX, l = 0.f;
-        f32x4 O[8];
+        ref = dead ? FLT_MAX : -FLT_MAX;
+        l = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        // a lane's places: 16 bytes of codes of row lane / 4, and the scales of row 4 (lane % 8) + lane / 8 % 4, K's or V's
-        const int c_row = lane >> 2, s_row = 4 * (lane & 7) + (lane >> 3 & 3);
-        const uint32_t k_chunk = ((lane & 3) ^ (lane >> 4)) * 16, v_chunk = (lane & 3) * 16, s_base = (lane < 32 ? 64u : 132u) * cap;
-        const uint32_t k_at = c_row * 64 + k_chunk, v_at = 68 * cap + c_row * 64 + v_chunk, s_at = s_base + s_row * 4;
-        // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
-        // 224K rows of eight heads, no logits 42.4 / 43.1, logits 53.3 / 47.6; two such heads and six short ones 16.6 / 18.2, 20.1 / 19.1.
-        static constexpr int NT = LOGITS ? 0 : 2;
-        auto load = [&](int t, auto buf) {
-            lds_char* const to = (lds_char*)&sm_tile[decltype(buf)::value][w][0];
-            // (a tile behind the last is loaded from a buffer of no bytes, which costs no memory: the number of loads on their way is then always the same)
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.arena + off), 0, t < t1 ? 136u * cap : 0u, 0x00027000);
-            const int r0 = t * KQ_TILE;
-            uint32_t k0 = k_at, k1 = k_at + 1024, v0 = v_at, v1 = v_at + 1024, s0 = s_at;
-            if (r0 + KQ_TILE > n) {                              // rows behind the last repeat it; their weights and values become zeros
-                const int last = max(n - 1 - r0, 0);
-                k0 = min(c_row, last) * 64 + k_chunk;
-                k1 = min(c_row + 16, last) * 64 + k_chunk;
-                v0 = 68 * cap + min(c_row, last) * 64 + v_chunk;
-                v1 = 68 * cap + min(c_row + 16, last) * 64 + v_chunk;
-                s0 = s_base + min(s_row, last) * 4;
+    }
+    // The queries are there: waits after this count the tiles' loads alone.
+    __device__ __forceinline__ void ready()
+    {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(Q[c]));
+    }
+    // Tile t to buffer BUF; none from `end` on.
+    template <int BUF, int NT>
+    __device__ __forceinline__ void load(int t, int end) const
+    {
+        lds_char* const to = lds + BUF * T_BYTES;
+        // (a tile behind the last is loaded from a buffer of no bytes, which costs no memory: the number of loads on their way is then always the same)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)block, 0, t < end ? 136u * cap : 0u, 0x00027000);
+        const int r0 = t * KQ_TILE;
+        uint32_t k0 = k_at, k1 = k_at + 1024, v0 = v_at, v1 = v_at + 1024, s0 = s_at;
+        if (r0 + KQ_TILE > n) {                              // rows behind the last repeat it; their weights and values become zeros
+            const int last = max(n - 1 - r0, 0);
+            k0 = min(c_row, last) * 64 + k_chunk;
+            k1 = min(c_row + 16, last) * 64 + k_chunk;
+            v0 = 68 * cap + min(c_row, last) * 64 + v_chunk;
+            v1 = 68 * cap + min(c_row + 16, last) * 64 + v_chunk;
+            s0 = s_base + min(s_row, last) * 4;
+        }
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, k0, r0 * 64, 0, NT);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 1024), 16, k1, r0 * 64, 0, NT);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_KS), 4, s0, r0 * 4, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V), 16, v0, r0 * 64, 0, NT);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V + 1024), 16, v1, r0 * 64, 0, NT);
+    }
+    // Tile t from buffer BUF, all but LATER of the wave's loads and stores having arrived; S: its logits, q . K.
+    template <int BUF, int LATER>
+    __device__ __forceinline__ void add(int t, float* logits, f32x4 (&S)[2])
+    {
+        Tile x;
+        read_tile<BUF, LATER>(x, k_read, s_read, v_read, f_read);
+        uint32_t xv[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xv[i] = x.v[i >> 1][i & 1];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            S[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const float f = kq_scale(x.ks[s]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const u32x4 k{kq_pair<0>(x.k[s][c], f), kq_pair<1>(x.k[s][c], f), kq_pair<2>(x.k[s][c], f), kq_pair<3>(x.k[s][c], f)};
+                S[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), Q[c], S[s], 0, 0, 0);
             }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, k0, r0 * 64, 0, NT);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 1024), 16, k1, r0 * 64, 0, NT);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_KS), 4, s0, r0 * 4, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V), 16, v0, r0 * 64, 0, NT);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + T_V + 1024), 16, v1, r0 * 64, 0, NT);
-        };
-        auto compute = [&](int t, auto buf) {
-            Tile x;
-            // three tiles' loads, and where logits are stored those of the three tiles before this one: not yet behind the first tiles
-            if (LOGITS && t < t0 + 3 * KA_WAVES) __builtin_amdgcn_s_waitcnt(0x0f7f);       // vmcnt(15)
-            read_tile<decltype(buf)::value, LOGITS ? 18 : 15>(x, k_read, s_read, v_read, f_read);
-            uint32_t xv[8];
+        }
+        float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) xv[i] = x.v[i >> 1][i & 1];
-            f32x4 S[2];
+        for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i >> 2][i & 3] >> (col >> 2) * 8 & 255u);
+        const int r0 = t * KQ_TILE;
+        if (logits && col < 2 * G)                           // (columns g and G + g have the same: 2 G lanes store half of the eight each)
+            *reinterpret_cast<f32x4*>(logits + ((size_t)t * 8 + 2 * grp) * G * 4 + col * 4) = col < G ? S[0] : S[1];
+        if (r0 + KQ_TILE > n) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                S[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-                const float f = kq_scale(x.ks[s]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const u32x4 k{kq_pair<0>(x.k[s][c], f), kq_pair<1>(x.k[s][c], f), kq_pair<2>(x.k[s][c], f), kq_pair<3>(x.k[s][c], f)};
-                    S[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), Q[c], S[s], 0, 0, 0);
+            for (int i = 0; i < 8; ++i)
+                if (r0 + 4 * i + grp >= n) {
+                    S[i >> 2][i & 3] = -INFINITY;
+                    xv[i] = 0;
+                    f[i] = 1.f;
                 }
+        }
+        float p[8], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+            top = fmaxf(top, p[i]);
+        }
+        if (__builtin_amdgcn_ballot_w64(top > KA_SLACK && !dead)) {
+            float y = S[0][0] * cs;
+#pragma unroll
+            for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * cs);
+            y = fmaxf(y, __shfl_xor(y, 16));
+            y = fmaxf(y, __shfl_xor(y, 32));
+            y = fmaxf(y, ref);
+            const float less = exp2f(ref - y);
+            ref = y;
+            l *= less;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) O[j] *= less;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+        }
+        uint32_t P1[8], P2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = dead ? 0.f : __builtin_amdgcn_exp2f(p[i]);
+            l += e;
+            const float r1 = e - __uint_as_float(__float_as_uint(e) & (G == 8 ? 0xffff0000u : m1));
+            if (G == 8) {
+                P1[i] = __float_as_uint(part ? r1 : e);
+                P2[i] = part ? 0u : __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u));
+            } else {
+                P1[i] = __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & m2));
             }
-            float f[8];
+        }
+        u32x4 B1, B2;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i >> 2][i & 3] >> (col >> 2) * 8 & 255u);
-            const int r0 = t * KQ_TILE;
-            if (LOGITS && col < 2 * G)                           // (columns g and G + g have the same: 2 G lanes store half of the eight each)
-                *reinterpret_cast<f32x4*>(a.logits + ((size_t)(first_tile + t) * 8 + 2 * grp) * G * 4 + col * 4) = col < G ? S[0] : S[1];
-            if (r0 + KQ_TILE > n) {
+        for (int i = 0; i < 4; ++i) {
+            B1[i] = __builtin_amdgcn_perm(P1[2 * i + 1], P1[2 * i], 0x07060302u);
+            if (G == 8) B2[i] = __builtin_amdgcn_perm(P2[2 * i + 1], P2[2 * i], 0x07060302u);
+        }
+        auto values = [&](auto byte) {
+            constexpr int B = decltype(byte)::value;
+            uint32_t c[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (r0 + 4 * i + grp >= n) {
-                        S[i >> 2][i & 3] = -INFINITY;
-                        xv[i] = 0;
-                        f[i] = 1.f;
-                    }
-            }
-            float p[8], top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
-                top = fmaxf(top, p[i]);
-            }
-            if (__builtin_amdgcn_ballot_w64(top > KA_SLACK && !dead)) {
-                float y = S[0][0] * cs;
-#pragma unroll
-                for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * cs);
-                y = fmaxf(y, __shfl_xor(y, 16));
-                y = fmaxf(y, __shfl_xor(y, 32));
-                y = fmaxf(y, ref);
-                const float less = exp2f(ref - y);
-                ref = y;
-                l *= less;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) O[j] *= less;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
-            }
-            uint32_t P1[8], P2[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = dead ? 0.f : __builtin_amdgcn_exp2f(p[i]);
-                l += e;
-                const float r1 = e - __uint_as_float(__float_as_uint(e) & (G == 8 ? 0xffff0000u : m1));
-                if (G == 8) {
-                    P1[i] = __float_as_uint(part ? r1 : e);
-                    P2[i] = part ? 0u : __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u));
-                } else {
-                    P1[i] = __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & m2));
-                }
-            }
-            u32x4 B1, B2;
+            for (int i = 0; i < 8; ++i) c[i] = kq_pair<B>(xv[i], f[i]);
+            u32x4 lo, hi;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                B1[i] = __builtin_amdgcn_perm(P1[2 * i + 1], P1[2 * i], 0x07060302u);
-                if (G == 8) B2[i] = __builtin_amdgcn_perm(P2[2 * i + 1], P2[2 * i], 0x07060302u);
+                lo[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+                hi[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
             }
-            auto values = [&](auto byte) {
-                constexpr int B = decltype(byte)::value;
-                uint32_t c[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = kq_pair<B>(xv[i], f[i]);
-                u32x4 lo, hi;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
-                    hi[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
-                }
-                O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B1), O[2 * B], 0, 0, 0);
-                O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B1), O[2 * B + 1], 0, 0, 0);
-                if (G == 8) {
-                    O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B2), O[2 * B], 0, 0, 0);
-                    O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B2), O[2 * B + 1], 0, 0, 0);
-                }
-            };
-            values(std::integral_constant<int, 0>{});
-            values(std::integral_constant<int, 1>{});
-            values(std::integral_constant<int, 2>{});
-            values(std::integral_constant<int, 3>{});
+            O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B1), O[2 * B], 0, 0, 0);
+            O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B1), O[2 * B + 1], 0, 0, 0);
+            if (G == 8) {
+                O[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, B2), O[2 * B], 0, 0, 0);
+                O[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, B2), O[2 * B + 1], 0, 0, 0);
+            }
         };
-
-        // a wave's tiles, KA_WAVES apart; while one is worked on, three are on their way
-        using B0 = std::integral_constant<int, 0>;
-        using B1 = std::integral_constant<int, 1>;
-        using B2 = std::integral_constant<int, 2>;
-        using B3 = std::integral_constant<int, 3>;
-        int t = t0 + w;
-        auto step = [&](auto buf) {
-            compute(t, buf);
-            load(t + 4 * KA_WAVES, buf);
-            t += KA_WAVES;
-        };
-#pragma unroll
-        for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(Q[c]));      // (they are there: the waits below count the tiles' loads alone)
-        load(t, B0{});
-        load(t + KA_WAVES, B1{});
-        load(t + 2 * KA_WAVES, B2{});
-        load(t + 3 * KA_WAVES, B3{});
-        while (t < t1) {
-            step(B0{});
-            if (t >= t1) break;
-            step(B1{});
-            if (t >= t1) break;
-            step(B2{});
-            if (t >= t1) break;
-            step(B3{});
-        }
-        __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): sums go through a buffer
-
-        // the parts of a weight, and the waves, together
+        values(std::integral_constant<int, 0>{});
+        values(std::integral_constant<int, 1>{});
+        values(std::integral_constant<int, 2>{});
+        values(std::integral_constant<int, 3>{});
+    }
+    // The parts of a weight, and the groups of lanes, together: to ml [G][2] and o [G][128].
+    __device__ __forceinline__ void finish(float (*ml)[2], float* o)
+    {
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (lane < G) {
-            sm_ml[w][lane][0] = ref;
-            sm_ml[w][lane][1] = l;
+            ml[lane][0] = ref;
+            ml[lane][1] = l;
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -345,11 +311,97 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                 hi[j] = sum_parts<G>(O[4 + j][r]);
             }
             if (col < G) {
-                float* const to = sm_o(w, col) + 8 * (4 * grp + r);
+                float* const to = o + col * HC_D + 8 * (4 * grp + r);
                 *reinterpret_cast<f32x4*>(to) = lo;
                 *reinterpret_cast<f32x4*>(to + 4) = hi;
             }
         }
+    }
+};
+static_assert(HC_MAX_G * HC_D * sizeof(float) <= T_BYTES, "a wave's sums go through its first buffer");
+constexpr int VMCNT0 = 0x0f70, VMCNT15 = 0x0f7f;                 // of s_waitcnt
+
+template <int G, bool LOGITS>
+__global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
+{
+    __shared__ float sm_ml[KA_WAVES][G][2];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KA_WAVES][KA_BUFS][T_BYTES];
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+
+    // this workgroup's share, and the head that it begins in
+    int window = 0, h_rows, h_cap, h_first;                      // a lane's of the 64 heads from `window` on
+    int64_t h_off;
+    auto look = [&]() {
+        const int i = min(window + lane, a.n - 1);
+        const int2 room = a.room[i];
+        h_rows = min(max(a.state[i].x, 0), room.x);
+        h_cap = room.x;
+        h_first = room.y;
+        h_off = a.heads[i].off;
+    };
+    look();
+    const int each = (a.n + 63) / 64, mine0 = min(a.n, lane * each), mine1 = min(a.n, mine0 + each);
+    int sum = 0;
+    if (each == 1) sum = lane < a.n ? places_of(h_rows) : 0;
+    else
+        for (int i = mine0; i < mine1; ++i) sum += places_of(kq_rows(a.state, a.room, i));
+    int upto = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63), per = share(total, (int)gridDim.x);
+    const int u0 = (int)min((long long)total, (long long)blockIdx.x * per), u1 = min(total, u0 + per);
+    if (u0 >= u1) return;
+    const int owner = __popcll(__builtin_amdgcn_ballot_w64(upto <= u0));
+    int bh = __builtin_amdgcn_readfirstlane(owner * each);
+    int before = __builtin_amdgcn_readlane(upto - sum, owner);
+    Wave<G> wave(&sm_tile[w][0][0]);
+    for (; before < u1 && bh < a.n; ++bh) {
+        if (bh >= window + 64) {
+            window = bh;
+            look();
+        }
+        const int n = __builtin_amdgcn_readlane(h_rows, bh - window), tiles = tiles_of(n), begin = before + KA_START;
+        before += places_of(n);
+        const int t0 = max(u0 - begin, 0), t1 = min(tiles, u1 - begin);
+        if (t0 >= t1) continue;
+        const int64_t off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h_off >> 32), bh - window) << 32 |
+                                      (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window));
+        if (t0 == 0 && tid == 0) a.plan[bh] = make_int2((int)blockIdx.x + bh, (begin + tiles - 1) / per - (int)blockIdx.x + 1);
+        wave.begin(a, bh, off, (uint32_t)__builtin_amdgcn_readlane(h_cap, bh - window), n);
+        float* const logits = LOGITS ? a.logits + (size_t)__builtin_amdgcn_readlane(h_first, bh - window) * KQ_TILE * G : nullptr;
+        // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
+        // 224K rows of eight heads, no logits 42.4 / 43.1, logits 53.3 / 47.6; two such heads and six short ones 16.6 / 18.2, 20.1 / 19.1.
+        static constexpr int NT = LOGITS ? 0 : 2;
+        // a wave's tiles, KA_WAVES apart; while one is worked on, three are on their way
+        int t = t0 + w;
+        wave.template load<0, NT>(t, t1);
+        wave.template load<1, NT>(t + KA_WAVES, t1);
+        wave.template load<2, NT>(t + 2 * KA_WAVES, t1);
+        wave.template load<3, NT>(t + 3 * KA_WAVES, t1);
+        wave.ready();
+        auto step = [&](auto buf) {
+            constexpr int BUF = decltype(buf)::value;
+            // three tiles' loads, and where logits are stored those of the three tiles before this one: not yet behind the first tiles
+            if (LOGITS && t < t0 + 3 * KA_WAVES) __builtin_amdgcn_s_waitcnt(VMCNT15);
+            f32x4 S[2];
+            wave.template add<BUF, LOGITS ? 18 : 15>(t, logits, S);
+            wave.template load<BUF, NT>(t + 4 * KA_WAVES, t1);
+            t += KA_WAVES;
+        };
+        while (t < t1) {
+            step(std::integral_constant<int, 0>{});
+            if (t >= t1) break;
+            step(std::integral_constant<int, 1>{});
+            if (t >= t1) break;
+            step(std::integral_constant<int, 2>{});
+            if (t >= t1) break;
+            step(std::integral_constant<int, 3>{});
+        }
+        __builtin_amdgcn_s_waitcnt(VMCNT0);                      // sums go through a buffer
+        wave.finish(sm_ml[w], reinterpret_cast<float*>(&sm_tile[w][0][0]));
         __syncthreads();
         const size_t slot = (size_t)blockIdx.x + bh;
         for (int i = tid; i < G * HC_D; i += KA_BLK) {
@@ -360,7 +412,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
 #pragma unroll
             for (int k = 0; k < KA_WAVES; ++k) {
                 const float f = exp2f(sm_ml[k][g][0] - m);
-                o = fmaf(f, sm_o(k, g)[d], o);
+                o = fmaf(f, reinterpret_cast<const float*>(&sm_tile[k][0][0])[i], o);
                 s = fmaf(f, sm_ml[k][g][1], s);
             }
             a.part_o[(slot * G + g) * HC_D + d] = o;
@@ -494,9 +546,100 @@ __global__ __launch_bounds__(KC_BLK) void kvq_combine_kernel(CombineArgs a)
     }
 }
 
+// ---- heads of few rows: all of one in a workgroup, and no second launch --------------------------------------------------------------------
+
+constexpr int KS_BLK = 512, KS_WAVES = KS_BLK / 64;
+constexpr int KS_ROWS = KS_WAVES * KA_BUFS * KQ_TILE;            // that a workgroup has at once: all of its loads are on their way before the first product
+
+struct ShortArgs {
+    AttnArgs a;
+    float *out, *lse, *acc;
+    float decay;
+};
+
+template <int G, bool WEIGHTS>
+__global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
+{
+    __shared__ float sm_ml[KS_WAVES][G][2], sm_all[G][2];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KS_WAVES][KA_BUFS][T_BYTES];
+    const AttnArgs& a = x.a;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), bh = blockIdx.x;
+    const int n = __builtin_amdgcn_readfirstlane(kq_rows(a.state, a.room, bh)), tiles = tiles_of(n);
+    const hc_kvq_head hd = a.heads[bh];
+    const int64_t off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(hd.off >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)hd.off));
+    Wave<G> wave(&sm_tile[w][0][0]);
+    wave.begin(a, bh, off, (uint32_t)__builtin_amdgcn_readfirstlane(hd.cap), n);
+    const int t = w;                                             // its tiles: KS_WAVES apart
+    // a lane's rows of a tile, eight of 4 i + lane / 16: lanes of columns i take row i to the table of weights
+    const int col = wave.col, row0 = 4 * (col & 7) + wave.grp;
+    float old[KA_BUFS];
+    if (WEIGHTS)
+#pragma unroll
+        for (int b = 0; b < KA_BUFS; ++b) {
+            const int r = (t + b * KS_WAVES) * KQ_TILE + row0;
+            old[b] = col < 8 && r < n ? x.acc[hd.row_off + r] : 0.f;
+        }
+    wave.template load<0, 0>(t, tiles);
+    wave.template load<1, 0>(t + KS_WAVES, tiles);
+    wave.template load<2, 0>(t + 2 * KS_WAVES, tiles);
+    wave.template load<3, 0>(t + 3 * KS_WAVES, tiles);
+    wave.ready();
+    f32x4 S[KA_BUFS][2];
+    if (t < tiles) wave.template add<0, 15>(t, nullptr, S[0]);
+    if (t + KS_WAVES < tiles) wave.template add<1, 10>(t + KS_WAVES, nullptr, S[1]);
+    if (t + 2 * KS_WAVES < tiles) wave.template add<2, 5>(t + 2 * KS_WAVES, nullptr, S[2]);
+    if (t + 3 * KS_WAVES < tiles) wave.template add<3, 0>(t + 3 * KS_WAVES, nullptr, S[3]);
+    __builtin_amdgcn_s_waitcnt(VMCNT0);                          // sums go through a buffer
+    wave.finish(sm_ml[w], reinterpret_cast<float*>(&sm_tile[w][0][0]));
+    __syncthreads();
+    for (int i = tid; i < G * HC_D; i += KS_BLK) {
+        const int g = i / HC_D;
+        float m = sm_ml[0][g][0], o = 0.f, l = 0.f;
+#pragma unroll
+        for (int k = 1; k < KS_WAVES; ++k) m = fmaxf(m, sm_ml[k][g][0]);
+#pragma unroll
+        for (int k = 0; k < KS_WAVES; ++k) {
+            const float f = exp2f(sm_ml[k][g][0] - m);
+            o = fmaf(f, reinterpret_cast<const float*>(&sm_tile[k][0][0])[i], o);
+            l = fmaf(f, sm_ml[k][g][1], l);
+        }
+        x.out[(size_t)bh * G * HC_D + i] = l == 0.f ? 0.f : o / l;       // (no rows: nothing)
+        if (i % HC_D == 0) {
+            x.lse[bh * G + g] = l == 0.f ? -INFINITY : (m + log2f(l)) * KA_LN2;
+            sm_all[g][0] = m;
+            sm_all[g][1] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
+        }
+    }
+    if (!WEIGHTS) return;
+    __syncthreads();
+    const float ref = sm_all[col & (G - 1)][0], part = sm_all[col & (G - 1)][1];
+#pragma unroll
+    for (int b = 0; b < KA_BUFS; ++b) {
+        if (t + b * KS_WAVES >= tiles) break;
+        float mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float p = __builtin_amdgcn_exp2f(fmaf(S[b][i >> 2][i & 3], KA_SCALE, -ref)) * part;
+            if (G > 4) p = dpp_add<0x124>(p);                    // over the queries: columns repeat every G
+            if (G > 2) p = dpp_add<0x122>(p);
+            if (G > 1) p = dpp_add<0x121>(p);
+            mine = (col & 7) == i ? p : mine;
+        }
+        const int r = (t + b * KS_WAVES) * KQ_TILE + row0;
+        if (col < 8 && r < n) x.acc[hd.row_off + r] = fmaf(old[b], x.decay, mine);
+    }
+}
+
 template <int G>
 hc_status launch(hc_ctx* ctx, const AttnArgs& a, const CombineArgs& c, int workgroups, int n_chunks, hipStream_t st)
 {
+    if (workgroups == 0) {
+        const ShortArgs x{a, c.out, c.lse, c.acc, c.decay};
+        if (c.acc) kvq_attn_short_kernel<G, true><<<dim3((unsigned)a.n), dim3(KS_BLK), 0, st>>>(x);
+        else kvq_attn_short_kernel<G, false><<<dim3((unsigned)a.n), dim3(KS_BLK), 0, st>>>(x);
+        HC_HIP(ctx, hipGetLastError());
+        return HC_OK;
+    }
     const dim3 grid((unsigned)workgroups), block(KA_BLK);
     if (a.logits) kvq_attn_kernel<G, true><<<grid, block, 0, st>>>(a);
     else kvq_attn_kernel<G, false><<<grid, block, 0, st>>>(a);
@@ -516,7 +659,7 @@ hc_status hc_launch_kvq_attn(hc_ctx* ctx, const hc_kvq* k, const void* arena, co
     float* const po = (float*)((char*)work + l.part_o);
     int2* const plan = (int2*)((char*)work + l.plan);
     float* const logits = acc ? (float*)((char*)work + l.logits) : nullptr;
-    const int workgroups = (int)std::min((int64_t)hc_kvq_workgroups(ctx), std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
+    const int workgroups = k->max_cap <= KS_ROWS ? 0 : (int)std::min((int64_t)hc_kvq_workgroups(ctx), std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
     const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->room, (const uint16_t*)q, ml, po, plan, logits, k->n};
     const CombineArgs c{(const int2*)state, k->room, k->heads, k->chunks, plan, ml, po, logits, out, lse, acc, decay, k->n};
     switch (ctx->G) {

@@ -41,12 +41,14 @@ def queries(heads, G, seed, scale=1.5):
     return (scale * torch.randn((heads * G, D), generator=g, device=U.DEV) + 0.3).to(torch.bfloat16)
 
 
+@pytest.mark.parametrize("slack", [40, 2000])            # (tables of few rows a head are done in one launch)
 @pytest.mark.parametrize("G", [1, 2, 4, 8])
 @pytest.mark.parametrize("rows", [
+    [1024], [1023, 993, 0, 512],
     [1], [31], [32], [33], [0, 0], [0, 5, 0], [127, 128, 129, 4097], [1000, 1, 0, 64, 31, 5000, 7, 0], [20011], [3] * 70, [0] * 66 + [100] + [0] * 10 + [70]])
-def test_lengths(G, rows):
-    ctx = U.context(1, len(rows), G, max(rows) + 100)
-    cache = filled(ctx, rows, len(rows))
+def test_lengths(G, rows, slack):
+    ctx = U.context(1, len(rows), G, max(rows) + 2100)
+    cache = filled(ctx, rows, len(rows), slack=min(slack, 1024 - max(rows)) if slack == 40 and max(rows) <= 1024 else slack)
     q = queries(len(rows), G, 5)
     arena, state = cache.arena.clone(), cache.state.clone()
     out, lse, before = run(ctx, cache, q, G)
@@ -78,12 +80,13 @@ def test_long_and_batched(B, Hkv, G):
     hc.hc_destroy(ctx)
 
 
+@pytest.mark.parametrize("slack", [40, 2000])
 @pytest.mark.parametrize("G", [1, 4, 8])
-def test_logits_far_apart(G):
+def test_logits_far_apart(G, slack):
     """Logits of some thousand, rising along the rows, so that the reference moves all the time; the weights' differences are as exact as the logits."""
     n = 700
-    ctx = U.context(1, 2, G, 800)
-    cache = filled(ctx, [n, n], 2, seed=4, spread=30.0)
+    ctx = U.context(1, 2, G, 2800)
+    cache = filled(ctx, [n, n], 2, seed=4, spread=30.0, slack=slack)
     x = torch.ones((n, D), device=U.DEV) * torch.linspace(0.1, 40, n, device=U.DEV)[:, None]
     cache.put(1, 0, 0, x.to(torch.bfloat16))
     q = queries(2, G, 7, scale=6.0)
@@ -93,12 +96,13 @@ def test_logits_far_apart(G):
     hc.hc_destroy(ctx)
 
 
+@pytest.mark.parametrize("slack", [40, 2000])
 @pytest.mark.parametrize("G", [1, 4, 8])
-def test_values_of_any_size(G):
+def test_values_of_any_size(G, slack):
     """Rows of values from 2^-120 to 2^70 under weights from 1 to 2^-60: every column is held to its own sum."""
     n = 300
-    ctx = U.context(1, 1, G, 400)
-    cache = filled(ctx, [n], 1, seed=4)
+    ctx = U.context(1, 1, G, 2400)
+    cache = filled(ctx, [n], 1, seed=4, slack=slack)
     e = torch.randint(-120, 70, (n, 4), generator=torch.Generator().manual_seed(1)).to(U.DEV).double().repeat_interleave(32, dim=1)
     cache.put(0, 1, 0, (U.rows_of(n, 8).double() * 2.0 ** e).to(torch.bfloat16))
     q = queries(1, G, 7, scale=3.0)
@@ -108,13 +112,14 @@ def test_values_of_any_size(G):
     hc.hc_destroy(ctx)
 
 
+@pytest.mark.parametrize("slack", [40, 2000])
 @pytest.mark.parametrize("G", [1, 4, 8])
-def test_what_is_not_finite(G):
+def test_what_is_not_finite(G, slack):
     """NaNs behind the last row, in every byte, reach nothing.  A group of V that is not finite reaches its 32 columns of every query of its head and no others; a
     group of K every query of its head, and no other head."""
     rows = [70, 33, 200, 5]
-    ctx = U.context(1, 4, G, 300)
-    cache = filled(ctx, rows, 4)
+    ctx = U.context(1, 4, G, 2300)
+    cache = filled(ctx, rows, 4, slack=slack)
     for i, n in enumerate(rows):
         for v in (0, 1):
             codes, scales = cache.blocks(i, v)
