@@ -71,7 +71,7 @@ struct RowsArgs {
     int end[RW_SEQS], first[RW_SEQS];
     // Where the heads' blocks of kv are: a K and a V offset to a head; or (even), where those of every sequence lie evenly apart, as they do but for heads of
     // different room, first K offset, step, first V offset, step to a sequence, so that a launch has room for 64 sequences of any number of heads.  Four
-    // launches in place of one cost 64 decode tokens of eight heads 13 us, rows of 64 sequences 336 us in place of LOADTIME.
+    // launches in place of one cost 64 decode tokens of eight heads 13 us, rows of 64 sequences their loading 485 us in place of 346 (then).
     int64_t off[2 * RW_HEADS];
 };
 // Where the K rows of a workgroup's tokens are (codes -1: nowhere); V's, 68 cap bytes and v_kv elements further on.
@@ -89,30 +89,42 @@ __device__ __forceinline__ int row_places(const RowsArgs& a, RowPlaces& x, R row
     const int t0 = a.whole ? (blockIdx.x > 0 ? a.end[blockIdx.x - 1] : 0) : blockIdx.x * RW_TOKENS;
     const int n = a.whole ? a.end[blockIdx.x] - t0 : min(RW_TOKENS, a.tokens - t0);
     if (tid < RW_TOKENS) {
-        // The launch's arguments may lie in the host's memory, microseconds away: a lane takes those of one sequence, and gets others' from its neighbours.
-        // (A search that read them step by step, and 64 rows to a workgroup, cost 1.97 million rows 346 us in place of LOADTIME.)
-        const int end = lane < a.n_seq ? a.end[lane] : INT_MAX, first = a.first[lane];
-        int64_t off[4] = {0, 0, 0, 0};
-        if (a.even)
+        int i, f, bh;
+        int64_t k, v;
+        if (a.whole || a.n_seq == 1) {                           // one sequence: its arguments are the same for all lanes
+            const int seq = a.whole ? blockIdx.x : 0;
+            i = a.whole ? tid : t0 + tid;
+            f = a.first[seq];
+            bh = seq * a.Hkv + h;
+            k = a.even ? a.off[4 * seq] + h * a.off[4 * seq + 1] : a.off[2 * bh];
+            v = a.even ? a.off[4 * seq + 2] + h * a.off[4 * seq + 3] : a.off[2 * bh + 1];
+        } else {
+            // The launch's arguments may lie in the host's memory, microseconds away: a lane takes those of one sequence, and gets others' from its
+            // neighbours.  (A search that read them step by step cost 1.97 million rows of 64 sequences 346 us in place of 294.)
+            const int end = lane < a.n_seq ? a.end[lane] : INT_MAX, first = a.first[lane];
+            int64_t off[4] = {0, 0, 0, 0};
+            if (a.even)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) off[i] = a.off[4 * lane + i];
-        const int t = t0 + min(tid, n - 1);
-        int seq = 0;                                             // sequences that end before this token
+                for (int e = 0; e < 4; ++e) off[e] = a.off[4 * lane + e];
+            const int t = t0 + min(tid, n - 1);
+            int seq = 0;                                         // sequences that end before this token
 #pragma unroll
-        for (int step = RW_SEQS / 2; step > 0; step >>= 1)
-            if (__shfl(end, seq + step - 1) <= t) seq += step;
-        const int before = __shfl(end, max(seq - 1, 0)), bh = seq * a.Hkv + h;
+            for (int step = RW_SEQS / 2; step > 0; step >>= 1)
+                if (__shfl(end, seq + step - 1) <= t) seq += step;
+            const int before = __shfl(end, max(seq - 1, 0));
+            i = t - (seq > 0 ? before : 0);
+            f = __shfl(first, seq);
+            bh = seq * a.Hkv + h;
+            if (a.even) {
+                k = __shfl(off[0], seq) + h * __shfl(off[1], seq);
+                v = __shfl(off[2], seq) + h * __shfl(off[3], seq);
+            } else {
+                k = a.off[2 * bh];
+                v = a.off[2 * bh + 1];
+            }
+        }
         const hc_kvq_head hd = a.heads[bh];
         const int rows = min(max(a.state[bh].x, 0), hd.cap);
-        const int i = t - (seq > 0 ? before : 0), f = __shfl(first, seq);
-        int64_t k, v;
-        if (a.even) {
-            k = __shfl(off[0], seq) + h * __shfl(off[1], seq);
-            v = __shfl(off[2], seq) + h * __shfl(off[3], seq);
-        } else {
-            k = a.off[2 * bh];
-            v = a.off[2 * bh + 1];
-        }
         const int64_t row = tid < n ? row_of(f, i, rows, hd) : -1;
         x.codes[tid] = row < 0 ? -1 : hd.off + row * 64;
         x.scales[tid] = hd.off + (int64_t)64 * hd.cap + row * 4;
