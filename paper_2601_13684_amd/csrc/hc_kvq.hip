@@ -618,21 +618,24 @@ __global__ __launch_bounds__(SP_BLK) void kvq_evict_place_kernel(EvictArgs a)
     const hc_kvq_head from = a.heads[bh], to = a.to[bh];
     const int2 st = a.state[bh];
     const Keep x = keep_of(from, to, st);
-    if (span.y == 0 && tid == 0) a.to_state[bh] = make_int2(x.m, st.y);
-    if (span.y >= x.n) return;
+    if (span.y >= x.n) {
+        if (span.y == 0 && tid == 0) a.to_state[bh] = make_int2(x.m, st.y);
+        return;
+    }
     int count, at;                                               // rows of this span that stay; the first one's place
     if (x.m == x.n) {
         count = min(KQ_SPAN, x.n - span.y);
         at = span.y;
         for (int i = tid; i < count; i += SP_BLK) sm_list[i] = (uint16_t)i;
     } else {
-        SpanKeys s;
-        span_keys(a, from, x, span.y, s);
-        const uint2 last = x.k > 0 ? a.found[(size_t)bh * 3 + 2] : make_uint2(~0u, 0u);
         // what the head's spans before this one keep
         const int index = span.y / KQ_SPAN;
-        uint32_t larger = 0, equal = 0;
-        for (int i = tid; i < index; i += SP_BLK) {
+        const uint2 last = x.k > 0 ? a.found[(size_t)bh * 3 + 2] : make_uint2(~0u, 0u);
+        const uint2 mine = tid < index ? a.counts[blockIdx.x - index + tid] : make_uint2(0u, 0u);
+        SpanKeys s;
+        span_keys(a, from, x, span.y, s);
+        uint32_t larger = mine.x, equal = mine.y;
+        for (int i = tid + SP_BLK; i < index; i += SP_BLK) {
             const uint2 c = a.counts[blockIdx.x - index + i];
             larger += c.x;
             equal += c.y;
@@ -693,6 +696,7 @@ __global__ __launch_bounds__(SP_BLK) void kvq_evict_place_kernel(EvictArgs a)
         }
     }
     __syncthreads();
+    if (span.y == 0 && tid == 0) a.to_state[bh] = make_int2(x.m, st.y);
     if (a.list)
         for (int i = tid; i < count; i += SP_BLK) a.list[to.row_off + at + i] = span.y + sm_list[i];
     const uint8_t* const src = a.arena + from.off;
