@@ -73,7 +73,7 @@ __device__ __forceinline__ float sum_parts(float x)
 // of a phase of the reads (one chunk of 16 rows) go over all banks; the scales of row 4 x + y are at place 8 y + x, so that the eight that a lane takes for V
 // lie side by side.
 constexpr int T_V = 2048, T_KS = 4096, T_VS = T_KS + 128, T_BYTES = T_VS + 128;
-constexpr int KA_BUFS = 4;                   // of a wave, one after the other
+constexpr int KA_BUFS = 2, KS_BUFS = 4;      // of a wave, one after the other
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -109,7 +109,7 @@ __device__ __forceinline__ void read_tile(Tile& x, uint32_t k_at, uint32_t s_at,
           "n"((BUF * T_BYTES + T_V) / 256 + 7), "n"(BUF * T_BYTES + T_VS), "n"(BUF * T_BYTES + T_VS + 16)
         : "memory");
 }
-static_assert(T_BYTES % 256 == 0 && T_V % 256 == 0 && KA_BUFS * T_BYTES / 256 < 256, "offsets of the reads");
+static_assert(T_BYTES % 256 == 0 && T_V % 256 == 0 && KS_BUFS * T_BYTES / 256 < 256, "offsets of the reads");
 
 // One wave's part of a head: what it has of its queries and sums, and where its tiles go.
 template <int G>
@@ -319,7 +319,7 @@ struct Wave {
     }
 };
 static_assert(HC_MAX_G * HC_D * sizeof(float) <= T_BYTES, "a wave's sums go through its first buffer");
-constexpr int VMCNT0 = 0x0f70, VMCNT15 = 0x0f7f;                 // of s_waitcnt
+constexpr int VMCNT0 = 0x0f70, VMCNT5 = 0x0f75;                  // of s_waitcnt
 
 template <int G, bool LOGITS>
 __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
@@ -375,30 +375,25 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
         // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
         // 224K rows of eight heads, no logits 42.4 / 43.1, logits 53.3 / 47.6; two such heads and six short ones 16.6 / 18.2, 20.1 / 19.1.
         static constexpr int NT = LOGITS ? 0 : 2;
-        // a wave's tiles, KA_WAVES apart; while one is worked on, three are on their way
+        // a wave's tiles, KA_WAVES apart; while one is worked on, the next is on its way.  (More of them in flight, three, two / one, took 224K rows of eight heads
+        // 42.5, 41.2 / 39.4 us, ragged batches in groups of eight 20.8, 20.1 / 19.7, with weights 23.8, 22.6 / 21.8; three workgroups to a compute unit 40.5 and 20.9.)
         int t = t0 + w;
         wave.template load<0, NT>(t, t1);
         wave.template load<1, NT>(t + KA_WAVES, t1);
-        wave.template load<2, NT>(t + 2 * KA_WAVES, t1);
-        wave.template load<3, NT>(t + 3 * KA_WAVES, t1);
         wave.ready();
         auto step = [&](auto buf) {
             constexpr int BUF = decltype(buf)::value;
-            // three tiles' loads, and where logits are stored those of the three tiles before this one: not yet behind the first tiles
-            if (LOGITS && t < t0 + 3 * KA_WAVES) __builtin_amdgcn_s_waitcnt(VMCNT15);
+            // the next tile's loads are not waited for, nor where logits are stored this one's before them: there are none yet behind the first tile
+            if (LOGITS && t == t0 + w) __builtin_amdgcn_s_waitcnt(VMCNT5);
             f32x4 S[2];
-            wave.template add<BUF, LOGITS ? 18 : 15>(t, logits, S);
-            wave.template load<BUF, NT>(t + 4 * KA_WAVES, t1);
+            wave.template add<BUF, (KA_BUFS - 1) * (LOGITS ? 6 : 5)>(t, logits, S);
+            wave.template load<BUF, NT>(t + KA_BUFS * KA_WAVES, t1);
             t += KA_WAVES;
         };
         while (t < t1) {
             step(std::integral_constant<int, 0>{});
             if (t >= t1) break;
             step(std::integral_constant<int, 1>{});
-            if (t >= t1) break;
-            step(std::integral_constant<int, 2>{});
-            if (t >= t1) break;
-            step(std::integral_constant<int, 3>{});
         }
         __builtin_amdgcn_s_waitcnt(VMCNT0);                      // sums go through a buffer
         wave.finish(sm_ml[w], reinterpret_cast<float*>(&sm_tile[w][0][0]));
@@ -550,7 +545,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 // ---- heads of few rows: all of one in a workgroup, and no second launch --------------------------------------------------------------------
 
 constexpr int KS_BLK = 512, KS_WAVES = KS_BLK / 64;
-constexpr int KS_ROWS = KS_WAVES * KA_BUFS * KQ_TILE;            // that a workgroup has at once: all of its loads are on their way before the first product
+constexpr int KS_ROWS = KS_WAVES * KS_BUFS * KQ_TILE;            // that a workgroup has at once: all of its loads are on their way before the first product
 
 struct ShortArgs {
     AttnArgs a;
@@ -562,7 +557,7 @@ template <int G, bool WEIGHTS>
 __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
 {
     __shared__ float sm_ml[KS_WAVES][G][2], sm_all[G][2];
-    __shared__ __attribute__((aligned(256))) char sm_tile[KS_WAVES][KA_BUFS][T_BYTES];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KS_WAVES][KS_BUFS][T_BYTES];
     const AttnArgs& a = x.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), bh = blockIdx.x;
     const int n = __builtin_amdgcn_readfirstlane(kq_rows(a.state, a.room, bh)), tiles = tiles_of(n);
@@ -573,10 +568,10 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     const int t = w;                                             // its tiles: KS_WAVES apart
     // a lane's rows of a tile, eight of 4 i + lane / 16: lanes of columns i take row i to the table of weights
     const int col = wave.col, row0 = 4 * (col & 7) + wave.grp;
-    float old[KA_BUFS];
+    float old[KS_BUFS];
     if (WEIGHTS)
 #pragma unroll
-        for (int b = 0; b < KA_BUFS; ++b) {
+        for (int b = 0; b < KS_BUFS; ++b) {
             const int r = (t + b * KS_WAVES) * KQ_TILE + row0;
             old[b] = col < 8 && r < n ? x.acc[hd.row_off + r] : 0.f;
         }
@@ -585,7 +580,7 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     wave.template load<2, 0>(t + 2 * KS_WAVES, tiles);
     wave.template load<3, 0>(t + 3 * KS_WAVES, tiles);
     wave.ready();
-    f32x4 S[KA_BUFS][2];
+    f32x4 S[KS_BUFS][2];
     if (t < tiles) wave.template add<0, 15>(t, nullptr, S[0]);
     if (t + KS_WAVES < tiles) wave.template add<1, 10>(t + KS_WAVES, nullptr, S[1]);
     if (t + 2 * KS_WAVES < tiles) wave.template add<2, 5>(t + 2 * KS_WAVES, nullptr, S[2]);
@@ -615,7 +610,7 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     __syncthreads();
     const float ref = sm_all[col & (G - 1)][0], part = sm_all[col & (G - 1)][1];
 #pragma unroll
-    for (int b = 0; b < KA_BUFS; ++b) {
+    for (int b = 0; b < KS_BUFS; ++b) {
         if (t + b * KS_WAVES >= tiles) break;
         float mine = 0.f;
 #pragma unroll
