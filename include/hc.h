@@ -495,7 +495,8 @@ hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope* rope, cons
  * sequence's next token.  Lengths live there alone: the calls take them from the device, so that every one of them may be captured and replayed while they
  * grow.  acc: dev f32, a number a row (see row_off), or NULL where nothing is accumulated.  A cache, its state and its acc belong to the caller;
  * the hc_kvq is the table of where its heads are, may serve any number of them (every layer's), and must outlive graphs that were captured with
- * it.  All calls but create and destroy only enqueue, and neither allocate nor wait; calls that touch the same cache, state or acc are put in order by the
+ * it.  All calls but create and destroy only enqueue on the current device, which has to be the context's, and neither allocate nor wait; HOST arrays are read before
+ * they return (a captured store or load repeats the same first and count); calls that touch the same cache, state or acc are put in order by the
  * caller, and so are two that are given the same work buffer. */
 typedef struct hc_kvq hc_kvq;
 typedef struct {
@@ -521,12 +522,12 @@ hc_status hc_kvq_store(hc_ctx* ctx, const hc_kvq* kvq, const void* kv_prefill, c
 hc_status hc_kvq_load(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const int32_t* first, const int32_t* count,
                       void* kv_out, const int64_t* k_off, const int64_t* v_off, void* stream);
 /* The decode token of sequence b, at its next position: norm and rotation of its query and key heads (arguments as hc_append_rope's; computed in 64 bits,
- * rounded once to bf16), the queries to q_out (dev bf16 [B][Hq][128]), the K and V rows behind every head's last, with an acc (if not NULL) of 0; rows and
+ * rounded once to bf16), the queries to q_out (dev bf16 [B][Hq][128], must not overlap the inputs), the K and V rows behind every head's last, with an acc (if not NULL) of 0; rows and
  * position grow by one.  A head that is full keeps the rows that it has, and its position moves on. */
 hc_status hc_kvq_append(hc_ctx* ctx, const hc_kvq* kvq, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
                         int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* arena, int32_t* state, float* acc, void* stream);
 /* hc_decode_attn over this cache: out (dev f32 [B][Hq][128]) and lse (dev f32 [B][Hq]) of q (dev bf16 [B][Hq][128]) over the rows that every head holds;
- * of a head with none, 0 and minus infinity.  acc (if not NULL) of row j becomes  decay acc + (1/G) sum over the head's queries of its weight,
+ * of a head with none, 0 and minus infinity.  out must not overlap q.  acc (if not NULL) of row j becomes  decay acc + (1/G) sum over the head's queries of its weight,
  * decay in 0 .. 1 (not read where acc is NULL).  Rows' values are taken exactly, everything else is 32-bit.  Sums over the rows are divided at the end: finite values
  * of V beyond 2^90 may come out as infinities. */
 hc_status hc_kvq_attn(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const int32_t* state, const void* q, float* out, float* lse, float* acc,

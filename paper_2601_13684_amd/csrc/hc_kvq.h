@@ -26,6 +26,7 @@ struct hc_kvq {
 constexpr uint32_t HC_KVQ_MAGIC = 0x4843344bu;
 constexpr int KQ_TILE = 32;                  // rows that a wave of the attention pass takes at a time
 constexpr int KQ_CHUNK = 1024;               // rows of accumulated weights that a workgroup takes
+constexpr int KQ_SHORT = 8 * 1024;           // longest head of a table whose evictions are done a workgroup to a head
 constexpr int KQ_SPAN = 4096;                // rows that a workgroup of an eviction takes
 constexpr int KQ_BINS = 2048;                // of an eviction's histograms: 11 bits of a key
 constexpr int KQ_WG_PER_CU = 2;              // workgroups of the attention pass to a compute unit
@@ -50,9 +51,10 @@ inline hc_kvq_layout hc_kvq_plan(const hc_kvq* k)
     const size_t attn = l.logits + up((size_t)k->units * KQ_TILE * G * sizeof(float));
     l.list = 0;
     l.hist = up((size_t)k->rows * sizeof(int32_t));
-    l.found = l.hist + up((size_t)k->n * 3 * KQ_BINS * sizeof(uint32_t));
-    l.counts = l.found + up((size_t)k->n * 3 * sizeof(uint2));
-    const size_t evict = l.counts + up((size_t)k->n_spans * sizeof(uint2));
+    const bool spans = k->max_cap > KQ_SHORT;
+    l.found = l.hist + (spans ? up((size_t)k->n * 3 * KQ_BINS * sizeof(uint32_t)) : 0);
+    l.counts = l.found + (spans ? up((size_t)k->n * 3 * sizeof(uint2)) : 0);
+    const size_t evict = l.counts + (spans ? up((size_t)k->n_spans * sizeof(uint2)) : 0);
     l.bytes = attn > evict ? attn : evict;
     return l;
 }

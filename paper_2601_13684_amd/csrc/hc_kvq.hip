@@ -427,7 +427,6 @@ __device__ __forceinline__ void put_row(const MovedRow& r, uint8_t* dst, const h
 }
 
 constexpr int EV_BLK = 1024, EV_WAVES = EV_BLK / 64;
-constexpr int EV_LDS_ROWS = 8 * 1024;         // longest head of a table that is done a workgroup to a head
 
 // One workgroup per head: the rows that stay, in order.  Keys in LDS.
 __global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(EvictArgs a)
@@ -435,7 +434,7 @@ __global__ __launch_bounds__(EV_BLK) void kvq_select_kernel(EvictArgs a)
     __shared__ uint32_t sm_hist[KQ_BINS];
     __shared__ uint32_t sm_wave[EV_WAVES], sm_more[EV_WAVES];
     __shared__ uint32_t sm_found[2];
-    __shared__ uint32_t sm_key[EV_LDS_ROWS];
+    __shared__ uint32_t sm_key[KQ_SHORT];
     const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const hc_kvq_head from = a.heads[bh], to = a.to[bh];
     const int2 st = a.state[bh];
@@ -735,6 +734,14 @@ __global__ __launch_bounds__(MV_BLK) void kvq_move_kernel(EvictArgs a)
 
 bool kvq_ok(const hc_kvq* k) { return k && k->magic == HC_KVQ_MAGIC; }
 
+// Kernels run on the current device, and what they are handed is the context's.
+hc_status device_check(hc_ctx* ctx, const char* who)
+{
+    int now = -1;
+    HC_HIP(ctx, hipGetDevice(&now));
+    return now == ctx->device ? HC_OK : hc_fail(ctx, HC_ESTATE, "%s: the context is device %d's, the current one is %d", who, ctx->device, now);
+}
+
 // The cache, its state and its tables as a call is handed them.
 hc_status cache_check(hc_ctx* ctx, const char* who, const hc_kvq* kvq, const void* arena, const int32_t* state, const float* acc, bool need_acc)
 {
@@ -742,7 +749,7 @@ hc_status cache_check(hc_ctx* ctx, const char* who, const hc_kvq* kvq, const voi
     if (!arena || !state || (need_acc && !acc)) return hc_fail(ctx, HC_EINVAL, "%s: null pointer", who);
     if ((uintptr_t)arena & 63) return hc_fail(ctx, HC_EINVAL, "%s: the cache must be 64-byte aligned", who);
     if (((uintptr_t)state & 7) || ((uintptr_t)acc & 3)) return hc_fail(ctx, HC_EINVAL, "%s: misaligned state or weights", who);
-    return HC_OK;
+    return device_check(ctx, who);
 }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb)
@@ -802,6 +809,8 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
     if (!hc_ctx_ok(ctx)) return HC_ESTATE;
     if (!heads || !out) return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: null argument");
     *out = nullptr;
+    const hc_status here = device_check(ctx, "hc_kvq_create");
+    if (here != HC_OK) return here;
     const int n = ctx->cfg.B * ctx->cfg.Hkv;
     int64_t bytes = 0, rows = 0, units = 0;
     int32_t most = 0;
@@ -977,6 +986,8 @@ extern "C" hc_status hc_kvq_attn(hc_ctx* ctx, const hc_kvq* kvq, const void* are
     if (!q || !out || !lse || !work) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: null pointer");
     if (((uintptr_t)q | (uintptr_t)out) & 15) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: q and out must be 16-byte aligned");
     if ((uintptr_t)lse & 3) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: misaligned float pointer");
+    const size_t rows = (size_t)ctx->cfg.B * ctx->cfg.Hq;
+    if (overlap(q, rows * HC_D * 2, out, rows * HC_D * 4)) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: out overlaps q");       // (others' queries are read meanwhile)
     if (acc && !(decay >= 0.f && decay <= 1.f)) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: decay must be 0 .. 1");
     if ((uintptr_t)work & 255) return hc_fail(ctx, HC_EINVAL, "hc_kvq_attn: work must be 256-byte aligned");
     if (work_bytes < hc_kvq_plan(kvq).bytes)
@@ -1013,7 +1024,7 @@ extern "C" hc_status hc_kvq_evict(hc_ctx* ctx, const hc_kvq* kvq, const void* ar
     EvictArgs a{kvq->heads, to->heads, (const int2*)state, (int2*)to_state, acc, to_acc, (const uint8_t*)arena, (uint8_t*)to_arena, kept, 1, kvq->spans,
                 (uint32_t*)(w + l.hist), (uint2*)(w + l.found), (uint2*)(w + l.counts)};
     const dim3 heads((unsigned)kvq->n);
-    if (kvq->max_cap <= EV_LDS_ROWS) {
+    if (kvq->max_cap <= KQ_SHORT) {
         if (!kept) {
             a.list = (int32_t*)(w + l.list);
             a.list_is_to = 0;

@@ -105,6 +105,7 @@ def test_refused_calls(fake):  # noqa: F811
         assert attn(ctx=None) == hc.HC_ESTATE
         for kw, want, text in ((dict(kvq=foreign), hc.HC_ESTATE, "cache"), (dict(q=None), hc.HC_EINVAL, "null"), (dict(out=None), hc.HC_EINVAL, "null"),
                                (dict(lse=None), hc.HC_EINVAL, "null"), (dict(work=None), hc.HC_EINVAL, "null"), (dict(q=A(3) + 8), hc.HC_EINVAL, "16-byte"),
+                               (dict(out=A(3)), hc.HC_EINVAL, "overlaps"), (dict(out=A(3) - 4080), hc.HC_EINVAL, "overlaps"), (dict(out=A(3) + 2 * 4 * 256 - 16), hc.HC_EINVAL, "overlaps"),
                                (dict(lse=A(5) + 2), hc.HC_EINVAL, "misaligned"), (dict(decay=-0.1), hc.HC_EINVAL, "decay"), (dict(decay=1.5), hc.HC_EINVAL, "decay"),
                                (dict(decay=float("nan")), hc.HC_EINVAL, "decay"), (dict(work=A(7) + 64), hc.HC_EINVAL, "256-byte"), (dict(size=W - 1), hc.HC_EINVAL, "needed"),
                                (dict(state=A(2) + 4), hc.HC_EINVAL, "state")):
