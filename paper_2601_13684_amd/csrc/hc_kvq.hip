@@ -12,6 +12,7 @@ namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x)
@@ -54,6 +55,11 @@ __device__ __forceinline__ void put_row(uint8_t* __restrict__ codes_at, uint8_t*
 }
 
 // ---- rows in and out --------------------------------------------------------------------------------------------------------------------
+//
+// A row is 16 lanes' work: a lane has 16 bytes of bf16 and a dword of codes, the largest of 32 values takes two moves between neighbours, and the conversions are the
+// hardware's.  Bound by memory: a workgroup has all rows of its 64 tokens (of one head, K and V) on their way at once.  32,003 tokens of eight heads: in 34 us
+// (166 MB, 4.9 TB/s, where a copy of 1 GiB reaches 5.2) and 4.4 for the counts behind them, out 27 (6.1, what was just written lies in the caches); 1.97 million
+// rows out 294 us, 1.28 GB, 4.4 TB/s.  17 tokens of two heads 3.7 and 4.3 us: the launch and a chain of three loads.
 
 constexpr int RW_BLK = 256;
 constexpr int RW_TOKENS = 64;                 // of a workgroup
@@ -185,6 +191,8 @@ __global__ __launch_bounds__(RW_BLK) void kvq_count_kernel(RowsArgs a)
     }
 }
 
+// (Heads of the same tokens side by side in the grid: 64 sequences of equal heads 281 us in place of 294, but a long head among short ones then runs on one die of
+// the eight, 41 us in place of 18.)
 __global__ __launch_bounds__(RW_BLK) void kvq_load_kernel(RowsArgs a)
 {
     __shared__ RowPlaces sm;
@@ -239,8 +247,10 @@ __device__ __forceinline__ double sum16(double x)
 }
 
 // One workgroup per KV head and sequence: the token's K row, its V row and the G query rows of the group, 16 lanes a row, eight elements in a row to
-// each.  Norm and rotation in 64 bits: next to the border between two codes the step from one to the other is a third of the value, and whoever
-// computes in more bits than the row's own has the same row; a row a head is too little work to show.
+// each.  y = x (mean(x^2) + eps)^(-1/2) w, then pairs (u, v) -> gain (u cos a - v sin a, v cos a + u sin a), a = position * frequency; rounded to bf16, then to codes.
+// Norm and rotation in 64 bits: next to the border between two codes the step from one to the other is a third of the value, and whoever computes in more
+// bits than the row's own has the same row.  Bound by latency: 4.7 us for one sequence of two heads, 5.8 for 64 of eight (the angles' sine and cosine in 64
+// bits are 1.2 of it, the norm 0.3).
 template <bool F32>
 __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(TokenArgs a)
 {
@@ -271,21 +281,26 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.0;
     }
+    const float* const weight = row == 0 || !mine ? nullptr : row == 1 ? a.k_norm : a.q_norm;
+    f32x4 w0{1.f, 1.f, 1.f, 1.f}, w1 = w0;                       // (on their way with the rest)
+    if (weight) {
+        w0 = *reinterpret_cast<const f32x4*>(weight + e0);
+        w1 = *reinterpret_cast<const f32x4*>(weight + e0 + 4);
+    }
     if (2 * tid < a.rot) {
         const double t = (double)st.y * a.turns[tid];
         double s, c;
         sincospi(2.0 * (t - rint(t)), &s, &c);
         sm_turn[tid] = make_double2(c * a.gain, s * a.gain);
     }
-    const float* const weight = row == 0 ? nullptr : row == 1 ? a.k_norm : a.q_norm;
     double q = 0.0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) q = fma(x[e], x[e], q);
     q = sum16(q);
-    if (weight && mine) {
+    if (weight) {
         const double f = 1.0 / sqrt(q * (1.0 / HC_D) + (double)a.eps);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= f * (double)weight[e0 + e];
+        for (int e = 0; e < 8; ++e) x[e] *= f * (double)(e < 4 ? w0[e & 3] : w1[e & 3]);
     }
     if (mine && row > 0)
 #pragma unroll
@@ -329,6 +344,14 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
 }
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------------------
+//
+// What stays is what sorting by (weight descending, row ascending) would leave: the k-th largest key is found exactly, every larger one stays, and of its
+// equals the first.  Tables of heads of up to KQ_SHORT rows: one workgroup a head, keys in LDS, then a launch that moves rows: 2,304 rows of two heads 7.5 and
+// 3-4 us, mostly barriers and the chain of loads.  Longer: six launches over spans of KQ_SPAN rows, each bound by its own latency: 224K rows of eight
+// heads 4.3 (clear), 3 x 4.9 (digits), 4.8 (count), 14.9 us (place); 512 heads of up to 32K rows 5, 3 x 13.5, 14 and 183 us.  The last is bound by memory: of
+// rows of 64 bytes, a quarter of which stay, the memory reads lines of 128 (784 MB moved, 4.3 TB/s); with all rows staying it runs at 4.7 TB/s.
+// Measured against that: one workgroup to a long head, 330 us in place of 44 at 224K rows and 78 in place of 60 for the 512 heads; spans of 2,048 and 8,192 rows, 256
+// and 1,024 threads to a span: all within a tenth, none better in both cases.
 
 // Keys order as the weights do (hc_score_key), larger ones first; the k-th largest is found digit by digit, 11, 11 and 10 bits from the top, with a histogram of
 // the keys that have the digits found so far.

@@ -4,8 +4,8 @@
 //   acc_j <- decay acc_j + (1/G) sum_g p_gj / sum_i p_gi
 //
 // A workgroup takes an equal share of the tiles of 32 rows of all heads one after the other; lengths are on the device, and each
-// wave finds its share by itself.  A wave takes whole tiles, the next one's loads in flight under the present one's arithmetic, and nothing goes
-// through LDS until a head's end.  S^T = K Q^T and O^T = V^T P^T on the matrix cores (16x16x32), keys along S^T's rows, so that the lane that has a
+// wave finds its share by itself.  A wave takes whole tiles, the next one on its way to LDS (asynchronous loads, five to a tile of 4,352 bytes; straight to
+// registers they were twenty, and 224K rows took 48 us) under the present one's arithmetic; waves meet at a head's end alone.  S^T = K Q^T and O^T = V^T P^T on the matrix cores (16x16x32), keys along S^T's rows, so that the lane that has a
 // weight is the lane that hands it to the second product, and the products' order of the keys is chosen (row 4 x + y of the first is key
 // 4 y + x) so that a load of V takes four rows side by side.
 //   K   a lane's 16 bytes are 32 values of one scale: what the first product's four steps take; q is laid out alike
@@ -13,6 +13,12 @@
 // Codes become bf16 exactly.  The matrix cores have 16 columns for a group of at most 8 query heads: the others take what the rounding of the weights to
 // bf16 leaves, in two steps, so that the weights lose nothing (8 + 8 + 8 bits): columns g, G + g, 2 G + g for the parts of query head g, added at the end.
 // Groups of eight take a second product for the last part.
+//
+// Bound by memory where rows are many: 224K rows of eight heads 39.4 us (250 MB, 6.3 TB/s; a plain read of 1 GiB runs at 5.9) and 4.1 for the partial results; in
+// groups of eight the same within 2 us, so that the products and the codes' conversion, about 230 vector instructions a tile, stay hidden.  With weights 45.5 +
+// 11.7: logits go through memory, 32 bytes a row in groups of four against 136 for the row.  Two such heads and six of 1,024 to 8,192 rows 14.0 + 5.6, with weights
+// 15.8 + 6.2; 16 ragged sequences of 1 to 32K rows, four heads in groups of eight, with weights 22.0 + 9.5: about 5 us of either pass are launch, the search for its
+// share and the first loads.  512 heads of 4,096 rows 54 + 4.2 us (285 MB).  Few rows: 500 rows of two heads 6.4 us in one launch.
 #include <float.h>
 #include <math.h>
 
@@ -543,6 +549,9 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 }
 
 // ---- heads of few rows: all of one in a workgroup, and no second launch --------------------------------------------------------------------
+//
+// Where no head of a table has room for more than KS_ROWS rows.  us, this way / split and joined: 500 rows of two heads 6.4 / 5.0 + 3.9 in two launches, 1,000 rows of eight
+// heads 8.1 / 5.1 + 5.1, of 512 heads 20.1 / 20.2 + 4.2, with weights 23.9 / 23.1 + 13.4.
 
 constexpr int KS_BLK = 512, KS_WAVES = KS_BLK / 64;
 constexpr int KS_ROWS = KS_WAVES * KS_BUFS * KQ_TILE;            // that a workgroup has at once: all of its loads are on their way before the first product
