@@ -351,7 +351,7 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
 // heads 4.3 (clear), 3 x 4.9 (digits), 4.8 (count), 14.9 us (place); 512 heads of up to 32K rows 5, 3 x 13.5, 14 and 183 us.  The last is bound by memory: of
 // rows of 64 bytes, a quarter of which stay, the memory reads lines of 128 (784 MB moved, 4.3 TB/s); with all rows staying it runs at 4.7 TB/s.
 // Measured against that: one workgroup to a long head, 330 us in place of 44 at 224K rows and 78 in place of 60 for the 512 heads; spans of 2,048 and 8,192 rows, 256
-// and 1,024 threads to a span: all within a tenth, none better in both cases.
+// and 1,024 threads to a span: none better in both cases.
 
 // Keys order as the weights do (hc_score_key), larger ones first; the k-th largest is found digit by digit, 11, 11 and 10 bits from the top, with a histogram of
 // the keys that have the digits found so far.

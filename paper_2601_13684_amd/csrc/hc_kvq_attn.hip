@@ -124,14 +124,14 @@ struct Wave {
     int part;                                // of the weights that this column takes
     bool dead;
     uint32_t m1, m2;
-    float cs;
     lds_char* lds;
     uint32_t k_read, s_read, v_read, f_read; // what the lane reads of a tile: K's rows 16 s + 4 (col % 4) + col / 4 and V's 4 i + grp
     const uint8_t* block;                    // the head's
     uint32_t cap, k_at, v_at, s_at, k_chunk, v_chunk, s_base;
     int n, c_row, s_row;
     bf16x8 Q[4];
-    float ref, l;                            // weights are 2^(t - ref)
+    float ref;                               // weights are 2^(t - ref)
+    f32x4 L;                                 // their sums, of the columns; four times the same
     f32x4 O[8];
 
     __device__ __forceinline__ explicit Wave(char* tiles)
@@ -143,7 +143,6 @@ struct Wave {
         dead = part > 2;
         m1 = part >= 1 ? 0xffff0000u : 0u;
         m2 = part >= 2 ? 0xffff0000u : 0u;
-        cs = dead ? 0.f : KA_SCALE;
         lds = (lds_char*)tiles;
         const uint32_t tile0 = (uint32_t)(uintptr_t)lds;
         k_read = tile0 + (4 * (col & 3) + (col >> 2)) * 64 + (grp ^ (col & 3)) * 16;
@@ -168,8 +167,8 @@ struct Wave {
         s_at = s_base + s_row * 4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
-        ref = dead ? FLT_MAX : -FLT_MAX;
-        l = 0.f;
+        ref = dead ? FLT_MAX : -FLT_MAX;                     // (2^(t - FLT_MAX) is nothing)
+        L = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -223,7 +222,7 @@ struct Wave {
         }
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = kq_scale(x.vs[i >> 2][i & 3] >> (col >> 2) * 8 & 255u);
+        for (int i = 0; i < 8; ++i) f[i] = kq_scale(__builtin_amdgcn_ubfe(x.vs[i >> 2][i & 3], (col >> 2) * 8, 8));
         const int r0 = t * KQ_TILE;
         if (logits && col < 2 * G)                           // (columns g and G + g have the same: 2 G lanes store half of the eight each)
             *reinterpret_cast<f32x4*>(logits + ((size_t)t * 8 + 2 * grp) * G * 4 + col * 4) = col < G ? S[0] : S[1];
@@ -239,29 +238,28 @@ struct Wave {
         float p[8], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+            p[i] = fmaf(S[i >> 2][i & 3], KA_SCALE, -ref);
             top = fmaxf(top, p[i]);
         }
-        if (__builtin_amdgcn_ballot_w64(top > KA_SLACK && !dead)) {
-            float y = S[0][0] * cs;
+        if (__builtin_amdgcn_ballot_w64(top > KA_SLACK)) {
+            float y = S[0][0] * KA_SCALE;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * cs);
+            for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * KA_SCALE);
             y = fmaxf(y, __shfl_xor(y, 16));
             y = fmaxf(y, __shfl_xor(y, 32));
             y = fmaxf(y, ref);
             const float less = exp2f(ref - y);
             ref = y;
-            l *= less;
+            L *= less;
 #pragma unroll
             for (int j = 0; j < 8; ++j) O[j] *= less;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], cs, -ref);
+            for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], KA_SCALE, -ref);
         }
         uint32_t P1[8], P2[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float e = dead ? 0.f : __builtin_amdgcn_exp2f(p[i]);
-            l += e;
+            const float e = __builtin_amdgcn_exp2f(p[i]);
             const float r1 = e - __uint_as_float(__float_as_uint(e) & (G == 8 ? 0xffff0000u : m1));
             if (G == 8) {
                 P1[i] = __float_as_uint(part ? r1 : e);
@@ -276,6 +274,10 @@ struct Wave {
             B1[i] = __builtin_amdgcn_perm(P1[2 * i + 1], P1[2 * i], 0x07060302u);
             if (G == 8) B2[i] = __builtin_amdgcn_perm(P2[2 * i + 1], P2[2 * i], 0x07060302u);
         }
+        // the weights' sum is a product as well: with ones
+        const u32x4 ones{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, B1), L, 0, 0, 0);
+        if (G == 8) L = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, B2), L, 0, 0, 0);
         auto values = [&](auto byte) {
             constexpr int B = decltype(byte)::value;
             uint32_t c[8];
@@ -302,8 +304,7 @@ struct Wave {
     // The parts of a weight, and the groups of lanes, together: to ml [G][2] and o [G][128].
     __device__ __forceinline__ void finish(float (*ml)[2], float* o)
     {
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
+        const float l = sum_parts<G>(L[0]);
         if (lane < G) {
             ml[lane][0] = ref;
             ml[lane][1] = l;
