@@ -79,7 +79,7 @@ __device__ __forceinline__ float sum_parts(float x)
 // of a phase of the reads (one chunk of 16 rows) go over all banks; the scales of row 4 x + y are at place 8 y + x, so that the eight that a lane takes for V
 // lie side by side.
 constexpr int T_V = 2048, T_KS = 4096, T_VS = T_KS + 128, T_BYTES = T_VS + 128;
-constexpr int KA_BUFS = 2, KS_BUFS = 4;      // of a wave, one after the other
+constexpr int KS_BUFS = 4;                   // buffers of a wave, where it has four
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -156,7 +156,8 @@ struct Wave {
         k_chunk = ((lane & 3) ^ (lane >> 4)) * 16;
         v_chunk = (lane & 3) * 16;
     }
-    __device__ __forceinline__ void begin(const AttnArgs& a, int bh, int64_t off, uint32_t room, int rows)
+    // The head to load from, and its queries.
+    __device__ __forceinline__ void aim(const AttnArgs& a, int bh, int64_t off, uint32_t room, int rows)
     {
         block = a.arena + off;
         cap = room;
@@ -167,6 +168,9 @@ struct Wave {
         s_at = s_base + s_row * 4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) Q[c] = *reinterpret_cast<const bf16x8*>(a.q + ((size_t)bh * G + (col & (G - 1))) * HC_D + 32 * grp + 8 * c);
+    }
+    __device__ __forceinline__ void reset()
+    {
         ref = dead ? FLT_MAX : -FLT_MAX;                     // (2^(t - FLT_MAX) is nothing)
         L = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -184,8 +188,10 @@ struct Wave {
     {
         lds_char* const to = lds + BUF * T_BYTES;
         // (a tile behind the last is loaded from a buffer of no bytes, which costs no memory: the number of loads on their way is then always the same)
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)block, 0, t < end ? 136u * cap : 0u, 0x00027000);
-        const int r0 = t * KQ_TILE;
+        // (the same for all lanes, which the compiler does not see across the parts of a share)
+        const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uintptr_t)block >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)block);
+        const int r0 = __builtin_amdgcn_readfirstlane(t * KQ_TILE);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, __builtin_amdgcn_readfirstlane(t < end ? 136u * cap : 0u), 0x00027000);
         uint32_t k0 = k_at, k1 = k_at + 1024, v0 = v_at, v1 = v_at + 1024, s0 = s_at;
         if (r0 + KQ_TILE > n) {                              // rows behind the last repeat it; their weights and values become zeros
             const int last = max(n - 1 - r0, 0);
@@ -326,13 +332,23 @@ struct Wave {
     }
 };
 static_assert(HC_MAX_G * HC_D * sizeof(float) <= T_BYTES, "a wave's sums go through its first buffer");
-constexpr int VMCNT0 = 0x0f70, VMCNT5 = 0x0f75;                  // of s_waitcnt
+constexpr int VMCNT0 = 0x0f70, VMCNT1 = 0x0f71, VMCNT5 = 0x0f75;                  // of s_waitcnt
+
+// The waves' own LDS stores and reads are done, and all waves are here.  (__syncthreads would wait for the tiles on their way to LDS as well.)
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");       // (nothing is moved across by the compiler)
+    __builtin_amdgcn_s_waitcnt(0xc07f);                          // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 template <int G, bool LOGITS>
 __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs a)
 {
     __shared__ float sm_ml[KA_WAVES][G][2];
-    __shared__ __attribute__((aligned(256))) char sm_tile[KA_WAVES][KA_BUFS][T_BYTES];
+    __shared__ __attribute__((aligned(16))) float sm_o[KA_WAVES][G][HC_D];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KA_WAVES][2][T_BYTES];
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
 
     // this workgroup's share, and the head that it begins in
@@ -351,7 +367,13 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
     int sum = 0;
     if (each == 1) sum = lane < a.n ? places_of(h_rows) : 0;
     else
-        for (int i = mine0; i < mine1; ++i) sum += places_of(kq_rows(a.state, a.room, i));
+        for (int i = mine0; i < mine0 + each; i += 8) {          // (eight at a time, so that their loads do not follow one another)
+            int rows[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rows[e] = kq_rows(a.state, a.room, min(i + e, a.n - 1));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += i + e < mine1 ? places_of(rows[e]) : 0;
+        }
     int upto = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -365,36 +387,53 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
     int bh = __builtin_amdgcn_readfirstlane(owner * each);
     int before = __builtin_amdgcn_readlane(upto - sum, owner);
     Wave<G> wave(&sm_tile[w][0][0]);
-    for (; before < u1 && bh < a.n; ++bh) {
-        if (bh >= window + 64) {
-            window = bh;
-            look();
+    // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
+    // 224K rows of eight heads, no logits 39.4 / 40.6, logits 52.1 / 45.5; two such heads and six short ones 14.0 / 14.9, 18.1 / 15.8.
+    static constexpr int NT = LOGITS ? 0 : 2;
+    int head = 0, t0 = 0, t1 = 0;                                // of the part at hand: tiles [t0, t1) of a head
+    float* logits = nullptr;
+    // The next part of the share: where it is, its queries' and its first tiles' loads.
+    auto next = [&]() -> bool {
+        for (; before < u1 && bh < a.n; ++bh) {
+            if (bh >= window + 64) {
+                window = bh;
+                look();
+            }
+            const int n = __builtin_amdgcn_readlane(h_rows, bh - window), tiles = tiles_of(n), begin = before + KA_START;
+            before += places_of(n);
+            t0 = max(u0 - begin, 0);
+            t1 = min(tiles, u1 - begin);
+            if (t0 >= t1) continue;
+            head = bh;
+            if (t0 == 0 && tid == 0) a.plan[bh] = make_int2((int)blockIdx.x + bh, (begin + tiles - 1) / per - (int)blockIdx.x + 1);
+            const int64_t off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h_off >> 32), bh - window) << 32 |
+                                          (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window));
+            wave.aim(a, bh, off, (uint32_t)__builtin_amdgcn_readlane(h_cap, bh - window), n);
+            if (LOGITS) logits = a.logits + (size_t)__builtin_amdgcn_readlane(h_first, bh - window) * KQ_TILE * G;
+            wave.template load<0, NT>(t0 + w, t1);
+            wave.template load<1, NT>(t0 + w + KA_WAVES, t1);
+            ++bh;
+            return true;
         }
-        const int n = __builtin_amdgcn_readlane(h_rows, bh - window), tiles = tiles_of(n), begin = before + KA_START;
-        before += places_of(n);
-        const int t0 = max(u0 - begin, 0), t1 = min(tiles, u1 - begin);
-        if (t0 >= t1) continue;
-        const int64_t off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h_off >> 32), bh - window) << 32 |
-                                      (uint32_t)__builtin_amdgcn_readlane((int)h_off, bh - window));
-        if (t0 == 0 && tid == 0) a.plan[bh] = make_int2((int)blockIdx.x + bh, (begin + tiles - 1) / per - (int)blockIdx.x + 1);
-        wave.begin(a, bh, off, (uint32_t)__builtin_amdgcn_readlane(h_cap, bh - window), n);
-        float* const logits = LOGITS ? a.logits + (size_t)__builtin_amdgcn_readlane(h_first, bh - window) * KQ_TILE * G : nullptr;
-        // Codes are read once: marked so (2), unless the logits on their way to the next kernel share the caches with them.  us of this pass, marked / not:
-        // 224K rows of eight heads, no logits 42.4 / 43.1, logits 53.3 / 47.6; two such heads and six short ones 16.6 / 18.2, 20.1 / 19.1.
-        static constexpr int NT = LOGITS ? 0 : 2;
+        return false;
+    };
+    for (bool more = next(); more;) {
+        wave.reset();
+        wave.ready();
         // a wave's tiles, KA_WAVES apart; while one is worked on, the next is on its way.  (More of them in flight, three, two / one, took 224K rows of eight heads
         // 42.5, 41.2 / 39.4 us, ragged batches in groups of eight 20.8, 20.1 / 19.7, with weights 23.8, 22.6 / 21.8; three workgroups to a compute unit 40.5 and 20.9.)
         int t = t0 + w;
-        wave.template load<0, NT>(t, t1);
-        wave.template load<1, NT>(t + KA_WAVES, t1);
-        wave.ready();
         auto step = [&](auto buf) {
             constexpr int BUF = decltype(buf)::value;
-            // the next tile's loads are not waited for, nor where logits are stored this one's before them: there are none yet behind the first tile
-            if (LOGITS && t == t0 + w) __builtin_amdgcn_s_waitcnt(VMCNT5);
+            // not waited for: the next tile's loads, and where logits are stored the store before them; behind the last tile there are no loads, and
+            // before the first no store
+            const bool first = t == t0 + w, last = t + KA_WAVES >= t1;
+            if (last && LOGITS && !first) __builtin_amdgcn_s_waitcnt(VMCNT1);
+            else if (last) __builtin_amdgcn_s_waitcnt(VMCNT0);
+            else if (LOGITS && first) __builtin_amdgcn_s_waitcnt(VMCNT5);
             f32x4 S[2];
-            wave.template add<BUF, (KA_BUFS - 1) * (LOGITS ? 6 : 5)>(t, logits, S);
-            wave.template load<BUF, NT>(t + KA_BUFS * KA_WAVES, t1);
+            wave.template add<BUF, LOGITS ? 6 : 5>(t, logits, S);
+            if (t + 2 * KA_WAVES < t1) wave.template load<BUF, NT>(t + 2 * KA_WAVES, t1);
             t += KA_WAVES;
         };
         while (t < t1) {
@@ -402,10 +441,11 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
             if (t >= t1) break;
             step(std::integral_constant<int, 1>{});
         }
-        __builtin_amdgcn_s_waitcnt(VMCNT0);                      // sums go through a buffer
-        wave.finish(sm_ml[w], reinterpret_cast<float*>(&sm_tile[w][0][0]));
-        __syncthreads();
-        const size_t slot = (size_t)blockIdx.x + bh;
+        if (t == t0 + w) __builtin_amdgcn_s_waitcnt(VMCNT0);     // (no tile: nothing has waited for the loads of none, and others follow into their places)
+        const size_t slot = (size_t)blockIdx.x + head;
+        more = next();                                           // (its loads are on their way while the waves' sums are put together)
+        wave.finish(sm_ml[w], &sm_o[w][0][0]);
+        meet();
         for (int i = tid; i < G * HC_D; i += KA_BLK) {
             const int g = i / HC_D, d = i % HC_D;
             float m = sm_ml[0][g][0], o = 0.f, s = 0.f;
@@ -414,7 +454,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
 #pragma unroll
             for (int k = 0; k < KA_WAVES; ++k) {
                 const float f = exp2f(sm_ml[k][g][0] - m);
-                o = fmaf(f, reinterpret_cast<const float*>(&sm_tile[k][0][0])[i], o);
+                o = fmaf(f, sm_o[k][g][d], o);
                 s = fmaf(f, sm_ml[k][g][1], s);
             }
             a.part_o[(slot * G + g) * HC_D + d] = o;
@@ -423,7 +463,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
                 a.part_ml[(slot * G + g) * 2 + 1] = s;
             }
         }
-        __syncthreads();
+        meet();
     }
 }
 
@@ -574,7 +614,8 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     const hc_kvq_head hd = a.heads[bh];
     const int64_t off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(hd.off >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)hd.off));
     Wave<G> wave(&sm_tile[w][0][0]);
-    wave.begin(a, bh, off, (uint32_t)__builtin_amdgcn_readfirstlane(hd.cap), n);
+    wave.aim(a, bh, off, (uint32_t)__builtin_amdgcn_readfirstlane(hd.cap), n);
+    wave.reset();
     const int t = w;                                             // its tiles: KS_WAVES apart
     // a lane's rows of a tile, eight of 4 i + lane / 16: lanes of columns i take row i to the table of weights
     const int col = wave.col, row0 = 4 * (col & 7) + wave.grp;
