@@ -79,7 +79,7 @@ __device__ __forceinline__ float sum_parts(float x)
 // of a phase of the reads (one chunk of 16 rows) go over all banks; the scales of row 4 x + y are at place 8 y + x, so that the eight that a lane takes for V
 // lie side by side.
 constexpr int T_V = 2048, T_KS = 4096, T_VS = T_KS + 128, T_BYTES = T_VS + 128;
-constexpr int KS_BUFS = 4;                   // buffers of a wave, where it has four
+constexpr int KS_BUFS = 4;                   // most buffers of a wave
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -591,11 +591,12 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 
 // ---- heads of few rows: all of one in a workgroup, and no second launch --------------------------------------------------------------------
 //
-// Where no head of a table has room for more than KS_ROWS rows.  us, this way / split and joined: 500 rows of two heads 6.4 / 5.0 + 3.9 in two launches, 1,000 rows of eight
-// heads 8.1 / 5.1 + 5.1, of 512 heads 20.1 / 20.2 + 4.2, with weights 23.9 / 23.1 + 13.4.
+// Where no head of a table has room for more than KS_BUFS KS_ROWS = 1,024 rows; where it is a half or a quarter of that, waves have fewer buffers, and a compute unit holds
+// two or four workgroups (4,096 heads of 100 rows 70 us with four buffers, 30 with one).  us, this way / split and joined: 500 rows of two heads 6.5 / 5.0 + 3.9 in two launches, 200 rows of eight
+// heads 4.8 / 5.1 + 4.8, 1,000 rows of eight heads 7.6 / 5.1 + 5.1, of 512 heads 19.8 / 20.2 + 4.2, with weights 23.9 / 23.1 + 13.4.
 
 constexpr int KS_BLK = 512, KS_WAVES = KS_BLK / 64;
-constexpr int KS_ROWS = KS_WAVES * KS_BUFS * KQ_TILE;            // that a workgroup has at once: all of its loads are on their way before the first product
+constexpr int KS_ROWS = KS_WAVES * KQ_TILE;  // that a workgroup has at once, to a buffer of its waves: all of its loads are on their way before the first product
 
 struct ShortArgs {
     AttnArgs a;
@@ -603,11 +604,11 @@ struct ShortArgs {
     float decay;
 };
 
-template <int G, bool WEIGHTS>
+template <int G, bool WEIGHTS, int BUFS>
 __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
 {
     __shared__ float sm_ml[KS_WAVES][G][2], sm_all[G][2];
-    __shared__ __attribute__((aligned(256))) char sm_tile[KS_WAVES][KS_BUFS][T_BYTES];
+    __shared__ __attribute__((aligned(256))) char sm_tile[KS_WAVES][BUFS][T_BYTES];
     const AttnArgs& a = x.a;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), bh = blockIdx.x;
     const int n = __builtin_amdgcn_readfirstlane(kq_rows(a.state, a.room, bh)), tiles = tiles_of(n);
@@ -619,23 +620,26 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     const int t = w;                                             // its tiles: KS_WAVES apart
     // a lane's rows of a tile, eight of 4 i + lane / 16: lanes of columns i take row i to the table of weights
     const int col = wave.col, row0 = 4 * (col & 7) + wave.grp;
-    float old[KS_BUFS];
+    float old[BUFS];
     if (WEIGHTS)
 #pragma unroll
-        for (int b = 0; b < KS_BUFS; ++b) {
+        for (int b = 0; b < BUFS; ++b) {
             const int r = (t + b * KS_WAVES) * KQ_TILE + row0;
             old[b] = col < 8 && r < n ? x.acc[hd.row_off + r] : 0.f;
         }
     wave.template load<0, 0>(t, tiles);
-    wave.template load<1, 0>(t + KS_WAVES, tiles);
-    wave.template load<2, 0>(t + 2 * KS_WAVES, tiles);
-    wave.template load<3, 0>(t + 3 * KS_WAVES, tiles);
+    if constexpr (BUFS > 1) wave.template load<1, 0>(t + KS_WAVES, tiles);
+    if constexpr (BUFS > 2) wave.template load<2, 0>(t + 2 * KS_WAVES, tiles);
+    if constexpr (BUFS > 3) wave.template load<3, 0>(t + 3 * KS_WAVES, tiles);
     wave.ready();
-    f32x4 S[KS_BUFS][2];
-    if (t < tiles) wave.template add<0, 15>(t, nullptr, S[0]);
-    if (t + KS_WAVES < tiles) wave.template add<1, 10>(t + KS_WAVES, nullptr, S[1]);
-    if (t + 2 * KS_WAVES < tiles) wave.template add<2, 5>(t + 2 * KS_WAVES, nullptr, S[2]);
-    if (t + 3 * KS_WAVES < tiles) wave.template add<3, 0>(t + 3 * KS_WAVES, nullptr, S[3]);
+    f32x4 S[BUFS][2];
+    if (t < tiles) wave.template add<0, 5 * (BUFS - 1)>(t, nullptr, S[0]);
+    if constexpr (BUFS > 1)
+        if (t + KS_WAVES < tiles) wave.template add<1, 5 * (BUFS - 2)>(t + KS_WAVES, nullptr, S[1]);
+    if constexpr (BUFS > 2)
+        if (t + 2 * KS_WAVES < tiles) wave.template add<2, 5 * (BUFS - 3)>(t + 2 * KS_WAVES, nullptr, S[2]);
+    if constexpr (BUFS > 3)
+        if (t + 3 * KS_WAVES < tiles) wave.template add<3, 0>(t + 3 * KS_WAVES, nullptr, S[3]);
     __builtin_amdgcn_s_waitcnt(VMCNT0);                          // sums go through a buffer
     wave.finish(sm_ml[w], reinterpret_cast<float*>(&sm_tile[w][0][0]));
     __syncthreads();
@@ -661,7 +665,7 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     __syncthreads();
     const float ref = sm_all[col & (G - 1)][0], part = sm_all[col & (G - 1)][1];
 #pragma unroll
-    for (int b = 0; b < KS_BUFS; ++b) {
+    for (int b = 0; b < BUFS; ++b) {
         if (t + b * KS_WAVES >= tiles) break;
         float mine = 0.f;
 #pragma unroll
@@ -677,13 +681,21 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
     }
 }
 
-template <int G>
-hc_status launch(hc_ctx* ctx, const AttnArgs& a, const CombineArgs& c, int workgroups, int n_chunks, hipStream_t st)
+template <int G, int BUFS>
+void launch_short(const ShortArgs& x, hipStream_t st)
 {
-    if (workgroups == 0) {
+    if (x.acc) kvq_attn_short_kernel<G, true, BUFS><<<dim3((unsigned)x.a.n), dim3(KS_BLK), 0, st>>>(x);
+    else kvq_attn_short_kernel<G, false, BUFS><<<dim3((unsigned)x.a.n), dim3(KS_BLK), 0, st>>>(x);
+}
+
+template <int G>
+hc_status launch(hc_ctx* ctx, const AttnArgs& a, const CombineArgs& c, int longest, int workgroups, int n_chunks, hipStream_t st)
+{
+    if (longest <= KS_BUFS * KS_ROWS) {
         const ShortArgs x{a, c.out, c.lse, c.acc, c.decay};
-        if (c.acc) kvq_attn_short_kernel<G, true><<<dim3((unsigned)a.n), dim3(KS_BLK), 0, st>>>(x);
-        else kvq_attn_short_kernel<G, false><<<dim3((unsigned)a.n), dim3(KS_BLK), 0, st>>>(x);
+        if (longest <= KS_ROWS) launch_short<G, 1>(x, st);
+        else if (longest <= 2 * KS_ROWS) launch_short<G, 2>(x, st);
+        else launch_short<G, KS_BUFS>(x, st);
         HC_HIP(ctx, hipGetLastError());
         return HC_OK;
     }
@@ -710,13 +722,13 @@ hc_status hc_launch_kvq_attn(hc_ctx* ctx, const hc_kvq* k, const void* arena, co
     float* const po = (float*)((char*)work + l.part_o);
     int2* const plan = (int2*)((char*)work + l.plan);
     float* const logits = acc ? (float*)((char*)work + l.logits) : nullptr;
-    const int workgroups = k->max_cap <= KS_ROWS ? 0 : (int)std::min((int64_t)hc_kvq_workgroups(ctx), std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
+    const int workgroups = (int)std::min((int64_t)hc_kvq_workgroups(ctx), std::max((int64_t)1, (k->units + (int64_t)k->n * KA_START + KA_LEAST - 1) / KA_LEAST));
     const AttnArgs a{(const uint8_t*)arena, (const int2*)state, k->heads, k->room, (const uint16_t*)q, ml, po, plan, logits, k->n};
     const CombineArgs c{(const int2*)state, k->room, k->heads, k->chunks, plan, ml, po, logits, out, lse, acc, decay, k->n};
     switch (ctx->G) {
-    case 1: return launch<1>(ctx, a, c, workgroups, k->n_chunks, st);
-    case 2: return launch<2>(ctx, a, c, workgroups, k->n_chunks, st);
-    case 4: return launch<4>(ctx, a, c, workgroups, k->n_chunks, st);
-    default: return launch<8>(ctx, a, c, workgroups, k->n_chunks, st);
+    case 1: return launch<1>(ctx, a, c, k->max_cap, workgroups, k->n_chunks, st);
+    case 2: return launch<2>(ctx, a, c, k->max_cap, workgroups, k->n_chunks, st);
+    case 4: return launch<4>(ctx, a, c, k->max_cap, workgroups, k->n_chunks, st);
+    default: return launch<8>(ctx, a, c, k->max_cap, workgroups, k->n_chunks, st);
     }
 }

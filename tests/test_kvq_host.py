@@ -46,7 +46,7 @@ def test_tables(fake):  # noqa: F811
         for kw, text in ((dict(cap=0), "cap 0"), (dict(cap=15), "cap 15"), (dict(cap=-16), "cap"), (dict(cap=4112), "cap 4112")):
             refused(change(2, **kw), hc.HC_ESHAPE, ctx, text)
         for kw, text in ((dict(off=-64), "off"), (dict(off=32), "off"), (dict(row_off=-1), "row_off"), (dict(budget=0), "budget"), (dict(budget=17), "budget"),
-                         (dict(sink=-1), "sink"), (dict(recent=-1), "recent"), (dict(off=64), "overlap"), (dict(row_off=63), "overlap"), (dict(off=0), "overlap")):
+                         (dict(sink=-1), "sink"), (dict(recent=-1), "recent"), (dict(sink=4097), "sink"), (dict(recent=2 ** 31 - 1), "recent"), (dict(off=64), "overlap"), (dict(row_off=63), "overlap"), (dict(off=0), "overlap")):
             refused(change(1, **kw), hc.HC_EINVAL, ctx, text)
         assert L.hc_kvq_create(ctx, None, C.byref(C.c_void_p())) == hc.HC_EINVAL
         assert L.hc_kvq_create(None, None, None) == hc.HC_ESTATE
@@ -163,4 +163,25 @@ def test_launches_of_many_heads(fake):  # noqa: F811
             fake.fake_reset(0)
             assert L.hc_kvq_load(ctx, kvq, A(1), A(2), i32(*[0] * 70), i32(*[0] * 69 + [2]), A(3), off, even, None) == 0
             assert len(log()) == 1
+    """))
+
+
+def test_launches_by_the_longest_head(fake):  # noqa: F811
+    """Attention over heads of little room is one launch, a workgroup to a head; eviction of short heads two launches, of long ones six."""
+    run(fake, body("""
+        ctx = ctx_of(1, 3, max_ctx=16384)
+        for cap, attn, evict in ((256, ["short"], 2), (272, ["short"], 2), (1024, ["short"], 2), (1040, ["attn", "combine"], 2), (8192, ["attn", "combine"], 2),
+                                 (8208, ["attn", "combine"], 6)):
+            kvq, to = create(table([16, cap, 32]), ctx)[1], create(table([16, 16, 16]), ctx)[1]
+            W = L.hc_kvq_work_bytes(ctx, kvq)
+            fake.fake_reset(0)
+            assert L.hc_kvq_attn(ctx, kvq, A(1), A(2), A(3), A(4), A(5), A(6), 1.0, A(7), W, None) == 0
+            assert len(log()) == len(attn) and all(k in l[0] for k, l in zip(attn, log())), log()
+            if attn == ["short"]:
+                assert log()[0][1] == "3"
+            else:
+                assert int(log()[0][1]) <= 512 and int(log()[1][1]) == 3 * 4 + 2 + (cap + 1023) // 1024
+            fake.fake_reset(0)
+            assert L.hc_kvq_evict(ctx, kvq, A(1), A(2), A(3), to, A(4), A(5), A(6), None, A(8), W, None) == 0
+            assert len(log()) == evict
     """))
