@@ -57,9 +57,9 @@ __device__ __forceinline__ void put_row(uint8_t* __restrict__ codes_at, uint8_t*
 // ---- rows in and out --------------------------------------------------------------------------------------------------------------------
 //
 // A row is 16 lanes' work: a lane has 16 bytes of bf16 and a dword of codes, the largest of 32 values takes two moves between neighbours, and the conversions are the
-// hardware's.  Bound by memory: a workgroup has all rows of its 64 tokens (of one head, K and V) on their way at once.  32,003 tokens of eight heads: in 34 us
-// (166 MB, 4.9 TB/s, where a copy of 1 GiB reaches 5.2) and 4.4 for the counts behind them, out 27 (6.1, what was just written lies in the caches); 1.97 million
-// rows out 294 us, 1.28 GB, 4.4 TB/s.  17 tokens of two heads 3.7 and 4.3 us: the launch and a chain of three loads.
+// hardware's.  Bound by memory: a workgroup has all rows of its 64 tokens (of one head, K and V) on their way at once.  32,003 tokens of eight heads: in 33 us
+// (166 MB, 5.0 TB/s, where a copy of 1 GiB reaches 5.2) and 4.8 for the counts behind them, out 26.5 (6.3, what was just written lies in the caches); 1.97 million
+// rows out 296 us, 1.28 GB, 4.3 TB/s.  17 tokens of two heads 4.2 and 3.7 us: the launch and a chain of three loads.
 
 constexpr int RW_BLK = 256;
 constexpr int RW_TOKENS = 64;                 // of a workgroup
@@ -346,9 +346,9 @@ __global__ __launch_bounds__(token_threads(HC_MAX_G)) void kvq_append_kernel(Tok
 // ---- eviction -------------------------------------------------------------------------------------------------------------------------------
 //
 // What stays is what sorting by (weight descending, row ascending) would leave: the k-th largest key is found exactly, every larger one stays, and of its
-// equals the first.  Tables of heads of up to KQ_SHORT rows: one workgroup a head, keys in LDS, then a launch that moves rows: 2,304 rows of two heads 7.5 and
-// 3-4 us, mostly barriers and the chain of loads.  Longer: six launches over spans of KQ_SPAN rows, each bound by its own latency: 224K rows of eight
-// heads 4.3 (clear), 3 x 4.9 (digits), 4.8 (count), 14.9 us (place); 512 heads of up to 32K rows 5, 3 x 13.5, 14 and 183 us.  The last is bound by memory: of
+// equals the first.  Tables of heads of up to KQ_SHORT rows: one workgroup a head, keys in LDS, then a launch that moves rows: 2,304 rows of two heads 7.7 and
+// 2.8 us, mostly barriers and the chain of loads.  Longer: six launches over spans of KQ_SPAN rows, each bound by its own latency: 224K rows of eight
+// heads 4.0 (clear), 3 x 5.1 (digits), 5.0 (count), 15.1 us (place); 512 heads of up to 32K rows 5.7, 3 x 13.7, 14 and 183 us.  The last is bound by memory: of
 // rows of 64 bytes, a quarter of which stay, the memory reads lines of 128 (784 MB moved, 4.3 TB/s); with all rows staying it runs at 4.7 TB/s.
 // Measured against that: one workgroup to a long head, 330 us in place of 44 at 224K rows and 78 in place of 60 for the 512 heads; spans of 2,048 and 8,192 rows, 256
 // and 1,024 threads to a span: none better in both cases.

@@ -14,11 +14,11 @@
 // bf16 leaves, in two steps, so that the weights lose nothing (8 + 8 + 8 bits): columns g, G + g, 2 G + g for the parts of query head g, added at the end.
 // Groups of eight take a second product for the last part.
 //
-// Bound by memory where rows are many: 224K rows of eight heads 39.4 us (250 MB, 6.3 TB/s; a plain read of 1 GiB runs at 5.9) and 4.1 for the partial results; in
-// groups of eight the same within 2 us, so that the products and the codes' conversion, about 230 vector instructions a tile, stay hidden.  With weights 45.5 +
-// 11.7: logits go through memory, 32 bytes a row in groups of four against 136 for the row.  Two such heads and six of 1,024 to 8,192 rows 14.0 + 5.6, with weights
-// 15.8 + 6.2; 16 ragged sequences of 1 to 32K rows, four heads in groups of eight, with weights 22.0 + 9.5: about 5 us of either pass are launch, the search for its
-// share and the first loads.  512 heads of 4,096 rows 54 + 4.2 us (285 MB).  Few rows: 500 rows of two heads 6.4 us in one launch.
+// Bound by memory where rows are many: 224K rows of eight heads 39.0 us (250 MB, 6.4 TB/s; a plain read of 1 GiB runs at 5.9) and 4.3 for the partial results; in
+// groups of eight the same within 2 us, so that the products and the codes' conversion, 214 vector instructions a tile, stay hidden.  With weights 45.1 +
+// 11.9: logits go through memory, 32 bytes a row in groups of four against 136 for the row.  Two such heads and six of 1,024 to 8,192 rows 13.8 + 5.6, with weights
+// 15.3 + 6.4; 16 ragged sequences of 1 to 32K rows, four heads in groups of eight, with weights 21.6 + 9.4: about 5 us of either pass are launch, the search for its
+// share and the first loads.  512 heads of 4,096 rows 50 to 54 + 4.2 us (285 MB).  Few rows: 500 rows of two heads 5.8 us in one launch.
 #include <float.h>
 #include <math.h>
 
