@@ -504,8 +504,8 @@ typedef struct {
     int64_t row_off;   /* element of its row 0 in acc and kept                                               */
     int32_t cap;       /* rows that it has room for: multiple of 16, 16 .. max_ctx                           */
     int32_t budget;    /* rows that hc_kvq_evict leaves when it fills this head, 1 .. cap ...                */
-    int32_t sink;      /* ... of which the first `sink` (0 .. max_ctx) ...                                   */
-    int32_t recent;    /* ... and the last `recent` (0 .. max_ctx) of the source always are                  */
+    int32_t sink;      /* ... of which the first `sink` (0 .. 2^30, also more than there are rows) ...       */
+    int32_t recent;    /* ... and the last `recent` (as `sink`) of the source always are                     */
 } hc_kvq_head;
 /* Table of B*Hkv entries, row (b*Hkv + h), HOST memory.  Blocks must not overlap, nor rows in acc.  Allocates and synchronises. */
 hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads_host, hc_kvq** out);

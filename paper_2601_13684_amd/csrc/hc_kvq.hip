@@ -843,7 +843,8 @@ extern "C" hc_status hc_kvq_create(hc_ctx* ctx, const hc_kvq_head* heads, hc_kvq
             return hc_fail(ctx, HC_ESHAPE, "hc_kvq_create: head %d: cap %d must be a multiple of 16, 16 .. max_ctx", i, (int)h.cap);
         if (h.off < 0 || (h.off & 63) || h.off > ((int64_t)1 << 50) || h.row_off < 0 || h.row_off > ((int64_t)1 << 45))
             return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: head %d: off must be a multiple of 64 bytes, and neither it nor row_off negative", i);
-        if (h.sink < 0 || h.sink > ctx->cfg.max_ctx || h.recent < 0 || h.recent > ctx->cfg.max_ctx || h.budget < 1 || h.budget > h.cap)
+        // (sink and recent may be more than a head has rows: then all stay.  Rows less both of them are a number of 32 bits.)
+        if (h.sink < 0 || h.sink > 1 << 30 || h.recent < 0 || h.recent > 1 << 30 || h.budget < 1 || h.budget > h.cap)
             return hc_fail(ctx, HC_EINVAL, "hc_kvq_create: head %d: budget %d of %d rows, sink %d, recent %d", i, (int)h.budget, (int)h.cap, (int)h.sink, (int)h.recent);
         bytes = std::max(bytes, h.off + (int64_t)136 * h.cap);
         rows = std::max(rows, h.row_off + h.cap);

@@ -33,7 +33,7 @@ def weights(n, kind, g):
     (1, 2, [300, 300], [100, 33], 4, 16, True), (1, 3, [1, 0, 64], [1, 5, 64], 0, 0, True), (2, 2, [2000, 1999, 5, 1023], [1998, 1, 4, 1022], 0, 1, False),
     (1, 1, [1500], [200], 128, 72, True), (1, 2, [40000, 37000], [30000, 129], 64, 64, True), (3, 1, [50000, 12, 36865], [49999, 100, 2000], 100, 0, False),
     (1, 2, [900, 900], [300, 900], 150, 100, True), (1, 1, [40], [64], 50, 50, True), (1, 2, [20000, 9000], [15000, 11000], 5000, 6000, True),
-    (1, 2, [8193, 16385], [8192, 4096], 0, 0, False)])
+    (1, 2, [8193, 16385], [8192, 4096], 0, 0, False), (1, 2, [1, 28], [32, 48], 4, 4096, True), (1, 2, [9000, 40], [9100, 9000], 2 ** 30, 2 ** 30, True)])
 def test_what_stays(kind, B, Hkv, rows, budget, sink, recent, kept):
     heads = B * Hkv
     ctx = U.context(B, Hkv, 2, max(rows) + 100)

@@ -46,8 +46,11 @@ def test_tables(fake):  # noqa: F811
         for kw, text in ((dict(cap=0), "cap 0"), (dict(cap=15), "cap 15"), (dict(cap=-16), "cap"), (dict(cap=4112), "cap 4112")):
             refused(change(2, **kw), hc.HC_ESHAPE, ctx, text)
         for kw, text in ((dict(off=-64), "off"), (dict(off=32), "off"), (dict(row_off=-1), "row_off"), (dict(budget=0), "budget"), (dict(budget=17), "budget"),
-                         (dict(sink=-1), "sink"), (dict(recent=-1), "recent"), (dict(sink=4097), "sink"), (dict(recent=2 ** 31 - 1), "recent"), (dict(off=64), "overlap"), (dict(row_off=63), "overlap"), (dict(off=0), "overlap")):
+                         (dict(sink=-1), "sink"), (dict(recent=-1), "recent"), (dict(sink=2 ** 30 + 1), "sink"), (dict(recent=2 ** 31 - 1), "recent"), (dict(off=64), "overlap"), (dict(row_off=63), "overlap"), (dict(off=0), "overlap")):
             refused(change(1, **kw), hc.HC_EINVAL, ctx, text)
+        # a program's sink and recent rows are the same for contexts shorter than they are
+        for kw in (dict(sink=4097), dict(recent=4097), dict(sink=2 ** 30, recent=2 ** 30)):
+            assert change(1, **kw) == 0, kw
         assert L.hc_kvq_create(ctx, None, C.byref(C.c_void_p())) == hc.HC_EINVAL
         assert L.hc_kvq_create(None, None, None) == hc.HC_ESTATE
         assert L.hc_kvq_destroy(None) == hc.HC_ESTATE
