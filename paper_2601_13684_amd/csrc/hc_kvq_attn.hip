@@ -1,7 +1,11 @@
 // hc_kvq_attn.hip -- attention of the decode token over the cache held in 4 bits (its format: hc_kvq.h), and every row's share of the weights.
 //
-//   t_j = q . K[j] log2(e) / sqrt(128),   p_j = 2^(t_j - m),   out = sum_j p_j V[j] / sum_j p_j,   lse = (m + log2 sum_j p_j) ln 2
+//   s_j = q . K[j],   p_j = 2^((s_j - m) log2(e) / sqrt(128)),   out = sum_j p_j V[j] / sum_j p_j,   lse = m / sqrt(128) + ln sum_j p_j
 //   acc_j <- decay acc_j + (1/G) sum_g p_gj / sum_i p_gi
+//
+// References m are logits as they leave the first product, not scaled: a difference of two is off by half a step of its own, whatever their size, and is scaled
+// after it.  (A scaled logit's rounding is a step of the logit's: from 2^31 binary orders on more than the exponents hold, so that the row's own weight would be
+// infinite, or nothing.)
 //
 // A workgroup takes an equal share of the tiles of 32 rows of all heads one after the other; lengths are on the device, and each
 // wave finds its share by itself.  A wave takes whole tiles, the next one on its way to LDS (asynchronous loads, five to a tile of 4,352 bytes; straight to
@@ -35,9 +39,10 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int KA_BLK = 256, KA_WAVES = KA_BLK / 64;
-constexpr float KA_SCALE = 1.4426950408889634f * 0.08838834764831845f;     // log2(e) / sqrt(128)
+constexpr float KA_SCALE = (float)(1.4426950408889634 * 0.08838834764831845);      // log2(e) / sqrt(128)
+constexpr float KA_ROOT = 0.08838834764831845f;      // 1 / sqrt(128)
 constexpr float KA_LN2 = 0.6931471805599453f;
-constexpr float KA_SLACK = 8.0f;             // a weight is at most 2^8 before the reference moves
+constexpr float KA_SLACK = 62.0f;            // a logit is at most this far above the reference before that moves: its weight is then below 2^8
 constexpr int KA_LEAST = KA_WAVES;           // tiles of a workgroup, where there are so few
 constexpr int KA_START = 16;                 // what beginning a head costs a workgroup, in tiles
 
@@ -58,6 +63,11 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + KQ_TILE - 1) 
 // The work is a line on which every head with rows has KA_START places and then one for each of its tiles; workgroup i has the share [i per, (i + 1) per) of it.
 __device__ __forceinline__ int places_of(int rows) { return rows > 0 ? KA_START + tiles_of(rows) : 0; }
 __device__ __forceinline__ int share(int places, int workgroups) { return max(KA_LEAST, (places + workgroups - 1) / workgroups); }
+
+__device__ __forceinline__ float weight(float s, float ref) { return __builtin_amdgcn_exp2f((s - ref) * KA_SCALE); }
+// What sums of reference `ref` come to for reference `top`.
+__device__ __forceinline__ float moved(float ref, float top) { return exp2f((ref - top) * KA_SCALE); }
+__device__ __forceinline__ float lse_of(float ref, float l) { return l == 0.f ? -INFINITY : fmaf(ref, KA_ROOT, log2f(l) * KA_LN2); }
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x)
@@ -130,7 +140,7 @@ struct Wave {
     uint32_t cap, k_at, v_at, s_at, k_chunk, v_chunk, s_base;
     int n, c_row, s_row;
     bf16x8 Q[4];
-    float ref;                               // weights are 2^(t - ref)
+    float ref;                               // of the weights
     f32x4 L;                                 // their sums, of the columns; four times the same
     f32x4 O[8];
 
@@ -171,7 +181,7 @@ struct Wave {
     }
     __device__ __forceinline__ void reset()
     {
-        ref = dead ? FLT_MAX : -FLT_MAX;                     // (2^(t - FLT_MAX) is nothing)
+        ref = dead ? FLT_MAX : -FLT_MAX;                     // (beside FLT_MAX a logit weighs nothing, or 1, of which the last part of the weights is nothing)
         L = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -244,28 +254,28 @@ struct Wave {
         float p[8], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = fmaf(S[i >> 2][i & 3], KA_SCALE, -ref);
+            p[i] = S[i >> 2][i & 3] - ref;
             top = fmaxf(top, p[i]);
         }
         if (__builtin_amdgcn_ballot_w64(top > KA_SLACK)) {
-            float y = S[0][0] * KA_SCALE;
+            float y = S[0][0];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3] * KA_SCALE);
+            for (int i = 1; i < 8; ++i) y = fmaxf(y, S[i >> 2][i & 3]);
             y = fmaxf(y, __shfl_xor(y, 16));
             y = fmaxf(y, __shfl_xor(y, 32));
             y = fmaxf(y, ref);
-            const float less = exp2f(ref - y);
+            const float less = moved(ref, y);
             ref = y;
             L *= less;
 #pragma unroll
             for (int j = 0; j < 8; ++j) O[j] *= less;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = fmaf(S[i >> 2][i & 3], KA_SCALE, -ref);
+            for (int i = 0; i < 8; ++i) p[i] = S[i >> 2][i & 3] - ref;
         }
         uint32_t P1[8], P2[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float e = __builtin_amdgcn_exp2f(p[i]);
+            const float e = __builtin_amdgcn_exp2f(p[i] * KA_SCALE);
             const float r1 = e - __uint_as_float(__float_as_uint(e) & (G == 8 ? 0xffff0000u : m1));
             if (G == 8) {
                 P1[i] = __float_as_uint(part ? r1 : e);
@@ -453,7 +463,7 @@ __global__ __launch_bounds__(KA_BLK, KQ_WG_PER_CU) void kvq_attn_kernel(AttnArgs
             for (int k = 1; k < KA_WAVES; ++k) m = fmaxf(m, sm_ml[k][g][0]);
 #pragma unroll
             for (int k = 0; k < KA_WAVES; ++k) {
-                const float f = exp2f(sm_ml[k][g][0] - m);
+                const float f = moved(sm_ml[k][g][0], m);
                 o = fmaf(f, sm_o[k][g][d], o);
                 s = fmaf(f, sm_ml[k][g][1], s);
             }
@@ -480,11 +490,11 @@ struct CombineArgs {
     int n;
 };
 
-// (m, l) and (n, k): sums l 2^m and k 2^n
+// (m, l) and (n, k): sums l and k of weights of references m and n
 __device__ __forceinline__ void join(float& m, float& l, float n, float k)
 {
     const float top = fmaxf(m, n);
-    l = l * exp2f(m - top) + k * exp2f(n - top);
+    l = l * moved(m, top) + k * moved(n, top);
     m = top;
 }
 
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 #pragma unroll 4
         for (int i = row; i < count; i += KC_ROWS) {
             const f32x4 x = *reinterpret_cast<const f32x4*>(po + (size_t)i * G * HC_D);
-            const float f = exp2f(sm_w[i] - m);
+            const float f = moved(sm_w[i], m);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
         }
@@ -541,7 +551,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 #pragma unroll
             for (int i = 0; i < KC_ROWS; ++i) x += sm_o[i][tid];
             a.out[(size_t)blockIdx.x * HC_D + tid] = l == 0.f ? 0.f : x / l;       // (no rows: nothing)
-            if (tid == 0) a.lse[blockIdx.x] = l == 0.f ? -INFINITY : (m + log2f(l)) * KA_LN2;
+            if (tid == 0) a.lse[blockIdx.x] = lse_of(m, l);
         }
         return;
     }
@@ -584,7 +594,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
         const int r = chunk.y + k * BLK + tid;
         float x = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) x = fmaf(__builtin_amdgcn_exp2f(fmaf(s[k][g], KA_SCALE, -sm_m[g])), sm_l[g], x);
+        for (int g = 0; g < G; ++g) x = fmaf(weight(s[k][g], sm_m[g]), sm_l[g], x);
         if (r < n) a.acc[row_off + r] = fmaf(old[k], a.decay, x);
     }
 }
@@ -650,13 +660,13 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
         for (int k = 1; k < KS_WAVES; ++k) m = fmaxf(m, sm_ml[k][g][0]);
 #pragma unroll
         for (int k = 0; k < KS_WAVES; ++k) {
-            const float f = exp2f(sm_ml[k][g][0] - m);
+            const float f = moved(sm_ml[k][g][0], m);
             o = fmaf(f, reinterpret_cast<const float*>(&sm_tile[k][0][0])[i], o);
             l = fmaf(f, sm_ml[k][g][1], l);
         }
         x.out[(size_t)bh * G * HC_D + i] = l == 0.f ? 0.f : o / l;       // (no rows: nothing)
         if (i % HC_D == 0) {
-            x.lse[bh * G + g] = l == 0.f ? -INFINITY : (m + log2f(l)) * KA_LN2;
+            x.lse[bh * G + g] = lse_of(m, l);
             sm_all[g][0] = m;
             sm_all[g][1] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
         }
@@ -670,7 +680,7 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
         float mine = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float p = __builtin_amdgcn_exp2f(fmaf(S[b][i >> 2][i & 3], KA_SCALE, -ref)) * part;
+            float p = weight(S[b][i >> 2][i & 3], ref) * part;
             if (G > 4) p = dpp_add<0x124>(p);                    // over the queries: columns repeat every G
             if (G > 2) p = dpp_add<0x122>(p);
             if (G > 1) p = dpp_add<0x121>(p);
