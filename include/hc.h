@@ -527,7 +527,7 @@ hc_status hc_kvq_load(hc_ctx* ctx, const hc_kvq* kvq, const void* arena, const i
 hc_status hc_kvq_append(hc_ctx* ctx, const hc_kvq* kvq, const hc_rope* rope, const void* q, const void* k, const void* v, int64_t q_stride,
                         int64_t k_stride, int64_t v_stride, int32_t in_type, void* q_out, void* arena, int32_t* state, float* acc, void* stream);
 /* hc_decode_attn over this cache: out (dev f32 [B][Hq][128]) and lse (dev f32 [B][Hq]) of q (dev bf16 [B][Hq][128]) over the rows that every head holds;
- * of a head with none, 0 and minus infinity.  out must not overlap q.  acc (if not NULL) of row j becomes  decay acc + (1/G) sum over the head's queries of its weight,
+ * of a head with none, 0 and minus infinity; of a query that is not finite, over one row or more, NaN.  out must not overlap q.  acc (if not NULL) of row j becomes  decay acc + (1/G) sum over the head's queries of its weight,
  * decay in 0 .. 1 (not read where acc is NULL).  Rows' values are taken exactly, everything else is 32-bit: logits of any size that
  * 32 bits hold as a dot product (below 2^128, not yet divided by sqrt(128)) are weighed by their differences.  Sums over the rows are divided at the end: finite
  * values of V beyond 2^90 may come out as infinities. */

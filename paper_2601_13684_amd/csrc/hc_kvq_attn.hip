@@ -550,7 +550,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
             float x = 0.f;
 #pragma unroll
             for (int i = 0; i < KC_ROWS; ++i) x += sm_o[i][tid];
-            a.out[(size_t)blockIdx.x * HC_D + tid] = l == 0.f ? 0.f : x / l;       // (no rows: nothing)
+            a.out[(size_t)blockIdx.x * HC_D + tid] = count == 0 ? 0.f : x / l;     // (no rows: nothing; nothing but logits of minus infinity: no number)
             if (tid == 0) a.lse[blockIdx.x] = lse_of(m, l);
         }
         return;
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
         for (int d = 32; d > 0; d >>= 1) join(m, l, __shfl_xor(m, d), __shfl_xor(l, d));
         if (lane == 0) {
             sm_m[g] = m;
-            sm_l[g] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
+            sm_l[g] = 1.0f / (l * (float)G);
         }
     }
     __syncthreads();
@@ -664,11 +664,11 @@ __global__ __launch_bounds__(KS_BLK) void kvq_attn_short_kernel(ShortArgs x)
             o = fmaf(f, reinterpret_cast<const float*>(&sm_tile[k][0][0])[i], o);
             l = fmaf(f, sm_ml[k][g][1], l);
         }
-        x.out[(size_t)bh * G * HC_D + i] = l == 0.f ? 0.f : o / l;       // (no rows: nothing)
+        x.out[(size_t)bh * G * HC_D + i] = n == 0 ? 0.f : o / l;         // (no rows: nothing; nothing but logits of minus infinity: no number)
         if (i % HC_D == 0) {
             x.lse[bh * G + g] = lse_of(m, l);
             sm_all[g][0] = m;
-            sm_all[g][1] = l == 0.f ? 0.f : 1.0f / (l * (float)G);
+            sm_all[g][1] = 1.0f / (l * (float)G);
         }
     }
     if (!WEIGHTS) return;
