@@ -350,10 +350,11 @@ def _as_stream(stream, device):
 class _Made:
     """When and where an object's buffers were allocated, on the then current stream.  Another one that they are used on waits for what was queued
     before they were there (their fill, and the last use of their memory), and their memory is not given away before its work is through.  (While a
-    graph is captured neither is possible; a capture begins on an idle device, and its buffers have to outlive its replays.)"""
+    graph is captured neither is possible; a capture begins on an idle device, and its buffers have to outlive its replays.)  With known=False the buffers are
+    there already, from whatever stream: any may be another one."""
 
-    def __init__(self, device):
-        self.device = device
+    def __init__(self, device, known: bool = True):
+        self.device, self.known = device, known
         self.stream = torch.cuda.current_stream(device)
         self.event = None
         if not torch.cuda.is_current_stream_capturing():
@@ -363,7 +364,7 @@ class _Made:
     def used_on(self, stream, *buffers: torch.Tensor) -> None:
         """Before a call on this stream (None: the current one)."""
         s = _as_stream(stream, self.device)
-        if self.event is None or s.cuda_stream == self.stream.cuda_stream:
+        if self.event is None or (self.known and s.cuda_stream == self.stream.cuda_stream):
             return
         with torch.cuda.stream(s):
             if torch.cuda.is_current_stream_capturing():
@@ -438,8 +439,9 @@ class QuantTable:
 
 class QuantCache:
     """One layer's cache held in 4 bits: bytes, rows and positions of its heads on the device, with ``weights`` the attention that every row has drawn, and the
-    work buffer of attention and eviction (``work``: another's, of at least the table's work_bytes, where their calls do not overlap).  Its calls may be put on any
-    stream; on different streams they are put in order by the caller."""
+    work buffer of attention and eviction (``work``: another cache's, or a tensor of the program's, of at least the table's work_bytes, where their calls do not
+    overlap; the program's own is there for the stream that is current when the cache is made).  Its calls may be put on any stream; on different streams they are put in
+    order by the caller."""
 
     def __init__(self, table: QuantTable, weights: bool = True, work: Optional[torch.Tensor] = None):
         self.ctx, self.table = table.ctx, table
@@ -448,11 +450,17 @@ class QuantCache:
         self.state = torch.zeros((len(table.heads), 2), dtype=torch.int32, device=dev)
         self.acc = torch.zeros((table.rows,), dtype=torch.float32, device=dev) if weights else None
         self.work = torch.empty((table.work_bytes(),), dtype=torch.uint8, device=dev) if work is None else work
-        self._own = [self.arena, self.state] + ([] if self.acc is None else [self.acc]) + ([self.work] if work is None else [])
+        self._own = [self.arena, self.state] + ([] if self.acc is None else [self.acc])
         self.made = _Made(dev)
+        if work is None:
+            self.work.made = self.made                   # (for whom it is lent to)
+        self._work_made = getattr(self.work, "made", None) or _Made(dev, known=False)
 
-    def _used_on(self, stream) -> None:
-        self.made.used_on(stream, *self._own)
+    def _used_on(self, stream, work: bool = False) -> None:
+        if work and self._work_made is not self.made:
+            self._work_made.used_on(stream, self.work)
+            work = False
+        self.made.used_on(stream, *self._own, *((self.work,) if work else ()))
 
     def store(self, prompt: Prompt, first: List[int], count: List[int], stream=None) -> None:
         """Rows first[b] .. of every sequence of the prompt's buffer, count[b] of them, behind what the cache holds (hc_kvq_store)."""
@@ -486,7 +494,7 @@ class QuantCache:
                 out = torch.empty((cfg.B, cfg.Hq, D), dtype=torch.float32, device=self.ctx.device)
             if lse is None:
                 lse = torch.empty((cfg.B, cfg.Hq), dtype=torch.float32, device=self.ctx.device)
-        self._used_on(stream)
+        self._used_on(stream, work=True)
         hc.hc_kvq_attn(self.ctx.handle, self.table.handle, self.arena, self.state, q, out, lse, self.acc, decay, self.work, self.work.numel(), stream)
         return out, lse
 
@@ -495,7 +503,7 @@ class QuantCache:
         they were."""
         if self.acc is None or to.acc is None:
             raise ValueError("eviction goes by the rows' weights: both caches need them")
-        self._used_on(stream)
+        self._used_on(stream, work=True)
         to._used_on(stream)
         hc.hc_kvq_evict(self.ctx.handle, self.table.handle, self.arena, self.state, self.acc, to.table.handle, to.arena, to.state, to.acc, kept, self.work,
                         self.work.numel(), stream)
