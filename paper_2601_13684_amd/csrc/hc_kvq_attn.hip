@@ -498,7 +498,7 @@ __device__ __forceinline__ void join(float& m, float& l, float n, float k)
     m = top;
 }
 
-constexpr int KC_FILL = 1024;                // workgroups of 512 threads that the GPU holds at once
+constexpr int KC_PER_CU = 3;                 // workgroups of 512 threads that a compute unit holds at once: 67 registers, seven waves a SIMD
 
 // The first n G workgroups: output and lse of a query head each, BLK / 32 partial results at a time, 32 lanes of four values to each.  Those behind them:
 // KQ_CHUNK rows' weights each.
@@ -602,7 +602,8 @@ __global__ __launch_bounds__(BLK) void kvq_combine_kernel(CombineArgs a)
 // ---- heads of few rows: all of one in a workgroup, and no second launch --------------------------------------------------------------------
 //
 // Where no head of a table has room for more than KS_BUFS KS_ROWS = 1,024 rows; where it is a half or a quarter of that, waves have fewer buffers, and a compute unit holds
-// two or four workgroups (4,096 heads of 100 rows 70 us with four buffers, 30 with one).  us, this way / split and joined: 500 rows of two heads 6.5 / 5.0 + 3.9 in two launches, 200 rows of eight
+// more workgroups: one with four buffers, two with two, with one buffer three (by registers; four without weights in groups of at most four).  4,096 heads of 100 rows, us with four
+// buffers / one: groups of one 63 / 25, of four 74 / 30, of eight 85 / 41; with weights 68 / 28, 77 / 36, 89 / 44.  us, this way / split and joined: 500 rows of two heads 6.5 / 5.0 + 3.9 in two launches, 200 rows of eight
 // heads 4.8 / 5.1 + 4.8, 1,000 rows of eight heads 7.6 / 5.1 + 5.1, of 512 heads 19.8 / 20.2 + 4.2, with weights 23.9 / 23.1 + 13.4.
 
 constexpr int KS_BLK = 512, KS_WAVES = KS_BLK / 64;
@@ -713,10 +714,11 @@ hc_status launch(hc_ctx* ctx, const AttnArgs& a, const CombineArgs& c, int longe
     if (a.logits) kvq_attn_kernel<G, true><<<grid, block, 0, st>>>(a);
     else kvq_attn_kernel<G, false><<<grid, block, 0, st>>>(a);
     HC_HIP(ctx, hipGetLastError());
-    // Where there are more query heads than the GPU holds workgroups of 512 threads, each has few partial results, and small workgroups take them all at once:
-    // 512 KV heads of 4,096 rows in groups of four 10.6 us with 512 threads, 4.2 with 128; with weights 21.6 and 14.6.
+    // Where there are more query heads than the GPU holds workgroups of 512 threads, each has few partial results, and small workgroups take them all at once.
+    // KV heads of 1,536 rows in groups of four, us with 512 / 128 threads, and with weights: 64 of them 4.2 / 4.3, 4.2 / 5.0; 128: 4.3 / 4.2, 4.8 / 5.3; 160: 5.1 / 4.1,
+    // 6.8 / 6.0; 192, the last that fit: 5.1 / 4.2, 8.0 / 6.2; 224: 6.6 / 4.2, 8.3 / 6.4; 512 of 4,096 rows 10.6 / 4.3, 21.1 / 15.2.
     const dim3 joins((unsigned)(a.n * G + (a.logits ? n_chunks : 0)));
-    if (a.n * G > KC_FILL) kvq_combine_kernel<G, 128><<<joins, dim3(128), 0, st>>>(c);
+    if (a.n * G > KC_PER_CU * ctx->n_cu) kvq_combine_kernel<G, 128><<<joins, dim3(128), 0, st>>>(c);
     else kvq_combine_kernel<G, 512><<<joins, dim3(512), 0, st>>>(c);
     HC_HIP(ctx, hipGetLastError());
     return HC_OK;

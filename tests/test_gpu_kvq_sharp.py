@@ -96,8 +96,8 @@ def drawn(n, most, seed):
 
 
 @pytest.mark.parametrize("acc", [True, False])
-@pytest.mark.parametrize("heads,G", [(1024, 1), (1028, 1), (256, 4), (260, 4), (128, 8), (132, 8)])
-def test_about_1024_query_heads(heads, G, acc):
+@pytest.mark.parametrize("heads,G", [(768, 1), (772, 1), (192, 4), (196, 4), (96, 8), (100, 8), (1024, 1), (1028, 1), (256, 4), (260, 4), (128, 8), (132, 8)])
+def test_many_query_heads(heads, G, acc):
     """On either side of what workgroups of either size join: heads of up to 1,500 rows, some without any."""
     rows = drawn(heads, 1500, heads)
     every_row_once(rows, [up(max(n, 1030 if i == 5 else 1)) for i, n in enumerate(rows)], G, acc, B=heads // 4, runs=(1, 32))
