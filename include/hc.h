@@ -481,9 +481,12 @@ hc_status hc_append_rope(hc_ctx* ctx, hc_layer* layer, const hc_rope* rope, cons
 
 /* ---- The cache held in 4 bits --------------------------------------------------------------------------------------------------
  * A second kind of cache, beside the bf16 arena that the calls above read: 136 bytes for a K row and a V row in place of 512, every head of it with a
- * capacity and a length of its own, and every row with the attention that it has drawn so far, by which heads are brought to a budget.
+ * capacity and a length of its own, and every row with the attention that it has drawn so far, by which heads are brought to a budget.  A layer's context is in one or
+ * the other: hc_layer, hc_decode_step, the monitor, satellites and the host tier know the arena alone.
  *     hc_kvq_store  (a prompt's rows, from the kv_prefill of hc_prefill_rope)  ->  then for every token
  *     hc_kvq_append  ->  hc_kvq_attn,   and from time to time   hc_kvq_evict  into another cache.   hc_kvq_load gives rows back as bf16.
+ * A later chunk of a prompt attends by hc_prefill_attn as long as rows are at their positions, in its own buffer or where hc_kvq_load puts them.  After an eviction they
+ * no longer are, and no call computes a chunk's attention over what is left: its tokens go one by one (hc_kvq_append, hc_kvq_attn).
  *
  * A row of 128 values is 64 bytes of codes and 4 scale bytes s, one per 32 values.  Element i is bits 4 (i % 8) .. 4 (i % 8) + 3 of dword i / 8: the sign
  * (bit 3) and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (0 .. 7), times 2^(s - 127).  s is the smallest, 2 at least, with no value beyond 7 of these units; codes are

@@ -18,11 +18,11 @@
 // bf16 leaves, in two steps, so that the weights lose nothing (8 + 8 + 8 bits): columns g, G + g, 2 G + g for the parts of query head g, added at the end.
 // Groups of eight take a second product for the last part.
 //
-// Bound by memory where rows are many: 224K rows of eight heads 39.0 us (250 MB, 6.4 TB/s; a plain read of 1 GiB runs at 5.9) and 4.3 for the partial results; in
-// groups of eight the same within 2 us, so that the products and the codes' conversion, 214 vector instructions a tile, stay hidden.  With weights 45.1 +
-// 11.9: logits go through memory, 32 bytes a row in groups of four against 136 for the row.  Two such heads and six of 1,024 to 8,192 rows 13.8 + 5.6, with weights
-// 15.3 + 6.4; 16 ragged sequences of 1 to 32K rows, four heads in groups of eight, with weights 21.6 + 9.4: about 5 us of either pass are launch, the search for its
-// share and the first loads.  512 heads of 4,096 rows 50 to 54 + 4.2 us (285 MB).  Few rows: 500 rows of two heads 5.8 us in one launch.
+// Bound by memory where rows are many: 224K rows of eight heads 39.6 us (250 MB, 6.3 TB/s; a plain read of 1 GiB runs at 5.9) and 4.6 for the partial results, the
+// products and the codes' conversion, 222 vector instructions a tile, all but hidden; in groups of eight 43 us.  With weights 45.1 +
+// 12.0: logits go through memory, 32 bytes a row in groups of four against 136 for the row.  Two such heads and six of 1,024 to 8,192 rows 14.0 + 5.8, with weights
+// 15.5 + 6.4; 16 ragged sequences of 1 to 32K rows, four heads in groups of eight, with weights 21.5 + 9.8: about 5 us of either pass are launch, the search for its
+// share and the first loads.  512 heads of 4,096 rows 50.5 + 4.2 us (285 MB).  Few rows: 500 rows of two heads 6.0 us in one launch.
 #include <float.h>
 #include <math.h>
 
@@ -44,7 +44,9 @@ constexpr float KA_ROOT = 0.08838834764831845f;      // 1 / sqrt(128)
 constexpr float KA_LN2 = 0.6931471805599453f;
 constexpr float KA_SLACK = 62.0f;            // a logit is at most this far above the reference before that moves: its weight is then below 2^8
 constexpr int KA_LEAST = KA_WAVES;           // tiles of a workgroup, where there are so few
-constexpr int KA_START = 16;                 // what beginning a head costs a workgroup, in tiles
+// What beginning a head costs a workgroup, in tiles.  us of the split pass with 6, 12 / 16 / 20, 28: 16 ragged sequences in groups of eight 22.5, 19.7 / 19.7 / 19.7, 19.9, with
+// weights 23.4, 21.8 / 21.7 / 21.6, 21.9; two heads of 224K rows and six short ones 15.0, 14.2 / 14.2 / 14.0, 14.0.
+constexpr int KA_START = 16;
 
 struct AttnArgs {
     const uint8_t* arena;
